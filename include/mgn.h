@@ -391,6 +391,143 @@ int mgn_pec_step(mgn_ctx* ctx, const mgn_dgraph* g, const float* params,
                  const float* efeat, float* y_next, int32_t first,
                  void* workspace, size_t ws_bytes, void* stream);
 
+/* ---- row operators ------------------------------------------------------ */
+/* Building blocks for layers that a model adds beside the MGN processor's own
+ * fused MLPs (wider MLPs on the latents, steps between the blocks of a
+ * residual stream): an 8-bit quantiser, the product of block-scaled 8-bit
+ * matrices, and the step norm -> gate -> residual -> norm with its reverse.
+ * They need no context; like the calls above they are asynchronous on
+ * `stream`, run on the current device, allocate nothing and have fixed
+ * summation orders (results are bitwise reproducible).  Row tensors are
+ * row-major with a leading dimension in elements (ld >= cols) and any
+ * alignment of their element type; rows x ld may exceed 2^31. */
+
+/* Types of row tensors: MGN_FP32, MGN_BF16.  8-bit formats: */
+#define MGN_E4M3 2 /* 4 exponent, 3 mantissa bits, largest 448, no infinity */
+#define MGN_E5M2 3 /* 5 exponent, 2 mantissa bits, largest finite 57344 */
+
+/* A matrix of 8-bit numbers with one scale for each block of block_rows (1 or
+ * 128) rows and 128 columns; blocks start at multiples of these, the last may
+ * be smaller.  Value (r, c) is q[r ld + c] * scale[(c / 128) R + r / block_rows],
+ * R = ceil(rows / block_rows).  q is 16-byte aligned, ld a multiple of 16, and
+ * the bytes from cols to the next multiple of 16 are zero (mgn_quant8 writes
+ * them so). */
+typedef struct mgn_mat8 {
+  const uint8_t* q;
+  const float* scale;
+  int64_t rows, cols, ld;
+  int32_t format;     /* MGN_E4M3 or MGN_E5M2 */
+  int32_t block_rows; /* 1 or 128 */
+} mgn_mat8;
+
+/* Quantises x [rows][cols] (MGN_FP32 or MGN_BF16).  The scale of a block is
+ * the float32 nearest amax / F (F the format's largest number), at least
+ * 2^-126; an element becomes the 8-bit number nearest x / scale, ties to even.
+ * A block that holds an infinity or a NaN gets a NaN scale and zero numbers.
+ * q, scale: x as an mgn_mat8 of that block_rows (NULL: not wanted).
+ * qt, scale_t: the transpose [cols][rows], block_rows 1 with blocks of 128
+ * rows of one column of x, block_rows 128 with the same blocks as q (NULL: not
+ * wanted).  colsum (nullable): [cols] sums of x over its rows (the gradient of
+ * a bias), added to what is there with accumulate != 0.
+ * The workspace is needed for colsum only (mgn_quant8_workspace).
+ * Errors: ARG, SHAPE (2^31 rows or columns), WORKSPACE, DEVICE. */
+int mgn_quant8_workspace(int64_t rows, int64_t cols, size_t* ws_bytes);
+int mgn_quant8(const void* x, int32_t x_type, int64_t rows, int64_t cols, int64_t ldx,
+               int32_t format, int32_t block_rows, uint8_t* q, int64_t ldq, float* scale,
+               uint8_t* qt, int64_t ldqt, float* scale_t, float* colsum, int32_t accumulate,
+               void* workspace, size_t ws_bytes, void* stream);
+
+/* What mgn_matmul8 does with the sums. */
+#define MGN_ACT_NONE 0
+#define MGN_ACT_RELU 1      /* max(v, 0); a NaN stays a NaN */
+#define MGN_ACT_RELU_GRAD 2 /* v where aux > 0, else 0 (aux: the saved output
+                               of the forward's ReLU) */
+typedef struct mgn_epilogue {
+  const float* bias; /* [b->rows], added before act; nullable */
+  int32_t act;       /* MGN_ACT_* */
+  int32_t aux_type;  /* MGN_FP32 or MGN_BF16 (MGN_ACT_RELU_GRAD only) */
+  const void* aux;   /* [a->rows][ldaux] */
+  int64_t ldaux;
+  int32_t accumulate; /* 1: add to c (after act) */
+} mgn_epilogue;
+
+/* c[m][n] = act(sum_k a[m][k] b[n][k] + bias[n]), c [a->rows][b->rows] of type
+ * MGN_FP32 or MGN_BF16.  A block of 128 products is summed, scaled, and added to
+ * a float32 sum.  For an MGN_FP32 c the block is summed in float32.  For an
+ * MGN_BF16 c it is summed by the 8-bit matrix instructions, twice as fast, which
+ * add eight products at a time and cut each off 2^-13 below the largest of the
+ * eight (1.5e-5 of a block's sum on normal values, a hundredth of the rounding
+ * of c).  A layer
+ * y = x W^T takes a = rows of x, b = rows of W; its input gradient dy W takes
+ * a = rows of dy, b = the transpose of W; its weight gradient dy^T x takes the
+ * transposes of dy and x, whose blocks run along the rows.  epilogue NULL: none.
+ * cols 0 gives zero sums.  A workspace of mgn_matmul8_workspace bytes (which
+ * may be 0) splits long sums over the device.
+ * Errors: ARG, SHAPE (a->cols != b->cols, 2^31 rows or columns), WORKSPACE,
+ * DEVICE. */
+int mgn_matmul8_workspace(int64_t a_rows, int64_t b_rows, int64_t cols, size_t* ws_bytes);
+int mgn_matmul8(const mgn_mat8* a, const mgn_mat8* b, const mgn_epilogue* epilogue,
+                int32_t c_type, void* c, int64_t ldc, void* workspace, size_t ws_bytes,
+                void* stream);
+
+/* The step between two blocks of a residual stream x whose block gave b:
+ *   p = post(b),  y = skip x + scale gate p,  z = pre(y),
+ * z being the next block's input.  post and pre are one of */
+#define MGN_NORM_NONE 0
+#define MGN_NORM_LAYER 1 /* (v - mean) / sqrt(var + eps) * gamma + beta, biased variance */
+#define MGN_NORM_RMS 2   /* v / sqrt(mean(v^2) + eps) * gamma + beta */
+#define MGN_NORM_MAX_COLS 16384
+typedef struct mgn_norm_gate {
+  int64_t rows;
+  int32_t cols;     /* 1 .. MGN_NORM_MAX_COLS */
+  int32_t x_type;   /* of x, y, dy, dx: MGN_FP32 or MGN_BF16 */
+  int32_t b_type;   /* of b, z, dz, db */
+  int32_t post, pre; /* MGN_NORM_* (pre MGN_NORM_NONE: no z) */
+  float eps;         /* > 0 */
+  float skip, scale;
+  /* float32 [cols]; NULL: gamma 1, beta 0 */
+  const float *post_gamma, *post_beta, *pre_gamma, *pre_beta;
+  /* gate: float32 [n_gates][cols].  n_gates 0: no gate (1); 1: one for all
+   * rows; rows: one for each row; any number with gate_ptr (int32 device
+   * [n_gates + 1], ascending): gate g for rows [gate_ptr[g], gate_ptr[g + 1]);
+   * rows outside of [gate_ptr[0], gate_ptr[n_gates]) are neither read nor
+   * written. */
+  const float* gate;
+  const int32_t* gate_ptr;
+  int64_t n_gates;
+} mgn_norm_gate;
+
+/* A row tensor of the types above. */
+typedef struct mgn_rows {
+  void* data;
+  int64_t ld;
+} mgn_rows;
+
+/* y and z from x and b; stats (nullable: inference) [rows][4] float32 keeps
+ * mean and 1 / standard deviation of both norms for the reverse.  y may be x
+ * and z may be b.  z is formed from the unrounded y.
+ * Errors: ARG, SHAPE, DEVICE. */
+int mgn_norm_gate_forward(const mgn_norm_gate* op, mgn_rows x, mgn_rows b, mgn_rows y,
+                          mgn_rows z, float* stats, void* stream);
+
+/* Gradients of the parameters, float32; each nullable; added to what is there
+ * with accumulate != 0.  dgate is [n_gates][cols]. */
+typedef struct mgn_norm_gate_grads {
+  float *post_gamma, *post_beta, *pre_gamma, *pre_beta, *gate;
+  int32_t accumulate;
+} mgn_norm_gate_grads;
+
+/* Reverse of mgn_norm_gate_forward: from x, b and stats of the forward and
+ * the gradients dy of y and dz of z (dy.data NULL: zero; dz.data NULL: zero)
+ * the gradients dx, db and those of grads.  dx may be dy or x, db may be dz or
+ * b (with the same ld).
+ * Errors: ARG, SHAPE, WORKSPACE, DEVICE. */
+int mgn_norm_gate_workspace(int64_t rows, int32_t cols, size_t* ws_bytes);
+int mgn_norm_gate_backward(const mgn_norm_gate* op, mgn_rows x, mgn_rows b,
+                           const float* stats, mgn_rows dy, mgn_rows dz, mgn_rows dx,
+                           mgn_rows db, const mgn_norm_gate_grads* grads, void* workspace,
+                           size_t ws_bytes, void* stream);
+
 /* Per-kernel timing for benchmarks.  While enabled, every kernel launch of
  * the context is bracketed by two HIP events recorded on the caller's stream.
  * mgn_profile_collect waits for the last recorded event, then fills, for up

@@ -8,6 +8,8 @@ raises, there is no fallback.
 """
 from __future__ import annotations
 
+import collections
+import contextlib
 import ctypes as C
 import os
 
@@ -19,7 +21,11 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.environ.get("MGN_LIB") or os.path.join(HERE, "libmgn.so")
 
 OK, ERR_ARG, ERR_RANGE, ERR_SHAPE, ERR_WORKSPACE, ERR_STATE, ERR_DEVICE, ERR_NOMEM = 0, -1, -2, -3, -4, -5, -6, -7
-FP32, BF16 = 0, 1
+FP32, BF16, E4M3, E5M2 = 0, 1, 2, 3
+FORMATS = {"e4m3": E4M3, "e5m2": E5M2}
+ACTS = {"none": 0, "relu": 1, "relu_grad": 2}
+NORMS = {"none": 0, "layer": 1, "rms": 2}
+NORM_MAX_COLS = 16384  # MGN_NORM_MAX_COLS of include/mgn.h
 EULER, HEUN2, MIDPOINT, HEUN3, RK4, RALSTON2, RALSTON3 = 0, 1, 2, 3, 4, 5, 6
 SCHEMES = {"euler": EULER, "heun2": HEUN2, "midpoint": MIDPOINT, "heun3": HEUN3, "rk4": RK4,
            "ralston2": RALSTON2, "ralston3": RALSTON3}
@@ -58,6 +64,33 @@ class Adam(C.Structure):
         super().__init__(lr_start, lr_end, decay_steps, beta1, beta2, eps)
 
 
+class CMat8(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("scale", C.c_void_p), ("rows", C.c_int64), ("cols", C.c_int64),
+                ("ld", C.c_int64), ("format", C.c_int32), ("block_rows", C.c_int32)]
+
+
+class Epilogue(C.Structure):
+    _fields_ = [("bias", C.c_void_p), ("act", C.c_int32), ("aux_type", C.c_int32), ("aux", C.c_void_p),
+                ("ldaux", C.c_int64), ("accumulate", C.c_int32)]
+
+
+class CNormGate(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("cols", C.c_int32), ("x_type", C.c_int32), ("b_type", C.c_int32),
+                ("post", C.c_int32), ("pre", C.c_int32), ("eps", C.c_float), ("skip", C.c_float),
+                ("scale", C.c_float), ("post_gamma", C.c_void_p), ("post_beta", C.c_void_p),
+                ("pre_gamma", C.c_void_p), ("pre_beta", C.c_void_p), ("gate", C.c_void_p),
+                ("gate_ptr", C.c_void_p), ("n_gates", C.c_int64)]
+
+
+class Rows(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("ld", C.c_int64)]
+
+
+class CNormGateGrads(C.Structure):
+    _fields_ = [("post_gamma", C.c_void_p), ("post_beta", C.c_void_p), ("pre_gamma", C.c_void_p),
+                ("pre_beta", C.c_void_p), ("gate", C.c_void_p), ("accumulate", C.c_int32)]
+
+
 _lib = None
 
 EXPORTS = [
@@ -66,7 +99,8 @@ EXPORTS = [
     "mgn_partition", "mgn_extract_patch", "mgn_patch_union", "mgn_patch_copy_maps", "mgn_ctx_create",
     "mgn_ctx_destroy", "mgn_forward", "mgn_forward_noalloc", "mgn_backward", "mgn_integrate_step",
     "mgn_pec_step", "mgn_patch_step", "mgn_adam_lr", "mgn_adam_step", "mgn_train_step", "mgn_scheme_stages", "mgn_version", "mgn_last_error", "mgn_profile_enable",
-    "mgn_profile_collect",
+    "mgn_profile_collect", "mgn_quant8_workspace", "mgn_quant8", "mgn_matmul8_workspace", "mgn_matmul8",
+    "mgn_norm_gate_forward", "mgn_norm_gate_workspace", "mgn_norm_gate_backward",
 ]
 
 
@@ -109,6 +143,15 @@ def lib():
         "mgn_last_error": (C.c_char_p, []),
         "mgn_profile_enable": (C.c_int, [vp, i32]),
         "mgn_profile_collect": (C.c_int, [vp, i32, vp, vp, vp, P(i32)]),
+        "mgn_quant8_workspace": (C.c_int, [i64, i64, P(C.c_size_t)]),
+        "mgn_quant8": (C.c_int, [vp, i32, i64, i64, i64, i32, i32, vp, i64, vp, vp, i64, vp, vp, i32, vp, C.c_size_t,
+                                 vp]),
+        "mgn_matmul8_workspace": (C.c_int, [i64, i64, i64, P(C.c_size_t)]),
+        "mgn_matmul8": (C.c_int, [P(CMat8), P(CMat8), P(Epilogue), i32, vp, i64, vp, C.c_size_t, vp]),
+        "mgn_norm_gate_forward": (C.c_int, [P(CNormGate), Rows, Rows, Rows, Rows, vp, vp]),
+        "mgn_norm_gate_workspace": (C.c_int, [i64, i32, P(C.c_size_t)]),
+        "mgn_norm_gate_backward": (C.c_int, [P(CNormGate), Rows, Rows, vp, Rows, Rows, Rows, Rows, P(CNormGateGrads),
+                                             vp, C.c_size_t, vp]),
     }
     for name, (res, args) in sig.items():
         f = getattr(L, name)
@@ -483,6 +526,297 @@ def scheme_stages(scheme):
     if n < 0:
         raise MgnError(n, last_error())
     return n
+
+
+# ------------------------------------------------------- row operators
+# Inputs of these may be slices of wider tensors: any row stride, columns next
+# to each other.  Outputs that are not given are allocated, and scratch is
+# taken from torch's allocator for the call.
+def _row_type(t, name):
+    torch = _torch()
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dim() != 2:
+        raise MgnError(ERR_ARG, f"{name} must be a two-dimensional device tensor")
+    if t.dtype == torch.float32:
+        return FP32
+    if t.dtype == torch.bfloat16:
+        return BF16
+    raise MgnError(ERR_ARG, f"{name} must be float32 or bfloat16, got {t.dtype}")
+
+
+def _row_ld(t, name, shape=None):
+    """Leading dimension of a row tensor (its columns have to be adjacent)."""
+    if shape is not None and tuple(t.shape) != shape:
+        raise MgnError(ERR_ARG, f"{name} has shape {tuple(t.shape)}, expected {shape}")
+    r, c = t.shape
+    if c > 1 and t.stride(1) != 1:
+        raise MgnError(ERR_ARG, f"{name}: the columns of a row must be adjacent")
+    ld = t.stride(0) if r > 1 else c
+    if r > 1 and ld < c:
+        raise MgnError(ERR_ARG, f"{name}: rows overlap (stride {ld} for {c} columns)")
+    return max(ld, c)
+
+
+def _vector(t, name, n, device):
+    torch = _torch()
+    if t is None:
+        return None
+    p = _dptr(t, torch.float32, name=name)
+    if t.numel() != n:
+        raise MgnError(ERR_ARG, f"{name} has {t.numel()} values, expected {n}")
+    if t.device != device:
+        raise MgnError(ERR_ARG, f"{name} is on {t.device}, expected {device}")
+    return p
+
+
+def _on(device, stream, *tensors):
+    """(context manager, stream pointer): the tensors' device made current,
+    and the tensors kept from reuse until a stream that is not the current one
+    has done its work."""
+    torch = _torch()
+    guard = contextlib.nullcontext() if device.index == torch.cuda.current_device() else torch.cuda.device(device)
+    current = torch.cuda.current_stream(device)
+    if stream is None or stream == current:
+        return guard, current.cuda_stream
+    if stream.device != device:
+        raise MgnError(ERR_ARG, f"the stream is of {stream.device}, the tensors are on {device}")
+    for t in tensors:
+        if t is not None:
+            t.record_stream(stream)
+    return guard, stream.cuda_stream
+
+
+def _scratch(nbytes, device):
+    return _torch().empty(nbytes, dtype=_torch().uint8, device=device) if nbytes else None
+
+
+def _at(t):
+    return None if t is None else t.data_ptr()
+
+
+class Mat8:
+    """An mgn_mat8 of include/mgn.h: q, a float8_e4m3fn or float8_e5m2 tensor
+    [rows][ld >= cols], and its scales [ceil(cols / 128)][ceil(rows /
+    block_rows)] in float32."""
+    __slots__ = ("q", "scale", "rows", "cols", "block_rows", "struct")
+
+    def __init__(self, q, scale, cols=None, block_rows=1):
+        torch = _torch()
+        if not isinstance(q, torch.Tensor) or not q.is_cuda or q.dim() != 2:
+            raise MgnError(ERR_ARG, "q must be a two-dimensional device tensor")
+        if q.dtype == torch.float8_e4m3fn:
+            fmt = E4M3
+        elif q.dtype == torch.float8_e5m2:
+            fmt = E5M2
+        else:
+            raise MgnError(ERR_ARG, f"q must be float8_e4m3fn or float8_e5m2, got {q.dtype}")
+        rows, width = q.shape
+        cols = width if cols is None else int(cols)
+        if block_rows not in (1, 128):
+            raise MgnError(ERR_ARG, f"blocks of {block_rows} rows (1 or 128)")
+        ld = _row_ld(q, "q") if rows > 1 else -(-width // 16) * 16
+        if not 0 <= cols <= width or (width < -(-cols // 16) * 16 and rows > 0):
+            raise MgnError(ERR_ARG, f"q has {width} columns for {cols}: rows are padded to multiples of 16")
+        want = (-(-cols // 128), -(-rows // block_rows))
+        if not isinstance(scale, torch.Tensor) or scale.dtype != torch.float32 or tuple(scale.shape) != want \
+                or scale.device != q.device or not scale.is_contiguous():
+            raise MgnError(ERR_ARG, f"scale must be a contiguous float32 tensor of shape {want} on {q.device}")
+        self.q, self.scale, self.rows, self.cols, self.block_rows = q, scale, rows, cols, block_rows
+        self.struct = CMat8(q.data_ptr(), scale.data_ptr(), rows, cols, ld, fmt, block_rows)
+
+
+Quantised = collections.namedtuple("Quantised", "rows columns colsum")
+
+
+def mgn_quant8(x, format="e4m3", block_rows=1, rowwise=True, transposed=False, colsum=False, accumulate=False,
+               stream=None):
+    """Quantises x [rows][cols] to 8 bits with a scale for each block of
+    block_rows x 128 (see include/mgn.h).  Returns (rows, columns, colsum): x
+    and its transpose as Mat8, or None, and the sums over x's rows: a new
+    tensor with colsum=True, or the given one (added to with accumulate)."""
+    torch = _torch()
+    xt = _row_type(x, "x")
+    if format not in FORMATS:
+        raise MgnError(ERR_ARG, f"unknown 8-bit format {format!r}")
+    if block_rows not in (1, 128):
+        raise MgnError(ERR_ARG, f"blocks of {block_rows} rows (1 or 128)")
+    r, c = x.shape
+    dev, f8 = x.device, torch.float8_e4m3fn if format == "e4m3" else torch.float8_e5m2
+    q = s = qt = st = sums = ws = None
+    if rowwise:
+        q = torch.empty((r, -(-c // 16) * 16), dtype=f8, device=dev)
+        s = torch.empty((-(-c // 128), -(-r // block_rows)), dtype=torch.float32, device=dev)
+    if transposed:
+        qt = torch.empty((c, -(-r // 16) * 16), dtype=f8, device=dev)
+        st = torch.empty((-(-r // 128), -(-c // block_rows)), dtype=torch.float32, device=dev)
+    if isinstance(colsum, torch.Tensor):
+        sums = colsum
+        _vector(sums, "colsum", c, dev)
+    elif colsum:
+        if accumulate:
+            raise MgnError(ERR_ARG, "accumulate needs the sums to add to")
+        sums = torch.empty(c, dtype=torch.float32, device=dev)
+    if sums is not None:
+        ws = _scratch(-(-r // 128) * c * 4, dev)
+    if r > 0 and c > 0 or sums is not None:
+        guard, st_ptr = _on(dev, stream, x, q, s, qt, st, sums, ws)
+        with guard:
+            _check(lib().mgn_quant8(_at(x), xt, r, c, _row_ld(x, "x"), FORMATS[format], block_rows,
+                                    _at(q) or None, q.shape[1] if q is not None else 0, _at(s) if q is not None else None,
+                                    _at(qt), qt.shape[1] if qt is not None else 0, _at(st), _at(sums),
+                                    1 if accumulate else 0, _at(ws), ws.numel() if ws is not None else 0, st_ptr))
+    return Quantised(Mat8(q, s, c, block_rows) if rowwise else None,
+                     Mat8(qt, st, r, block_rows) if transposed else None, sums)
+
+
+def mgn_matmul8(a, b, bias=None, act="none", aux=None, out=None, dtype=None, accumulate=False, stream=None):
+    """act(a b^T + bias) of two Mat8 (see include/mgn.h): [a.rows][b.rows] in
+    float32 or bfloat16 (dtype, default float32; out: written, or added to
+    with accumulate)."""
+    torch = _torch()
+    if not isinstance(a, Mat8) or not isinstance(b, Mat8):
+        raise MgnError(ERR_ARG, "a and b must be Mat8")
+    if a.cols != b.cols:
+        raise MgnError(ERR_SHAPE, f"a has {a.cols} columns, b {b.cols}")
+    if act not in ACTS:
+        raise MgnError(ERR_ARG, f"unknown act {act!r}")
+    dev, m, n = a.q.device, a.rows, b.rows
+    if b.q.device != dev:
+        raise MgnError(ERR_ARG, f"b is on {b.q.device}, expected {dev}")
+    if out is None:
+        if accumulate:
+            raise MgnError(ERR_ARG, "accumulate needs an out to add to")
+        out = torch.empty((m, n), dtype=dtype or torch.float32, device=dev)
+    elif dtype is not None and out.dtype != dtype:
+        raise MgnError(ERR_ARG, f"out must be {dtype}, got {out.dtype}")
+    ct, ldc = _row_type(out, "out"), _row_ld(out, "out", (m, n))
+    if out.device != dev:
+        raise MgnError(ERR_ARG, f"out is on {out.device}, expected {dev}")
+    ep = Epilogue(bias=_vector(bias, "bias", n, dev), act=ACTS[act], accumulate=1 if accumulate else 0)
+    if act == "relu_grad":
+        ep.aux_type, ep.ldaux = _row_type(aux, "aux"), _row_ld(aux, "aux", (m, n))
+        if aux.device != dev:
+            raise MgnError(ERR_ARG, f"aux is on {aux.device}, expected {dev}")
+        ep.aux = aux.data_ptr()
+    elif aux is not None:
+        raise MgnError(ERR_ARG, "aux is for relu_grad only")
+    if m == 0 or n == 0:
+        return out
+    need = C.c_size_t()
+    _check(lib().mgn_matmul8_workspace(m, n, a.cols, C.byref(need)))
+    ws = _scratch(need.value, dev)
+    guard, st_ptr = _on(dev, stream, a.q, a.scale, b.q, b.scale, bias, aux, out, ws)
+    with guard:
+        _check(lib().mgn_matmul8(C.byref(a.struct), C.byref(b.struct), C.byref(ep), ct, out.data_ptr(), ldc, _at(ws),
+                                 need.value, st_ptr))
+    return out
+
+
+def _norm_gate(x, b, post, pre, post_gamma, post_beta, pre_gamma, pre_beta, gate, gate_ptr, skip, scale, eps):
+    torch = _torch()
+    xt, bt = _row_type(x, "x"), _row_type(b, "b")
+    if post not in NORMS or pre not in NORMS:
+        raise MgnError(ERR_ARG, f"unknown norm {post!r} or {pre!r}")
+    rows, cols = x.shape
+    dev, n_gates = x.device, 0
+    if b.device != dev:
+        raise MgnError(ERR_ARG, f"b is on {b.device}, expected {dev}")
+    if not 1 <= cols <= NORM_MAX_COLS:
+        raise MgnError(ERR_SHAPE, f"{cols} columns (1 to {NORM_MAX_COLS})")
+    if gate is not None:
+        if gate.dim() != 2 or gate.shape[1] != cols:
+            raise MgnError(ERR_ARG, f"gate has shape {tuple(gate.shape)}, expected (gates, {cols})")
+        n_gates = gate.shape[0]
+        _vector(gate, "gate", n_gates * cols, dev)
+    if gate_ptr is not None:
+        _dptr(gate_ptr, torch.int32, (n_gates + 1,), "gate_ptr")
+        if gate_ptr.device != dev:
+            raise MgnError(ERR_ARG, f"gate_ptr is on {gate_ptr.device}, expected {dev}")
+    return CNormGate(rows, cols, xt, bt, NORMS[post], NORMS[pre], eps, skip, scale,
+                     _vector(post_gamma, "post_gamma", cols, dev), _vector(post_beta, "post_beta", cols, dev),
+                     _vector(pre_gamma, "pre_gamma", cols, dev), _vector(pre_beta, "pre_beta", cols, dev), _at(gate),
+                     _at(gate_ptr), n_gates)
+
+
+def _as_rows(t, name, shape, dtype, device):
+    if t is None:
+        return Rows(None, 0)
+    if _row_type(t, name) is None or t.dtype != dtype:
+        raise MgnError(ERR_ARG, f"{name} must be {dtype}, got {t.dtype}")
+    if t.device != device:
+        raise MgnError(ERR_ARG, f"{name} is on {t.device}, expected {device}")
+    return Rows(t.data_ptr(), _row_ld(t, name, shape))
+
+
+def mgn_norm_gate_forward(x, b, post="none", pre="none", post_gamma=None, post_beta=None, pre_gamma=None,
+                          pre_beta=None, gate=None, gate_ptr=None, skip=1.0, scale=1.0, eps=1e-5, save=False, y=None,
+                          z=None, stream=None):
+    """y = skip x + scale gate post(b), z = pre(y) (see include/mgn.h).
+    Returns (y, z, stats): z None with pre="none", stats None without save.
+    y may be x, z may be b."""
+    torch = _torch()
+    op = _norm_gate(x, b, post, pre, post_gamma, post_beta, pre_gamma, pre_beta, gate, gate_ptr, skip, scale, eps)
+    shape, dev = tuple(x.shape), x.device
+    if y is None:
+        y = torch.empty(shape, dtype=x.dtype, device=dev)
+    if pre == "none":
+        if z is not None:
+            raise MgnError(ERR_ARG, "z without a norm before the next block")
+    elif z is None:
+        z = torch.empty(shape, dtype=b.dtype, device=dev)
+    stats = torch.empty((shape[0], 4), dtype=torch.float32, device=dev) if save else None
+    xr, br = _as_rows(x, "x", shape, x.dtype, dev), _as_rows(b, "b", shape, b.dtype, dev)
+    yr, zr = _as_rows(y, "y", shape, x.dtype, dev), _as_rows(z, "z", shape, b.dtype, dev)
+    guard, st_ptr = _on(dev, stream, x, b, y, z, stats, gate, gate_ptr, post_gamma, post_beta, pre_gamma, pre_beta)
+    with guard:
+        _check(lib().mgn_norm_gate_forward(C.byref(op), xr, br, yr, zr, _at(stats), st_ptr))
+    return y, z, stats
+
+
+NormGateGrads = collections.namedtuple("NormGateGrads", "dx db dgate dpost_gamma dpost_beta dpre_gamma dpre_beta")
+
+
+def mgn_norm_gate_backward(x, b, stats, dy, dz, post="none", pre="none", post_gamma=None, post_beta=None,
+                           pre_gamma=None, pre_beta=None, gate=None, gate_ptr=None, skip=1.0, scale=1.0, eps=1e-5,
+                           dx=None, db=None, grads=None, stream=None):
+    """Reverse of mgn_norm_gate_forward (see include/mgn.h) from its inputs and
+    stats.  dy or dz None: zero.  Returns NormGateGrads; the gradients of the
+    vectors and of the gate are those of the parameters that were given, new
+    tensors, or those of grads (a NormGateGrads of an earlier call) added to."""
+    torch = _torch()
+    op = _norm_gate(x, b, post, pre, post_gamma, post_beta, pre_gamma, pre_beta, gate, gate_ptr, skip, scale, eps)
+    shape, dev = tuple(x.shape), x.device
+    rows, cols = shape
+    dx = torch.empty(shape, dtype=x.dtype, device=dev) if dx is None else dx
+    db = torch.empty(shape, dtype=b.dtype, device=dev) if db is None else db
+    if not isinstance(stats, torch.Tensor) or tuple(stats.shape) != (rows, 4):
+        raise MgnError(ERR_ARG, "stats must be the forward's, of shape (rows, 4)")
+    _vector(stats, "stats", rows * 4, dev)
+    out = {}
+    for name, p, used in (("dgate", gate, True), ("dpost_gamma", post_gamma, post != "none"),
+                          ("dpost_beta", post_beta, post != "none"), ("dpre_gamma", pre_gamma, pre != "none"),
+                          ("dpre_beta", pre_beta, pre != "none")):
+        g = getattr(grads, name) if grads is not None else None
+        if p is None or not used:
+            if g is not None:
+                raise MgnError(ERR_ARG, f"{name} without its parameter")
+        elif grads is None:
+            g = torch.empty(p.shape, dtype=torch.float32, device=dev)
+        elif g is not None:
+            _vector(g, name, p.numel(), dev)
+        out[name] = g
+    cg = CNormGateGrads(_at(out["dpost_gamma"]), _at(out["dpost_beta"]), _at(out["dpre_gamma"]), _at(out["dpre_beta"]),
+                        _at(out["dgate"]), 0 if grads is None else 1)
+    rs = [_as_rows(t, n, shape, d.dtype, dev) for t, n, d in
+          ((x, "x", x), (b, "b", b), (dy, "dy", x), (dz, "dz", b), (dx, "dx", x), (db, "db", b))]
+    need = C.c_size_t()
+    _check(lib().mgn_norm_gate_workspace(rows, cols, C.byref(need)))
+    ws = _scratch(need.value, dev)
+    guard, st_ptr = _on(dev, stream, x, b, stats, dy, dz, dx, db, ws, gate, gate_ptr, post_gamma, post_beta, pre_gamma,
+                        pre_beta, *out.values())
+    with guard:
+        _check(lib().mgn_norm_gate_backward(C.byref(op), rs[0], rs[1], stats.data_ptr(), rs[2], rs[3], rs[4], rs[5],
+                                            C.byref(cg), _at(ws), need.value, st_ptr))
+    return NormGateGrads(dx, db, **out)
 
 
 # short aliases
