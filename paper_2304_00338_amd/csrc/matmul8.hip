@@ -49,110 +49,512 @@ __device__ __forceinline__ bf16x8 widen(int lo, int hi) {
   return bf16x8{v[0][0], v[0][1], v[1][0], v[1][1], v[2][0], v[2][1], v[3][0], v[3][1]};
 }
 
+// What a call asks for, and how it is dealt to blocks.
+struct Job {
+  Matmul8 p;
+  int64_t mt, nt;      // tiles
+  int64_t kb, per;     // blocks of 128 columns, and of a split
+  int splits;          // > 1: sums of the splits go to p.part [splits][M][N]
+};
+
+__device__ const uint4 zero16 = {0, 0, 0, 0};
+
+__device__ __forceinline__ f32x4 load4(const float* p, int n) {
+  f32x4 v = {0.f, 0.f, 0.f, 0.f};
+  if (n >= 4) {
+    __builtin_memcpy(&v, p, 16);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 3; ++e)
+      if (e < n) v[e] = p[e];
+  }
+  return v;
+}
+__device__ __forceinline__ f32x4 load4(const bf16* p, int n) {
+  f32x4 v = {0.f, 0.f, 0.f, 0.f};
+  if (n >= 4) {
+    uint32_t w[2];
+    __builtin_memcpy(w, p, 8);
+    v = f32x4{__uint_as_float(w[0] << 16), __uint_as_float(w[0] & 0xffff0000u), __uint_as_float(w[1] << 16),
+              __uint_as_float(w[1] & 0xffff0000u)};
+  } else {
+#pragma unroll
+    for (int e = 0; e < 3; ++e)
+      if (e < n) v[e] = tof(p[e]);
+  }
+  return v;
+}
+template <typename T>
+__device__ __forceinline__ void store4(T* p, f32x4 v, int n) {
+  if (n >= 4) {
+    const T w[4] = {(T)v[0], (T)v[1], (T)v[2], (T)v[3]};
+    __builtin_memcpy(p, w, sizeof(w));
+  } else {
+#pragma unroll
+    for (int e = 0; e < 3; ++e)
+      if (e < n) p[e] = (T)v[e];
+  }
+}
+
+// Four sums of row m, columns n .. n + 3 (those inside c), become c.
+__device__ __forceinline__ void finish(const Matmul8& p, int64_t m, int64_t n, f32x4 v) {
+  const int k = (int)min(p.b.rows - n, (int64_t)4);
+  if (p.ep.bias != nullptr) v += load4(p.ep.bias + n, k);
+  if (p.ep.act == MGN_ACT_RELU) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = v[e] < 0.f ? 0.f : v[e];  // a NaN stays
+  } else if (p.ep.act == MGN_ACT_RELU_GRAD) {
+    const int64_t i = m * p.ep.ldaux + n;
+    const f32x4 h = p.ep.aux_type == MGN_FP32 ? load4((const float*)p.ep.aux + i, k) : load4((const bf16*)p.ep.aux + i, k);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = h[e] > 0.f ? v[e] : 0.f;
+  }
+  const int64_t i = m * p.ldc + n;
+  if (p.c_type == MGN_FP32) {
+    float* c = (float*)p.c + i;
+    if (p.ep.accumulate) v += load4(c, k);
+    store4(c, v, k);
+  } else {
+    bf16* c = (bf16*)p.c + i;
+    if (p.ep.accumulate) v += load4(c, k);
+    store4(c, v, k);
+  }
+}
+
+// Four sums of a split, or of the whole.
+__device__ __forceinline__ void put4(const Job& J, int split, int64_t m, int64_t n, f32x4 v) {
+  if (J.splits == 1)
+    finish(J.p, m, n, v);
+  else
+    store4(J.p.part + ((int64_t)split * J.p.a.rows + m) * J.p.b.rows + n, v, (int)min(J.p.b.rows - n, (int64_t)4));
+}
+
+// Sums of the splits in their order, 4 columns a thread.
+__global__ void __launch_bounds__(256) k_matmul8_join(Job J) {
+  const int64_t N = J.p.b.rows, n4 = ceil_div(N, 4), t = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (t >= J.p.a.rows * n4) return;
+  const int64_t m = t / n4, n = t % n4 * 4;
+  const int k = (int)min(N - n, (int64_t)4);
+  const float* p = J.p.part + m * N + n;
+  f32x4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+  for (int s = 0; s < J.splits; ++s) v += load4(p + (int64_t)s * J.p.a.rows * N, k);
+  finish(J.p, m, n, v);
+}
+
+// ---- tiles: BM x BN of c a block of WM x WN waves, each TM x TN times 32 x 32.
+//
+// Steps of 128 columns, one scale block, go through two LDS buffers by loads
+// that write LDS themselves (16 bytes a lane, 8 rows of 128 bytes a wave and
+// load), the next step's under the products of the current one, with one
+// barrier a step.  A row's 16-byte chunk c sits at place c ^ (row % 8), so the
+// 8 rows of each eighth of a fragment read start in distinct banks; the lanes'
+// source addresses are permuted to match.  What lies beyond the matrix comes
+// from 16 zero bytes.  The results go through the wave's own piece of LDS to be
+// stored as whole rows.
+template <bool WIDE, int FA, int FB, bool BROW, int WM, int WN, int TM, int TN>
+__global__ void __launch_bounds__(WM * WN * 64, 2) k_matmul8_tile(Job J) {
+  constexpr int BM = WM * TM * 32, BN = WN * TN * 32, NWV = WM * WN;
+  constexpr int LOADS = (BM + BN) / 8 / NWV;  // of a wave and step
+  static_assert((BM / 8) % NWV == 0 && (BN / 8) % NWV == 0, "a load is of one operand for all waves");
+  static_assert((BM + BN) * 128 >= NWV * 32 * TN * 32 * 4, "results fit a buffer");
+  __shared__ __align__(16) uint8_t buf0[(BM + BN) * 128], buf1[(BM + BN) * 128];
+  __shared__ __align__(16) float sbuf[BROW ? 2 : 1][BROW ? BN : 4];
+  const Matmul8& p = J.p;
+  const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), j = l & 31, h = l >> 5;
+  const int wm = w / WN, wn = w % WN;
+  // tiles: XCD x (blocks go to the 8 XCDs in turn) takes an eighth of them, in
+  // groups of 8 rows of tiles, so that the blocks it runs at a time share
+  // operands in its L2
+  const int64_t tiles = J.mt * J.nt, chunk = ceil_div(tiles, 8);
+  const int64_t t = (int64_t)(blockIdx.x & 7) * chunk + (blockIdx.x >> 3);
+  if ((int64_t)(blockIdx.x >> 3) >= chunk || t >= tiles) return;
+  const int64_t group = t / (8 * J.nt), in = t - group * 8 * J.nt, gm = min(J.mt - group * 8, (int64_t)8);
+  const int64_t m0 = (group * 8 + in % gm) * BM, n0 = in / gm * BN;
+  const int split = blockIdx.y;
+  const int64_t kb0 = split * J.per, kb1 = min(kb0 + J.per, J.kb);
+  const int64_t end = (p.a.cols + 15) & ~15LL;
+
+  // loads: of wave w the 8 rows from 8 (i NWV + w) on.  A wave's rows have a
+  // scalar base and 32-bit offsets (ld < 2^28).  At the matrices' ends a row that
+  // is not there is the last one again (its results are not stored), and what
+  // lies beyond the columns comes from the 16 zero bytes.  The offsets there are
+  // formed anew each time (opaque lane and wave): kept, they would spill.
+  const int lrow = l >> 3, lchunk = ((l & 7) ^ lrow) * 16;
+  const uint32_t ata = lrow * (uint32_t)p.a.ld + lchunk, atb = lrow * (uint32_t)p.b.ld + lchunk;
+  const bool inner = m0 + BM <= p.a.rows && n0 + BN <= p.b.rows;
+  const uint8_t* const wa = p.a.q + (m0 + w * 8) * p.a.ld;
+  const uint8_t* const wb = p.b.q + (n0 + w * 8) * p.b.ld;
+  auto to_lds = [&](const uint8_t* src, uint8_t* buf, int i) {
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src,
+                                     (__attribute__((address_space(3))) void*)(buf + (i * NWV + w) * 1024), 16, 0, 0);
+  };
+  auto fetch = [&](uint8_t* buf, int64_t kb) {
+    const int64_t k = kb * 128;
+    if (inner && k + 128 <= end) {
+      int64_t lda = p.a.ld * (NWV * 8), ldb = p.b.ld * (NWV * 8);
+      uint32_t la = ata, lb = atb;
+      asm volatile("" : "+s"(lda), "+s"(ldb), "+v"(la), "+v"(lb));
+      const uint8_t *xa = wa + k, *xb = wb + k;
+#pragma unroll
+      for (int i = 0; i < BM / 8 / NWV; ++i) to_lds(xa + i * lda + la, buf, i);
+#pragma unroll
+      for (int i = 0; i < BN / 8 / NWV; ++i) to_lds(xb + i * ldb + lb, buf, i + BM / 8 / NWV);
+    } else {
+      int lr = lrow, lc = lchunk;
+      asm volatile("" : "+v"(lr), "+v"(lc));
+      const uint8_t* zero = (const uint8_t*)&zero16;
+#pragma unroll 1
+      for (int i = 0; i < LOADS; ++i) {
+        const bool isa = i < BM / 8 / NWV;
+        const mgn_mat8& x = isa ? p.a : p.b;
+        const int64_t r = min((isa ? m0 + (i * NWV + w) * 8 : n0 + (i * NWV + w) * 8 - BM) + lr, x.rows - 1);
+        to_lds(k + lc < end ? x.q + r * x.ld + k + lc : zero, buf, i);
+      }
+    }
+  };
+  // scales: of the wave's rows of a one a lane and 32 rows; of b one for the
+  // wave's columns, which lie in one block of 128, or one for each of the tile's
+  const int sha = p.a.block_rows == 128 ? 7 : 0, shb = p.b.block_rows == 128 ? 7 : 0;
+  const int64_t Ra = ceil_div(p.a.rows, p.a.block_rows), Rb = ceil_div(p.b.rows, p.b.block_rows);
+  const int64_t ma = m0 + wm * TM * 32, ma0 = min(ma, p.a.rows - 1) >> sha;
+  uint32_t ia[TM];
+#pragma unroll
+  for (int i = 0; i < TM; ++i) ia[i] = (uint32_t)((min(ma + i * 32 + j, p.a.rows - 1) >> sha) - ma0);
+  const int64_t nb0 = BROW ? n0 : min(n0 + wn * TN * 32, p.b.rows - 1) >> shb;
+  const uint32_t ib = BROW ? (uint32_t)min((int64_t)(threadIdx.x & (BN - 1)), p.b.rows - 1 - n0) : 0;
+  float sa[TM], sb, na[TM], nb;
+  auto scales = [&](int64_t kb) {
+    const float* pa = p.a.scale + kb * Ra + ma0;
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+      uint32_t at = ia[i];
+      asm volatile("" : "+v"(at));
+      na[i] = pa[at];
+    }
+    nb = (p.b.scale + kb * Rb + nb0)[ib];
+  };
+
+  f32x16 acc[TM][TN] = {};
+  int off[2][2];
+#pragma unroll
+  for (int s = 0; s < 2; ++s)
+#pragma unroll
+    for (int c = 0; c < 2; ++c) off[s][c] = j * 128 + (((4 * s + 2 * h + c) ^ (j & 7)) * 16);
+  auto frag = [&](const uint8_t* rows, int s) {
+    const uint4 lo = *(const uint4*)(rows + off[s][0]), hi = *(const uint4*)(rows + off[s][1]);
+    return i32x8{(int)lo.x, (int)lo.y, (int)lo.z, (int)lo.w, (int)hi.x, (int)hi.y, (int)hi.z, (int)hi.w};
+  };
+  auto add = [&](f32x16& to, const f32x16& part, float fa, const float* sbn) {
+    if constexpr (BROW) {
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const f32x4 s4 = *(const f32x4*)(sbn + 8 * g + 4 * h);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) to[4 * g + e] = __builtin_fmaf(part[4 * g + e], fa * s4[e], to[4 * g + e]);
+      }
+    } else {
+      const float f = fa * sb;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) to[r] = __builtin_fmaf(part[r], f, to[r]);
+    }
+  };
+  auto products = [&](const uint8_t* buf, const float* sbn) {
+    const uint8_t* rowsa = buf + wm * TM * 32 * 128;
+    const uint8_t* rowsb = buf + (BM + wn * TN * 32) * 128;
+    sbn += BROW ? wn * TN * 32 : 0;
+    if constexpr (WIDE) {
+      // every operand is widened once: 16 columns of all TM + TN at a time
+      f32x16 part[TM][TN] = {};
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        i32x8 fa[TM], fb[TN];
+#pragma unroll
+        for (int m = 0; m < TM; ++m) fa[m] = frag(rowsa + m * 4096, s);
+#pragma unroll
+        for (int n = 0; n < TN; ++n) fb[n] = frag(rowsb + n * 4096, s);
+#pragma unroll
+        for (int i = 0; i < 8; i += 2) {
+          bf16x8 wa[TM], wb[TN];
+#pragma unroll
+          for (int m = 0; m < TM; ++m) wa[m] = widen<FA>(fa[m][i], fa[m][i + 1]);
+#pragma unroll
+          for (int n = 0; n < TN; ++n) wb[n] = widen<FB>(fb[n][i], fb[n][i + 1]);
+#pragma unroll
+          for (int m = 0; m < TM; ++m)
+#pragma unroll
+            for (int n = 0; n < TN; ++n)
+              part[m][n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wb[n], wa[m], part[m][n], 0, 0, 0);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+#pragma unroll
+      for (int m = 0; m < TM; ++m)
+#pragma unroll
+        for (int n = 0; n < TN; ++n) add(acc[m][n], part[m][n], sa[m], sbn + (BROW ? n * 32 : 0));
+    } else {
+      i32x8 fb[TN][2], fa[2][2];
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+#pragma unroll
+        for (int n = 0; n < TN; ++n) fb[n][s] = frag(rowsb + n * 4096, s);
+        fa[0][s] = frag(rowsa, s);
+      }
+#pragma unroll
+      for (int m = 0; m < TM; ++m) {
+        f32x16 part[TN];
+#pragma unroll
+        for (int n = 0; n < TN; ++n) {
+          part[n] = f32x16{};
+#pragma unroll
+          for (int s = 0; s < 2; ++s)
+            part[n] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fb[n][s], fa[m & 1][s], part[n], FB - MGN_E4M3,
+                                                                      FA - MGN_E4M3, 0, 0, 0, 0);
+        }
+        if (m + 1 < TM) {
+#pragma unroll
+          for (int s = 0; s < 2; ++s) fa[(m + 1) & 1][s] = frag(rowsa + (m + 1) * 4096, s);
+        }
+#pragma unroll
+        for (int n = 0; n < TN; ++n) add(acc[m][n], part[n], sa[m], sbn + (BROW ? n * 32 : 0));
+        // else the compiler has all reads and products of a step in registers at once
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+  };
+  auto take = [&](int to) {  // the fetched scales are the next step's
+#pragma unroll
+    for (int i = 0; i < TM; ++i) sa[i] = na[i];
+    sb = nb;
+    if constexpr (BROW) {
+      if ((int)threadIdx.x < BN) sbuf[to][threadIdx.x] = nb;
+    }
+  };
+
+  if (kb0 < kb1) {
+    scales(kb0);
+    fetch(buf0, kb0);
+    take(0);
+    __syncthreads();
+    for (int64_t kb = kb0; kb < kb1; kb += 2) {
+      const int64_t left = kb1 - kb;
+      if (left > 1) {
+        scales(kb + 1);
+        fetch(buf1, kb + 1);
+      }
+      products(buf0, sbuf[0]);
+      if (left > 1) {
+        take(BROW ? 1 : 0);
+        __syncthreads();
+        if (left > 2) {
+          scales(kb + 2);
+          fetch(buf0, kb + 2);
+        }
+        products(buf1, sbuf[BROW ? 1 : 0]);
+        take(0);
+        __syncthreads();
+      }
+    }
+  }
+  __syncthreads();  // every wave has read its last operands
+  // rows of TN * 8 chunks of 4 columns, chunk c at place c ^ row
+  constexpr int CH = TN * 8;
+  f32x4* mine = (f32x4*)buf0 + w * 32 * CH;
+#pragma unroll
+  for (int m = 0; m < TM; ++m) {
+#pragma unroll
+    for (int n = 0; n < TN; ++n)
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+        mine[j * CH + ((n * 8 + 2 * g + h) ^ (j & (CH - 1)))] =
+            f32x4{acc[m][n][4 * g], acc[m][n][4 * g + 1], acc[m][n][4 * g + 2], acc[m][n][4 * g + 3]};
+    wave_lds_sync();
+    const int64_t n = n0 + wn * TN * 32 + (l % CH) * 4;
+#pragma unroll
+    for (int i = 0; i < 32; i += 64 / CH) {
+      const int r = i + l / CH;
+      const int64_t row = m0 + (wm * TM + m) * 32 + r;
+      const f32x4 v = mine[r * CH + ((l % CH) ^ (r & (CH - 1)))];
+      if (row < p.a.rows && n < p.b.rows) put4(J, split, row, n, v);
+    }
+    wave_lds_sync();
+  }
+}
+
+// ---- few rows of a (up to TM times 16): the weights' bytes.
+//
+// A block takes 16 rows of b, its 8 waves the steps of 128 columns in turn;
+// operands come straight from memory, 32 consecutive bytes a lane (four lanes
+// cover a row's 128), some steps ahead, and the waves' sums meet in LDS.  The
+// instruction is 16x16x128: lane l holds row l & 15, bytes [32 (l >> 4), + 32);
+// result r is row 4 (l >> 4) + r of b, column l & 15 a row of a.
 template <bool WIDE, int FB, int FA>
-__device__ __forceinline__ f32x16 mma8(i32x8 b, i32x8 a, f32x16 c) {
+__device__ __forceinline__ f32x4 mma16(i32x8 b, i32x8 a) {
+  f32x4 c = {0.f, 0.f, 0.f, 0.f};
   if constexpr (WIDE) {
 #pragma unroll
     for (int i = 0; i < 8; i += 2)
-      c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen<FB>(b[i], b[i + 1]), widen<FA>(a[i], a[i + 1]), c, 0, 0, 0);
+      c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen<FB>(b[i], b[i + 1]), widen<FA>(a[i], a[i + 1]), c, 0, 0, 0);
     return c;
   } else {
-    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(b, a, c, FB - MGN_E4M3, FA - MGN_E4M3, 0, 0, 0, 0);
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b, a, c, FB - MGN_E4M3, FA - MGN_E4M3, 0, 0, 0, 0);
   }
 }
 
-// 32 bytes of a row from byte k on; what lies beyond `end` (a multiple of 16)
-// counts as zero.
-__device__ __forceinline__ i32x8 frag(const uint8_t* row, int64_t k, int64_t end) {
-  uint4 lo = {0, 0, 0, 0}, hi = {0, 0, 0, 0};
-  if (k < end) lo = *(const uint4*)(row + k);
-  if (k + 16 < end) hi = *(const uint4*)(row + k + 16);
-  return i32x8{(int)lo.x, (int)lo.y, (int)lo.z, (int)lo.w, (int)hi.x, (int)hi.y, (int)hi.z, (int)hi.w};
-}
-
-// Four consecutive columns n .. n + 3 of row m of c.
-__device__ __forceinline__ void finish(const Matmul8& p, int64_t m, int64_t n, f32x4 v) {
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    if (n + e >= p.b.rows) break;
-    float f = v[e];
-    if (p.ep.bias != nullptr) f += p.ep.bias[n + e];
-    if (p.ep.act == MGN_ACT_RELU) {
-      f = f < 0.f ? 0.f : f;
-    } else if (p.ep.act == MGN_ACT_RELU_GRAD) {
-      const int64_t i = m * p.ep.ldaux + n + e;
-      const float h = p.ep.aux_type == MGN_FP32 ? ((const float*)p.ep.aux)[i] : tof(((const bf16*)p.ep.aux)[i]);
-      f = h > 0.f ? f : 0.f;
-    }
-    const int64_t i = m * p.ldc + n + e;
-    if (p.c_type == MGN_FP32) {
-      float* c = (float*)p.c;
-      c[i] = p.ep.accumulate ? c[i] + f : f;
-    } else {
-      bf16* c = (bf16*)p.c;
-      c[i] = (bf16)(p.ep.accumulate ? tof(c[i]) + f : f);
-    }
-  }
-}
-
-// One wave a 32 x 32 tile, operands straight from memory.
-template <bool WIDE, int FA, int FB>
-__global__ void __launch_bounds__(256) k_matmul8(Matmul8 p, int64_t mt, int64_t nt) {
-  const int l = threadIdx.x & 63, j = l & 31, h = l >> 5;
-  const int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (t >= mt * nt) return;
-  const int64_t m = t / nt * 32 + j, n0 = t % nt * 32;
-  const int64_t K = p.a.cols, kb = ceil_div(K, 128), end = (K + 15) & ~15LL;
+template <bool WIDE, int FA, int FB, int TM>
+__global__ void __launch_bounds__(512) k_matmul8_few(Job J) {
+  constexpr int NWV = 8;
+  __shared__ f32x4 sums[NWV][TM][64];
+  const Matmul8& p = J.p;
+  const int l = threadIdx.x & 63, w = threadIdx.x >> 6, j = l & 15, q = l >> 4;
+  const int64_t n0 = (int64_t)blockIdx.x * 16;
+  const int split = blockIdx.y;
+  const int64_t kb0 = split * J.per, kb1 = min(kb0 + J.per, J.kb);
+  const int64_t end = (p.a.cols + 15) & ~15LL;
   const int sha = p.a.block_rows == 128 ? 7 : 0, shb = p.b.block_rows == 128 ? 7 : 0;
   const int64_t Ra = ceil_div(p.a.rows, p.a.block_rows), Rb = ceil_div(p.b.rows, p.b.block_rows);
-  const int64_t ma = min(m, p.a.rows - 1), nb = min(n0 + j, p.b.rows - 1);
-  const uint8_t* ra = p.a.q + ma * p.a.ld;
-  const uint8_t* rb = p.b.q + nb * p.b.ld;
-  float acc[16] = {};
-  for (int64_t b = 0; b < kb; ++b) {
-    f32x16 part = {};
+  const uint8_t* rb = p.b.q + min(n0 + j, p.b.rows - 1) * p.b.ld + q * 32;
+  const uint8_t* ra[TM];
+  const float* psa[TM];
+  const float* psb[4];
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      const int64_t k = b * 128 + s * 64 + h * 32;
-      part = mma8<WIDE, FB, FA>(frag(rb, k, end), frag(ra, k, end), part);
-    }
-    const float sa = p.a.scale[b * Ra + (ma >> sha)];
+  for (int i = 0; i < TM; ++i) {
+    const int64_t m = min((int64_t)i * 16 + j, p.a.rows - 1);
+    ra[i] = p.a.q + m * p.a.ld + q * 32;
+    psa[i] = p.a.scale + (m >> sha);
+  }
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      const int64_t n = min(n0 + 8 * (r / 4) + 4 * h + r % 4, p.b.rows - 1);
-      acc[r] = __builtin_fmaf(part[r], sa * p.b.scale[b * Rb + (n >> shb)], acc[r]);
+  for (int r = 0; r < 4; ++r) psb[r] = p.b.scale + (min(n0 + 4 * q + r, p.b.rows - 1) >> shb);
+  auto get = [&](const uint8_t* row, int64_t kb) {
+    const int64_t k = kb * 128;
+    const uint8_t* z = (const uint8_t*)&zero16;
+    const uint4 lo = *(const uint4*)(k + q * 32 < end ? row + k : z);
+    const uint4 hi = *(const uint4*)(k + q * 32 + 16 < end ? row + k + 16 : z);
+    return i32x8{(int)lo.x, (int)lo.y, (int)lo.z, (int)lo.w, (int)hi.x, (int)hi.y, (int)hi.z, (int)hi.w};
+  };
+  f32x4 acc[TM] = {};
+  for (int64_t kb = kb0 + w; kb < kb1; kb += NWV) {
+    const i32x8 b = get(rb, kb);
+    float sb[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) sb[r] = psb[r][kb * Rb];
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+      const f32x4 part = mma16<WIDE, FB, FA>(b, get(ra[i], kb));
+      const float sa = psa[i][kb * Ra];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) acc[i][r] = __builtin_fmaf(part[r], sa * sb[r], acc[i][r]);
     }
   }
-  if (m >= p.a.rows) return;
 #pragma unroll
-  for (int r = 0; r < 16; r += 4) finish(p, m, n0 + 2 * r + 4 * h, f32x4{acc[r], acc[r + 1], acc[r + 2], acc[r + 3]});
+  for (int i = 0; i < TM; ++i) sums[w][i][l] = acc[i];
+  __syncthreads();
+  if (w < TM) {
+    f32x4 v = sums[0][w][l];
+#pragma unroll
+    for (int k = 1; k < NWV; ++k) v += sums[k][w][l];
+    const int64_t m = w * 16 + j, n = n0 + 4 * q;
+    if (m < p.a.rows && n < p.b.rows) put4(J, split, m, n, v);
+  }
 }
 
 }  // namespace dev
 
 using namespace dev;
 
-size_t matmul8_workspace(int64_t, int64_t, int64_t) { return 0; }
+namespace {
+
+constexpr int64_t kFewRows = 64;
+constexpr int64_t kCUs = 256;
+
+enum { kFew, kSmallTile, kBigTile };
+struct Plan {
+  int kind;
+  int64_t mt, nt, per;
+  int splits;
+};
+
+Plan plan(int64_t m, int64_t n, int64_t k, bool big_ok) {
+  Plan r;
+  const int64_t kb = ceil_div(k, 128);
+  int64_t want;
+  if (m <= kFewRows) {
+    r.kind = kFew;
+    r.mt = 1;
+    r.nt = ceil_div(n, 16);
+    want = std::min(2 * kCUs / std::max<int64_t>(r.nt, 1), kb / 16);
+  } else {
+    const int64_t big = ceil_div(m, 256) * ceil_div(n, 256);
+    r.kind = big_ok && big >= kCUs * 3 / 4 ? kBigTile : kSmallTile;
+    const int64_t bm = r.kind == kBigTile ? 256 : 128;
+    r.mt = ceil_div(m, bm);
+    r.nt = ceil_div(n, bm);
+    want = r.kind == kBigTile ? 1 : std::min(2 * kCUs / (r.mt * r.nt), kb / 4);
+  }
+  r.splits = (int)std::max<int64_t>(want, 1);
+  r.per = std::max<int64_t>(ceil_div(kb, r.splits), 1);
+  r.splits = (int)std::max<int64_t>(ceil_div(kb, r.per), 1);
+  return r;
+}
+
+template <bool WIDE, int FA, int FB>
+void launch(const Job& J, const Plan& r, hipStream_t s) {
+  const dim3 grid((unsigned)(8 * ceil_div(r.mt * r.nt, 8)), (unsigned)r.splits);
+  if (r.kind == kFew) {
+    const dim3 g((unsigned)r.nt, (unsigned)r.splits);
+    const int64_t m = J.p.a.rows;
+    if (m <= 16)
+      hipLaunchKernelGGL((k_matmul8_few<WIDE, FA, FB, 1>), g, dim3(512), 0, s, J);
+    else if (m <= 32)
+      hipLaunchKernelGGL((k_matmul8_few<WIDE, FA, FB, 2>), g, dim3(512), 0, s, J);
+    else
+      hipLaunchKernelGGL((k_matmul8_few<WIDE, FA, FB, 4>), g, dim3(512), 0, s, J);
+    return;
+  }
+  const bool brow = J.p.b.block_rows == 1;
+  if constexpr (!WIDE) {
+    if (r.kind == kBigTile) {
+      hipLaunchKernelGGL((k_matmul8_tile<WIDE, FA, FB, false, 2, 4, 4, 2>), grid, dim3(512), 0, s, J);
+      return;
+    }
+  }
+  if (brow)
+    hipLaunchKernelGGL((k_matmul8_tile<WIDE, FA, FB, true, 2, 2, 2, 2>), grid, dim3(256), 0, s, J);
+  else
+    hipLaunchKernelGGL((k_matmul8_tile<WIDE, FA, FB, false, 2, 2, 2, 2>), grid, dim3(256), 0, s, J);
+}
+
+}  // namespace
+
+// The type of c is not known here: as much as either plan takes.
+size_t matmul8_workspace(int64_t m, int64_t n, int64_t k) {
+  if (m <= 0 || n <= 0) return 0;
+  const int splits = std::max(plan(m, n, k, false).splits, plan(m, n, k, true).splits);
+  return splits > 1 ? (size_t)splits * (size_t)m * (size_t)n * 4 : 0;
+}
 
 hipError_t launch_matmul8(const Matmul8& p, hipStream_t s) {
-  const int64_t mt = ceil_div(p.a.rows, 32), nt = ceil_div(p.b.rows, 32);
-  const dim3 grid((unsigned)ceil_div(mt * nt, 4)), block(256);
-#define MGN_MM8(W, FA, FB) hipLaunchKernelGGL((k_matmul8<W, FA, FB>), grid, block, 0, s, p, mt, nt)
+  const bool wide = p.c_type == MGN_FP32;
+  const Plan r = plan(p.a.rows, p.b.rows, p.a.cols, !wide && p.b.block_rows == 128);
+  const Job J = {p, r.mt, r.nt, ceil_div(p.a.cols, 128), r.per, r.splits};
 #define MGN_MM8_FORMATS(W)                                           \
   do {                                                               \
     if (p.a.format == MGN_E4M3 && p.b.format == MGN_E4M3)            \
-      MGN_MM8(W, MGN_E4M3, MGN_E4M3);                                \
+      launch<W, MGN_E4M3, MGN_E4M3>(J, r, s);                        \
     else if (p.a.format == MGN_E4M3)                                 \
-      MGN_MM8(W, MGN_E4M3, MGN_E5M2);                                \
+      launch<W, MGN_E4M3, MGN_E5M2>(J, r, s);                        \
     else if (p.b.format == MGN_E4M3)                                 \
-      MGN_MM8(W, MGN_E5M2, MGN_E4M3);                                \
+      launch<W, MGN_E5M2, MGN_E4M3>(J, r, s);                        \
     else                                                             \
-      MGN_MM8(W, MGN_E5M2, MGN_E5M2);                                \
+      launch<W, MGN_E5M2, MGN_E5M2>(J, r, s);                        \
   } while (0)
-  if (p.c_type == MGN_FP32)
+  if (wide)
     MGN_MM8_FORMATS(true);
   else
     MGN_MM8_FORMATS(false);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || r.splits == 1) return e;
+  hipLaunchKernelGGL(k_matmul8_join, dim3((unsigned)ceil_div(p.a.rows * ceil_div(p.b.rows, 4), 256)), dim3(256), 0, s, J);
   return hipGetLastError();
 }
 
