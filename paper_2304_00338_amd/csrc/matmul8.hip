@@ -129,17 +129,28 @@ __device__ __forceinline__ void put4(const Job& J, int split, int64_t m, int64_t
     store4(J.p.part + ((int64_t)split * J.p.a.rows + m) * J.p.b.rows + n, v, (int)min(J.p.b.rows - n, (int64_t)4));
 }
 
-// Sums of the splits in their order, 4 columns a thread.
+// Sums of the splits, 4 columns a thread: G threads for each, thread g the splits
+// g, g + G, ..., then the G sums in order.
+template <int G>
 __global__ void __launch_bounds__(256) k_matmul8_join(Job J) {
-  const int64_t N = J.p.b.rows, n4 = ceil_div(N, 4), t = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (t >= J.p.a.rows * n4) return;
-  const int64_t m = t / n4, n = t % n4 * 4;
+  __shared__ f32x4 sums[G][256 / G];
+  const int g = threadIdx.x / (256 / G), q = threadIdx.x % (256 / G);
+  const int64_t M = J.p.a.rows, N = J.p.b.rows, n4 = ceil_div(N, 4), t = (int64_t)blockIdx.x * (256 / G) + q;
+  const bool in = t < M * n4;
+  const int64_t m = in ? t / n4 : 0, n = in ? t % n4 * 4 : 0;
   const int k = (int)min(N - n, (int64_t)4);
   const float* p = J.p.part + m * N + n;
   f32x4 v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 8
-  for (int s = 0; s < J.splits; ++s) v += load4(p + (int64_t)s * J.p.a.rows * N, k);
-  finish(J.p, m, n, v);
+  for (int s = g; s < J.splits; s += G) v += load4(p + (int64_t)s * M * N, k);
+  if constexpr (G > 1) {
+    sums[g][q] = v;
+    __syncthreads();
+    if (g > 0) return;
+#pragma unroll
+    for (int i = 1; i < G; ++i) v += sums[i][q];
+  }
+  if (in) finish(J.p, m, n, v);
 }
 
 // ---- tiles: BM x BN of c a block of WM x WN waves, each TM x TN times 32 x 32.
@@ -147,8 +158,8 @@ __global__ void __launch_bounds__(256) k_matmul8_join(Job J) {
 // Steps of 128 columns, one scale block, go through two LDS buffers by loads
 // that write LDS themselves (16 bytes a lane, 8 rows of 128 bytes a wave and
 // load), the next step's under the products of the current one, with one
-// barrier a step.  A row's 16-byte chunk c sits at place c ^ (row % 8), so the
-// 8 rows of each eighth of a fragment read start in distinct banks; the lanes'
+// barrier a step.  A row's 16-byte chunk c sits at place c ^ (row / 2 % 8), so
+// that 16 rows of a fragment read cover all 64 banks; the lanes'
 // source addresses are permuted to match.  What lies beyond the matrix comes
 // from 16 zero bytes.  The results go through the wave's own piece of LDS to be
 // stored as whole rows.
@@ -157,21 +168,23 @@ __global__ void __launch_bounds__(WM * WN * 64, 2) k_matmul8_tile(Job J) {
   constexpr int BM = WM * TM * 32, BN = WN * TN * 32, NWV = WM * WN;
   constexpr int LOADS = (BM + BN) / 8 / NWV;  // of a wave and step
   static_assert((BM / 8) % NWV == 0 && (BN / 8) % NWV == 0, "a load is of one operand for all waves");
+  static_assert(NWV % 2 == 0, "a wave's groups of 8 rows have one parity");
   static_assert((BM + BN) * 128 >= NWV * 32 * TN * 32 * 4, "results fit a buffer");
   __shared__ __align__(16) uint8_t buf0[(BM + BN) * 128], buf1[(BM + BN) * 128];
   __shared__ __align__(16) float sbuf[BROW ? 2 : 1][BROW ? BN : 4];
   const Matmul8& p = J.p;
   const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), j = l & 31, h = l >> 5;
   const int wm = w / WN, wn = w % WN;
-  // tiles: XCD x (blocks go to the 8 XCDs in turn) takes an eighth of them, in
-  // groups of 8 rows of tiles, so that the blocks it runs at a time share
-  // operands in its L2
-  const int64_t tiles = J.mt * J.nt, chunk = ceil_div(tiles, 8);
-  const int64_t t = (int64_t)(blockIdx.x & 7) * chunk + (blockIdx.x >> 3);
-  if ((int64_t)(blockIdx.x >> 3) >= chunk || t >= tiles) return;
+  // XCD x (blocks go to the 8 XCDs in turn) takes an eighth of the tiles of all
+  // splits, a split's tiles one after the other in groups of 8 rows of tiles, so
+  // that the blocks it runs at a time share operands in its L2
+  const int64_t tiles = J.mt * J.nt, all = tiles * J.splits, chunk = ceil_div(all, 8);
+  const int64_t job = (int64_t)(blockIdx.x & 7) * chunk + (blockIdx.x >> 3);
+  if (job >= all) return;
+  const int split = (int)(job / tiles);
+  const int64_t t = job - split * tiles;
   const int64_t group = t / (8 * J.nt), in = t - group * 8 * J.nt, gm = min(J.mt - group * 8, (int64_t)8);
   const int64_t m0 = (group * 8 + in % gm) * BM, n0 = in / gm * BN;
-  const int split = blockIdx.y;
   const int64_t kb0 = split * J.per, kb1 = min(kb0 + J.per, J.kb);
   const int64_t end = (p.a.cols + 15) & ~15LL;
 
@@ -180,7 +193,7 @@ __global__ void __launch_bounds__(WM * WN * 64, 2) k_matmul8_tile(Job J) {
   // is not there is the last one again (its results are not stored), and what
   // lies beyond the columns comes from the 16 zero bytes.  The offsets there are
   // formed anew each time (opaque lane and wave): kept, they would spill.
-  const int lrow = l >> 3, lchunk = ((l & 7) ^ lrow) * 16;
+  const int lrow = l >> 3, lchunk = ((l & 7) ^ ((4 * (w & 1) + (l >> 4)) & 7)) * 16;
   const uint32_t ata = lrow * (uint32_t)p.a.ld + lchunk, atb = lrow * (uint32_t)p.b.ld + lchunk;
   const bool inner = m0 + BM <= p.a.rows && n0 + BN <= p.b.rows;
   const uint8_t* const wa = p.a.q + (m0 + w * 8) * p.a.ld;
@@ -194,12 +207,20 @@ __global__ void __launch_bounds__(WM * WN * 64, 2) k_matmul8_tile(Job J) {
     if (inner && k + 128 <= end) {
       int64_t lda = p.a.ld * (NWV * 8), ldb = p.b.ld * (NWV * 8);
       uint32_t la = ata, lb = atb;
-      asm volatile("" : "+s"(lda), "+s"(ldb), "+v"(la), "+v"(lb));
+      asm volatile("" : "+v"(la), "+v"(lb));
       const uint8_t *xa = wa + k, *xb = wb + k;
 #pragma unroll
-      for (int i = 0; i < BM / 8 / NWV; ++i) to_lds(xa + i * lda + la, buf, i);
+      for (int i = 0; i < BM / 8 / NWV; ++i) {
+        asm volatile("" : "+s"(xa));
+        to_lds(xa + la, buf, i);
+        xa += lda;
+      }
 #pragma unroll
-      for (int i = 0; i < BN / 8 / NWV; ++i) to_lds(xb + i * ldb + lb, buf, i + BM / 8 / NWV);
+      for (int i = 0; i < BN / 8 / NWV; ++i) {
+        asm volatile("" : "+s"(xb));
+        to_lds(xb + lb, buf, i + BM / 8 / NWV);
+        xb += ldb;
+      }
     } else {
       int lr = lrow, lc = lchunk;
       asm volatile("" : "+v"(lr), "+v"(lc));
@@ -240,12 +261,12 @@ __global__ void __launch_bounds__(WM * WN * 64, 2) k_matmul8_tile(Job J) {
 #pragma unroll
   for (int s = 0; s < 2; ++s)
 #pragma unroll
-    for (int c = 0; c < 2; ++c) off[s][c] = j * 128 + (((4 * s + 2 * h + c) ^ (j & 7)) * 16);
+    for (int c = 0; c < 2; ++c) off[s][c] = j * 128 + (((4 * s + 2 * h + c) ^ ((j >> 1) & 7)) * 16);
   auto frag = [&](const uint8_t* rows, int s) {
     const uint4 lo = *(const uint4*)(rows + off[s][0]), hi = *(const uint4*)(rows + off[s][1]);
     return i32x8{(int)lo.x, (int)lo.y, (int)lo.z, (int)lo.w, (int)hi.x, (int)hi.y, (int)hi.z, (int)hi.w};
   };
-  auto add = [&](f32x16& to, const f32x16& part, float fa, const float* sbn) {
+  auto add = [&](f32x16& to, const f32x16& part, float fa, float fb, const float* sbn) {
     if constexpr (BROW) {
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
@@ -254,9 +275,18 @@ __global__ void __launch_bounds__(WM * WN * 64, 2) k_matmul8_tile(Job J) {
         for (int e = 0; e < 4; ++e) to[4 * g + e] = __builtin_fmaf(part[4 * g + e], fa * s4[e], to[4 * g + e]);
       }
     } else {
-      const float f = fa * sb;
+      const float f = fa * fb;
 #pragma unroll
       for (int r = 0; r < 16; ++r) to[r] = __builtin_fmaf(part[r], f, to[r]);
+    }
+  };
+  // 8-bit products of the step's last 32 rows that are still to be added
+  f32x16 open[TN] = {};
+  float open_a = 0.f, open_b = 0.f;
+  auto settle = [&]() {
+    if constexpr (!WIDE && !BROW) {
+#pragma unroll
+      for (int n = 0; n < TN; ++n) add(acc[TM - 1][n], open[n], open_a, open_b, nullptr);
     }
   };
   auto products = [&](const uint8_t* buf, const float* sbn) {
@@ -291,32 +321,41 @@ __global__ void __launch_bounds__(WM * WN * 64, 2) k_matmul8_tile(Job J) {
 #pragma unroll
       for (int m = 0; m < TM; ++m)
 #pragma unroll
-        for (int n = 0; n < TN; ++n) add(acc[m][n], part[m][n], sa[m], sbn + (BROW ? n * 32 : 0));
+        for (int n = 0; n < TN; ++n) add(acc[m][n], part[m][n], sa[m], sb, sbn + (BROW ? n * 32 : 0));
     } else {
+      // the last 32 rows' products are added under the next step's first reads
       i32x8 fb[TN][2], fa[2][2];
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
+        fa[0][s] = frag(rowsa, s);
 #pragma unroll
         for (int n = 0; n < TN; ++n) fb[n][s] = frag(rowsb + n * 4096, s);
-        fa[0][s] = frag(rowsa, s);
+        __builtin_amdgcn_sched_barrier(0);
       }
+      settle();
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int m = 0; m < TM; ++m) {
         f32x16 part[TN];
 #pragma unroll
-        for (int n = 0; n < TN; ++n) {
-          part[n] = f32x16{};
+        for (int s = 0; s < 2; ++s)
 #pragma unroll
-          for (int s = 0; s < 2; ++s)
-            part[n] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fb[n][s], fa[m & 1][s], part[n], FB - MGN_E4M3,
-                                                                      FA - MGN_E4M3, 0, 0, 0, 0);
-        }
+          for (int n = 0; n < TN; ++n)
+            part[n] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fb[n][s], fa[m & 1][s], s ? part[n] : f32x16{},
+                                                                      FB - MGN_E4M3, FA - MGN_E4M3, 0, 0, 0, 0);
         if (m + 1 < TM) {
 #pragma unroll
           for (int s = 0; s < 2; ++s) fa[(m + 1) & 1][s] = frag(rowsa + (m + 1) * 4096, s);
         }
+        if (BROW || m + 1 < TM) {
 #pragma unroll
-        for (int n = 0; n < TN; ++n) add(acc[m][n], part[n], sa[m], sbn + (BROW ? n * 32 : 0));
+          for (int n = 0; n < TN; ++n) add(acc[m][n], part[n], sa[m], sb, sbn + (BROW ? n * 32 : 0));
+        } else {
+#pragma unroll
+          for (int n = 0; n < TN; ++n) open[n] = part[n];
+          open_a = sa[m];
+          open_b = sb;
+        }
         // else the compiler has all reads and products of a step in registers at once
         __builtin_amdgcn_sched_barrier(0);
       }
@@ -356,6 +395,7 @@ __global__ void __launch_bounds__(WM * WN * 64, 2) k_matmul8_tile(Job J) {
       }
     }
   }
+  settle();
   __syncthreads();  // every wave has read its last operands
   // rows of TN * 8 chunks of 4 columns, chunk c at place c ^ row
   constexpr int CH = TN * 8;
@@ -499,7 +539,7 @@ Plan plan(int64_t m, int64_t n, int64_t k, bool big_ok) {
 
 template <bool WIDE, int FA, int FB>
 void launch(const Job& J, const Plan& r, hipStream_t s) {
-  const dim3 grid((unsigned)(8 * ceil_div(r.mt * r.nt, 8)), (unsigned)r.splits);
+  const dim3 grid((unsigned)(8 * ceil_div(r.mt * r.nt * r.splits, 8)));
   if (r.kind == kFew) {
     const dim3 g((unsigned)r.nt, (unsigned)r.splits);
     const int64_t m = J.p.a.rows;
@@ -554,7 +594,11 @@ hipError_t launch_matmul8(const Matmul8& p, hipStream_t s) {
     MGN_MM8_FORMATS(false);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || r.splits == 1) return e;
-  hipLaunchKernelGGL(k_matmul8_join, dim3((unsigned)ceil_div(p.a.rows * ceil_div(p.b.rows, 4), 256)), dim3(256), 0, s, J);
+  const int64_t quads = p.a.rows * ceil_div(p.b.rows, 4);
+  if (r.splits >= 16)  // 256 splits of 128 x 256: 23 -> @ us
+    hipLaunchKernelGGL((k_matmul8_join<16>), dim3((unsigned)ceil_div(quads, 16)), dim3(256), 0, s, J);
+  else
+    hipLaunchKernelGGL((k_matmul8_join<1>), dim3((unsigned)ceil_div(quads, 256)), dim3(256), 0, s, J);
   return hipGetLastError();
 }
 

@@ -125,8 +125,52 @@ __device__ __forceinline__ void statistics(const float (&v)[NV][8], const int (&
   rstd = 1.f / __builtin_sqrtf(__builtin_fmaf(red.sum(q), inv, eps));
 }
 
-template <typename XT, typename BT, int LPR, int NV>
-__global__ void __launch_bounds__(LPR ? 256 : 1024) k_norm_gate_fwd(NormGate a) {
+// Which gate a row has.  Groups are looked up once and followed from row to row.
+struct Gates {
+  int64_t g = 0, held = -1;
+  __device__ __forceinline__ Gates(const NormGate& a, int64_t r0) {
+    if (a.gmode == kGateGroup) g = find_group(a.op.gate_ptr, a.op.n_gates, r0);
+  }
+  // Whether row r has one; fresh: it is another than the row's before.
+  __device__ __forceinline__ bool at(const NormGate& a, int64_t r, bool& fresh) {
+    fresh = false;
+    if (a.gmode == kGateRow) {
+      fresh = true;
+      held = r;
+    } else if (a.gmode == kGateGroup) {
+      while (g + 1 < a.op.n_gates && r >= a.op.gate_ptr[g + 1]) ++g;
+      if (r < a.op.gate_ptr[g] || r >= a.op.gate_ptr[g + 1]) return false;
+      fresh = g != held;
+      held = g;
+    }
+    return true;
+  }
+};
+
+// y = skip x + ga bhat + gb: ga = scale gate gamma, gb = scale gate beta.
+template <int NV>
+__device__ __forceinline__ void gate_vectors(float (&ga)[NV][8], float (&gb)[NV][8], const NormGate& a, int64_t gate,
+                                             const int (&col)[NV], const int (&n)[NV]) {
+  const mgn_norm_gate& op = a.op;
+  const float* g = a.gmode == kGateNone ? nullptr : op.gate + gate * op.cols;
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+    // opaque, or the addresses of all vectors are kept in registers from row to row
+    int c0 = col[k];
+    asm volatile("" : "+v"(c0));
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const bool in = e < n[k];
+      const int c = in ? c0 + e : 0;
+      const float v = in ? op.scale * (g != nullptr ? g[c] : 1.f) : 0.f;
+      ga[k][e] = v * (op.post_gamma != nullptr ? op.post_gamma[c] : 1.f);
+      gb[k][e] = op.post_beta != nullptr ? v * op.post_beta[c] : 0.f;
+    }
+  }
+}
+
+template <typename XT, typename BT, int LPR, int NV, int MAXT>
+__global__ void __launch_bounds__(MAXT) k_norm_gate_fwd(NormGate a) {
   __shared__ float buf[64];
   const mgn_norm_gate& op = a.op;
   const Place<LPR, NV> at(op.rows, op.cols, a.per);
@@ -135,14 +179,12 @@ __global__ void __launch_bounds__(LPR ? 256 : 1024) k_norm_gate_fwd(NormGate a) 
   int col[NV];
 #pragma unroll
   for (int k = 0; k < NV; ++k) col[k] = at.col(k);
-  float pg[NV][8], pb[NV][8], qg[NV][8], qb[NV][8], gate[NV][8];
-  load_vec(pg, op.post_gamma, col, at.n, 1.f);
-  load_vec(pb, op.post_beta, col, at.n, 0.f);
+  float ga[NV][8], gb[NV][8], qg[NV][8], qb[NV][8];
+  gate_vectors(ga, gb, a, 0, col, at.n);
   load_vec(qg, op.pre_gamma, col, at.n, 1.f);
   load_vec(qb, op.pre_beta, col, at.n, 0.f);
-  load_vec(gate, a.gmode == kGateOne ? op.gate : nullptr, col, at.n, 1.f);
   const int64_t last = op.rows - 1;
-  int64_t g = a.gmode == kGateGroup ? find_group(op.gate_ptr, op.n_gates, at.r0) : 0, held = -1;
+  Gates gates(a, at.r0);
   Raw8<XT> nx[NV];
   Raw8<BT> nb[NV];
   auto fetch = [&](int64_t r) {
@@ -157,7 +199,6 @@ __global__ void __launch_bounds__(LPR ? 256 : 1024) k_norm_gate_fwd(NormGate a) 
   // every walker of a wave or block takes as many turns: the sums cross lanes
   for (int64_t i = 0; i < a.per; ++i) {
     const int64_t r = at.r0 + i;
-    bool mine = r < at.r1;
     float x[NV][8], b[NV][8];
 #pragma unroll
     for (int k = 0; k < NV; ++k)
@@ -167,28 +208,17 @@ __global__ void __launch_bounds__(LPR ? 256 : 1024) k_norm_gate_fwd(NormGate a) 
         b[k][e] = nb[k].get(e);
       }
     if (i + 1 < a.per) fetch(r + 1);
-    if (a.gmode == kGateGroup && mine) {
-      while (g + 1 < op.n_gates && r >= op.gate_ptr[g + 1]) ++g;
-      mine = r >= op.gate_ptr[g] && r < op.gate_ptr[g + 1];
-      if (mine && g != held) {
-        load_vec(gate, op.gate + g * op.cols, col, at.n, 1.f);
-        held = g;
-      }
-    }
-    if (a.gmode == kGateRow && mine) load_vec(gate, op.gate + r * op.cols, col, at.n, 1.f);
+    bool fresh = false;
+    const bool mine = r < at.r1 && gates.at(a, r, fresh);
+    if (fresh) gate_vectors(ga, gb, a, gates.held, col, at.n);
     float pm = 0.f, pr = 1.f, qm = 0.f, qr = 1.f;
-    if (op.post != MGN_NORM_NONE) {
-      statistics(b, at.n, op.post, inv, op.eps, red, pm, pr);
-#pragma unroll
-      for (int k = 0; k < NV; ++k)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) b[k][e] = __builtin_fmaf((b[k][e] - pm) * pr, pg[k][e], pb[k][e]);
-    }
+    if (op.post != MGN_NORM_NONE) statistics(b, at.n, op.post, inv, op.eps, red, pm, pr);
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
+      // beyond the row x, ga and gb are 0
 #pragma unroll
       for (int e = 0; e < 8; ++e)
-        x[k][e] = e < at.n[k] ? __builtin_fmaf(op.scale, gate[k][e] * b[k][e], op.skip * x[k][e]) : 0.f;
+        x[k][e] = __builtin_fmaf(op.skip, x[k][e], __builtin_fmaf((b[k][e] - pm) * pr, ga[k][e], gb[k][e]));
       if (mine) store8((XT*)a.y.data + r * a.y.ld + col[k], at.n[k], x[k]);
     }
     if (op.pre != MGN_NORM_NONE) {
@@ -205,105 +235,122 @@ __global__ void __launch_bounds__(LPR ? 256 : 1024) k_norm_gate_fwd(NormGate a) 
 }
 
 // Reverse.  With t = dy + pre'(dz), dp = scale gate t:
-//   dx = skip t, db = post'(dp), dgate = sum of scale p t, and the gammas' and
-//   betas' sums; norm'(d) = rstd (u - mean(u) - vhat mean(u vhat)), u = gamma d
-//   (RMS: without mean(u)).  y is formed again from x and b, unrounded, and
-// with the forward's statistics no sum precedes those of the gradients.
-template <typename XT, typename BT, int LPR, int NV>
-__global__ void __launch_bounds__(LPR ? 256 : 1024) k_norm_gate_bwd(NormGate a) {
+//   dx = skip t, db = post'(dp), dgate = sum of scale p t, dgamma_post = sum of
+//   dp bhat, dbeta_post = sum of dp, dgamma_pre = sum of dz yhat, dbeta_pre =
+//   sum of dz; norm'(d) = rstd (u - mean(u) - vhat mean(u vhat)), u = gamma d
+//   (RMS: without mean(u)).
+// y is formed again from x and b, unrounded, and with the forward's statistics
+// no sum precedes those of the gradients.  While the gate stays the same, two
+// column sums, st = sum of t and sb = sum of t bhat, stand for three:
+//   dgate = scale (gamma sb + beta st), dgamma_post += scale gate sb,
+//   dbeta_post += scale gate st.
+// MANY: there are gates of rows or groups; without, these are formed once.
+template <typename XT, typename BT, int LPR, int NV, int MAXT, bool MANY>
+__global__ void __launch_bounds__(MAXT) k_norm_gate_bwd(NormGate a) {
   __shared__ float buf[64];
   extern __shared__ float sums[];  // LPR: [walkers of the block][cols]
   const mgn_norm_gate& op = a.op;
+  constexpr bool PRE = LPR == 0;  // the next row's loads under this one; else other walkers fill the wait
   const Place<LPR, NV> at(op.rows, op.cols, a.per);
   Reduce<LPR> red{buf};
   const float inv = 1.f / (float)op.cols;
   int col[NV];
 #pragma unroll
   for (int k = 0; k < NV; ++k) col[k] = at.col(k);
-  float pg[NV][8], pb[NV][8], qg[NV][8], gate[NV][8];
-  load_vec(pg, op.post_gamma, col, at.n, 1.f);
-  load_vec(pb, op.post_beta, col, at.n, 0.f);
+  float ga[NV][8], gb[NV][8], qg[NV][8];
+  gate_vectors(ga, gb, a, 0, col, at.n);
   load_vec(qg, op.pre_gamma, col, at.n, 1.f);
-  load_vec(gate, a.gmode == kGateOne ? op.gate : nullptr, col, at.n, 1.f);
-  float dpg[NV][8] = {}, dpb[NV][8] = {}, dqg[NV][8] = {}, dqb[NV][8] = {}, dg[NV][8] = {};
+  float st[NV][8] = {}, sb[NV][8] = {}, dqg[NV][8] = {}, dqb[NV][8] = {};
+  float dpg[MANY ? NV : 1][8] = {}, dpb[MANY ? NV : 1][8] = {};
   const int64_t last = op.rows - 1;
-  int64_t g = a.gmode == kGateGroup ? find_group(op.gate_ptr, op.n_gates, at.r0) : 0, held = -1;
-  // the gate's sums of a group that ends here: into dgate if all its rows are
-  // this walker's, else into one of its two slots (first: the group began
-  // before its rows)
-  auto flush = [&]() {
-    if (held < 0) return;
+  Gates gates(a, at.r0);
+  auto vec = [&](const float* p, int c, float other) { return p != nullptr ? p[c] : other; };
+  // The sums st and sb of a gate become those of the vectors.  dgate goes to
+  // its place if all the group's rows are this walker's, else into one of its
+  // two slots (first: the group began before its rows).
+  auto settle = [&](int64_t held) {
+    const float* gate = op.gate + held * op.cols;
+    float* to = nullptr;
+    bool add = a.grads.accumulate;
     if (a.grads.gate != nullptr) {
-      const int64_t p0 = op.gate_ptr[held], p1 = op.gate_ptr[held + 1];
-      const bool head = p0 < at.r0, tail = p1 > at.r1;
-      float* to = head || tail ? a.slots + (at.walker * 2 + (head ? 0 : 1)) * op.cols : a.grads.gate + held * op.cols;
-      const bool add = !(head || tail) && a.grads.accumulate;
-#pragma unroll
-      for (int k = 0; k < NV; ++k)
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (e < at.n[k]) to[col[k] + e] = add ? to[col[k] + e] + dg[k][e] : dg[k][e];
-    }
-#pragma unroll
-    for (int k = 0; k < NV; ++k)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) dg[k][e] = 0.f;
-  };
-  for (int64_t i = 0; i < a.per; ++i) {
-    const int64_t r = at.r0 + i, rr = min(r, last);
-    bool mine = r < at.r1;
-    float x[NV][8], b[NV][8], t[NV][8], z[NV][8];
-    const float4 st = ((const float4*)a.stats)[rr];
-#pragma unroll
-    for (int k = 0; k < NV; ++k) {
-      const Raw8<XT> rx = load8((const XT*)a.x.data + rr * a.x.ld + col[k], at.n[k]);
-      const Raw8<BT> rb = load8((const BT*)a.b.data + rr * a.b.ld + col[k], at.n[k]);
-      const Raw8<XT> ry = load8((const XT*)a.dy.data + rr * a.dy.ld + col[k], a.dy.data ? at.n[k] : 0);
-      const Raw8<BT> rz = load8((const BT*)a.dz.data + rr * a.dz.ld + col[k], a.dz.data ? at.n[k] : 0);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        x[k][e] = rx.get(e);
-        b[k][e] = rb.get(e);
-        t[k][e] = ry.get(e);
-        z[k][e] = rz.get(e);
-      }
-    }
-    if (a.gmode == kGateGroup && mine) {
-      while (g + 1 < op.n_gates && r >= op.gate_ptr[g + 1]) ++g;
-      mine = r >= op.gate_ptr[g] && r < op.gate_ptr[g + 1];
-      if (mine && g != held) {
-        flush();
-        load_vec(gate, op.gate + g * op.cols, col, at.n, 1.f);
-        held = g;
-      }
-    }
-    if (a.gmode == kGateRow && mine) load_vec(gate, op.gate + r * op.cols, col, at.n, 1.f);
-    float p[NV][8];
-#pragma unroll
-    for (int k = 0; k < NV; ++k)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        p[k][e] = b[k][e];
-        if (op.post != MGN_NORM_NONE) {
-          b[k][e] = (b[k][e] - st.x) * st.y;  // bhat
-          p[k][e] = __builtin_fmaf(b[k][e], pg[k][e], pb[k][e]);
+      to = a.grads.gate + held * op.cols;
+      if (a.gmode == kGateGroup) {
+        const bool head = op.gate_ptr[held] < at.r0, tail = op.gate_ptr[held + 1] > at.r1;
+        if (head || tail) {
+          to = a.slots + (at.walker * 2 + (head ? 0 : 1)) * op.cols;
+          add = false;
         }
       }
+    }
+#pragma unroll
+    for (int k = 0; k < (MANY ? NV : 1); ++k) {
+      int c0 = col[k];
+      asm volatile("" : "+v"(c0));  // as in gate_vectors
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (e < at.n[k]) {
+          const int c = c0 + e;
+          const float v = op.scale * gate[c];
+          const float d = op.scale * (vec(op.post_gamma, c, 1.f) * sb[k][e] + vec(op.post_beta, c, 0.f) * st[k][e]);
+          dpg[k][e] = __builtin_fmaf(v, sb[k][e], dpg[k][e]);
+          dpb[k][e] = __builtin_fmaf(v, st[k][e], dpb[k][e]);
+          if (to != nullptr) to[c] = add ? to[c] + d : d;
+          st[k][e] = 0.f;
+          sb[k][e] = 0.f;
+        }
+    }
+  };
+  Raw8<XT> nx[NV], ny[NV];
+  Raw8<BT> nb[NV], nz[NV];
+  float4 ns;
+  auto fetch = [&](int64_t r) {
+    const int64_t rr = min(r, last);
+    ns = ((const float4*)a.stats)[rr];
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      nx[k] = load8((const XT*)a.x.data + rr * a.x.ld + col[k], at.n[k]);
+      nb[k] = load8((const BT*)a.b.data + rr * a.b.ld + col[k], at.n[k]);
+      ny[k] = load8((const XT*)a.dy.data + rr * a.dy.ld + col[k], a.dy.data ? at.n[k] : 0);
+      nz[k] = load8((const BT*)a.dz.data + rr * a.dz.ld + col[k], a.dz.data ? at.n[k] : 0);
+    }
+  };
+  if (PRE) fetch(at.r0);
+  int64_t open = -1;  // the gate that st and sb belong to
+  for (int64_t i = 0; i < a.per; ++i) {
+    const int64_t r = at.r0 + i;
+    bool fresh = false;
+    const bool mine = r < at.r1 && (!MANY || gates.at(a, r, fresh));
+    if (MANY && fresh) {
+      if (open >= 0) settle(open);
+      open = gates.held;
+      gate_vectors(ga, gb, a, open, col, at.n);
+    }
+    if (!PRE) fetch(r);
+    float x[NV][8], b[NV][8], t[NV][8], z[NV][8];
+    const float4 s = ns;
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        x[k][e] = nx[k].get(e);
+        b[k][e] = (nb[k].get(e) - s.x) * s.y;  // bhat (b itself without a norm: statistics 0 and 1)
+        t[k][e] = mine ? ny[k].get(e) : 0.f;
+        z[k][e] = mine ? nz[k].get(e) : 0.f;
+      }
+    if (PRE && i + 1 < a.per) fetch(r + 1);
     if (op.pre != MGN_NORM_NONE && a.dz.data != nullptr) {
       float s1 = 0.f, s2 = 0.f;
 #pragma unroll
       for (int k = 0; k < NV; ++k)
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          const float y = __builtin_fmaf(op.scale, gate[k][e] * p[k][e], op.skip * x[k][e]);
-          const float yhat = (y - st.z) * st.w, u = z[k][e] * qg[k][e];
-          if (mine && e < at.n[k]) {
-            dqb[k][e] += z[k][e];
-            dqg[k][e] = __builtin_fmaf(z[k][e], yhat, dqg[k][e]);
-            s1 += u;
-            s2 = __builtin_fmaf(u, yhat, s2);
-          }
-          x[k][e] = yhat;
+          const float y = __builtin_fmaf(op.skip, x[k][e], __builtin_fmaf(b[k][e], ga[k][e], gb[k][e]));
+          x[k][e] = mine ? (y - s.z) * s.w : 0.f;  // yhat
+          dqb[k][e] += z[k][e];
+          dqg[k][e] = __builtin_fmaf(z[k][e], x[k][e], dqg[k][e]);
+          z[k][e] *= qg[k][e];
+          s1 += z[k][e];
+          s2 = __builtin_fmaf(z[k][e], x[k][e], s2);
         }
       red.sum2(s1, s2);
       s1 = op.pre == MGN_NORM_LAYER ? s1 * inv : 0.f;
@@ -312,7 +359,7 @@ __global__ void __launch_bounds__(LPR ? 256 : 1024) k_norm_gate_bwd(NormGate a) 
       for (int k = 0; k < NV; ++k)
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-          t[k][e] = __builtin_fmaf(st.w, z[k][e] * qg[k][e] - s1 - x[k][e] * s2, t[k][e]);
+          t[k][e] = mine && e < at.n[k] ? __builtin_fmaf(s.w, z[k][e] - s1 - x[k][e] * s2, t[k][e]) : 0.f;
     }
     float s1 = 0.f, s2 = 0.f;
 #pragma unroll
@@ -321,16 +368,12 @@ __global__ void __launch_bounds__(LPR ? 256 : 1024) k_norm_gate_bwd(NormGate a) 
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         dx[e] = op.skip * t[k][e];
-        const float dgv = op.scale * (p[k][e] * t[k][e]);
-        const float dp = op.scale * (gate[k][e] * t[k][e]), u = dp * pg[k][e];
-        if (mine && e < at.n[k]) {
-          dg[k][e] = a.gmode == kGateRow ? dgv : dg[k][e] + dgv;
-          dpb[k][e] += dp;
-          dpg[k][e] = __builtin_fmaf(dp, b[k][e], dpg[k][e]);
-          s1 += u;
-          s2 = __builtin_fmaf(u, b[k][e], s2);
-        }
-        t[k][e] = op.post != MGN_NORM_NONE ? u : dp;
+        if (!mine) b[k][e] = 0.f;
+        st[k][e] += t[k][e];
+        sb[k][e] = __builtin_fmaf(t[k][e], b[k][e], sb[k][e]);
+        t[k][e] *= ga[k][e];  // gamma dp
+        s1 += t[k][e];
+        s2 = __builtin_fmaf(t[k][e], b[k][e], s2);
       }
       if (mine) store8((XT*)a.dx.data + r * a.dx.ld + col[k], at.n[k], dx);
     }
@@ -341,24 +384,16 @@ __global__ void __launch_bounds__(LPR ? 256 : 1024) k_norm_gate_bwd(NormGate a) 
 #pragma unroll
       for (int k = 0; k < NV; ++k)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) t[k][e] = st.y * (t[k][e] - s1 - b[k][e] * s2);
+        for (int e = 0; e < 8; ++e) t[k][e] = s.y * (t[k][e] - s1 - b[k][e] * s2);
     }
 #pragma unroll
     for (int k = 0; k < NV; ++k)
       if (mine) store8((BT*)a.db.data + r * a.db.ld + col[k], at.n[k], t[k]);
-    if (a.gmode == kGateRow && mine && a.grads.gate != nullptr) {
-      float* to = a.grads.gate + r * op.cols;
-#pragma unroll
-      for (int k = 0; k < NV; ++k)
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (e < at.n[k]) to[col[k] + e] = a.grads.accumulate ? to[col[k] + e] + dg[k][e] : dg[k][e];
-    }
   }
-  if (a.gmode == kGateGroup) flush();
+  if (MANY && open >= 0) settle(open);
   // the block's sums, one vector after the other
   float* part = a.part + (int64_t)blockIdx.x * 5 * op.cols;
-  auto put = [&](int which, const float (&v)[NV][8]) {
+  auto put = [&](int which, auto value) {
     if constexpr (LPR != 0) {
       const int w = threadIdx.x / LPR, nw = blockDim.x / LPR;
       __syncthreads();
@@ -366,7 +401,7 @@ __global__ void __launch_bounds__(LPR ? 256 : 1024) k_norm_gate_bwd(NormGate a) 
       for (int k = 0; k < NV; ++k)
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-          if (e < at.n[k]) sums[w * op.cols + col[k] + e] = v[k][e];
+          if (e < at.n[k]) sums[w * op.cols + col[k] + e] = value(k, e, col[k] + e);
       __syncthreads();
       for (int c = threadIdx.x; c < op.cols; c += blockDim.x) {
         float s = 0.f;
@@ -378,18 +413,50 @@ __global__ void __launch_bounds__(LPR ? 256 : 1024) k_norm_gate_bwd(NormGate a) 
       for (int k = 0; k < NV; ++k)
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-          if (e < at.n[k]) part[which * op.cols + col[k] + e] = v[k][e];
+          if (e < at.n[k]) part[which * op.cols + col[k] + e] = value(k, e, col[k] + e);
     }
   };
-  if (a.grads.post_gamma != nullptr) put(0, dpg);
-  if (a.grads.post_beta != nullptr) put(1, dpb);
-  if (a.grads.pre_gamma != nullptr) put(2, dqg);
-  if (a.grads.pre_beta != nullptr) put(3, dqb);
-  if (a.grads.gate != nullptr && a.gmode == kGateOne) put(4, dg);
+  const float* one = a.gmode == kGateOne ? op.gate : nullptr;
+  if (a.grads.post_gamma != nullptr)
+    put(0, [&](int k, int e, int c) { return MANY ? dpg[MANY ? k : 0][e] : op.scale * vec(one, c, 1.f) * sb[k][e]; });
+  if (a.grads.post_beta != nullptr)
+    put(1, [&](int k, int e, int c) { return MANY ? dpb[MANY ? k : 0][e] : op.scale * vec(one, c, 1.f) * st[k][e]; });
+  if (a.grads.pre_gamma != nullptr) put(2, [&](int k, int e, int) { return dqg[k][e]; });
+  if (a.grads.pre_beta != nullptr) put(3, [&](int k, int e, int) { return dqb[k][e]; });
+  if (a.grads.gate != nullptr && one != nullptr)
+    put(4, [&](int k, int e, int c) {
+      return op.scale * (vec(op.post_gamma, c, 1.f) * sb[k][e] + vec(op.post_beta, c, 0.f) * st[k][e]);
+    });
 }
 
-// Sums over blocks of up to five vectors: 64 columns x 16 groups of rows a
-// block, each group's rows and then the groups in order.
+// Sums over rows of partial sums, 16 columns x 64 groups of rows a block: a
+// group's rows in order, then the groups in order.
+constexpr int kSumCols = 16, kSumGroups = 64;
+template <typename F>
+__device__ __forceinline__ float column_sum(int64_t n, bool in, F value) {
+  __shared__ float s[kSumGroups][kSumCols + 1];
+  const int c = threadIdx.x % kSumCols, g = threadIdx.x / kSumCols;
+  float v = 0.f;
+  if (in) {
+#pragma unroll 4
+    for (int64_t b = g; b < n; b += kSumGroups) v += value(b);
+  }
+  s[g][c] = v;
+  __syncthreads();
+  float u = 0.f;
+  if (g < 8) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) u += s[8 * g + j][c];
+  }
+  __syncthreads();
+  if (g < 8) s[g][c] = u;
+  __syncthreads();
+  u = 0.f;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) u += s[j][c];
+  return u;  // of column c, for every group
+}
+
 struct ColumnSums {
   const float* part;
   int64_t nb, stride, cols;
@@ -397,52 +464,33 @@ struct ColumnSums {
   int32_t accumulate;
 };
 __global__ void __launch_bounds__(1024) k_column_sums(ColumnSums a) {
-  __shared__ float s[16][64];
-  const int c = threadIdx.x & 63, g = threadIdx.x >> 6;
-  const int64_t col = (int64_t)blockIdx.x * 64 + c;
+  const int64_t col = (int64_t)blockIdx.x * kSumCols + threadIdx.x % kSumCols;
   float* out = a.out[blockIdx.y];
   if (out == nullptr) return;  // the whole block
   const float* p = a.part + blockIdx.y * a.cols + col;
-  float v = 0.f;
-  if (col < a.cols)
-    for (int64_t b = g; b < a.nb; b += 16) v += p[b * a.stride];
-  s[g][c] = v;
-  __syncthreads();
-  if (g == 0 && col < a.cols) {
-    float t = a.accumulate ? out[col] : 0.f;
-    float u = 0.f;
-    for (int j = 0; j < 16; ++j) u += s[j][c];
-    out[col] = t + u;
-  }
+  const float v = column_sum(a.nb, col < a.cols, [&](int64_t b) { return p[b * a.stride]; });
+  if (threadIdx.x < kSumCols && col < a.cols) out[col] = a.accumulate ? out[col] + v : v;
 }
 
-// dgate rows of the groups that several walkers share, summed in the walkers'
-// order, and zeros for groups without rows.
+// dgate rows of the groups that several walkers share, and zeros for groups
+// without rows.
 __global__ void __launch_bounds__(1024) k_gate_slots(NormGate a) {
-  __shared__ float s[16][64];
   const mgn_norm_gate& op = a.op;
-  const int c = threadIdx.x & 63, q = threadIdx.x >> 6;
-  const int col = blockIdx.y * 64 + c;
-  const int64_t g = blockIdx.x;
-  const int64_t p0 = max((int64_t)op.gate_ptr[g], (int64_t)0), p1 = min((int64_t)op.gate_ptr[g + 1], op.rows);
+  const int col = blockIdx.y * kSumCols + threadIdx.x % kSumCols;
+  const int64_t g = blockIdx.x, b0 = op.gate_ptr[g], b1 = op.gate_ptr[g + 1];
+  const int64_t p0 = max(b0, (int64_t)0), p1 = min(b1, op.rows);
   const bool none = p1 <= p0;
-  const int64_t w0 = none ? 0 : p0 / a.per, w1 = none ? 0 : (p1 - 1) / a.per;
+  const int64_t w0 = none ? 0 : p0 / a.per, w1 = none ? -1 : (p1 - 1) / a.per;
   // one walker's rows only: it has written the sums itself (its last row may
   // be the group's)
-  if (!none && w0 == w1 && op.gate_ptr[g] >= w0 * a.per && op.gate_ptr[g + 1] <= min((w0 + 1) * a.per, op.rows)) return;
-  float v = 0.f;
-  if (!none && col < op.cols)
-    for (int64_t w = w0 + q; w <= w1; w += 16) {
-      const bool head = op.gate_ptr[g] < w * a.per;
-      v += a.slots[(w * 2 + (head ? 0 : 1)) * op.cols + col];
-    }
-  s[q][c] = v;
-  __syncthreads();
-  if (q == 0 && col < op.cols) {
-    float u = 0.f;
-    for (int j = 0; j < 16; ++j) u += s[j][c];
+  if (!none && w0 == w1 && b0 >= w0 * a.per && b1 <= min((w0 + 1) * a.per, op.rows)) return;
+  const float v = column_sum(w1 - w0 + 1, col < op.cols, [&](int64_t i) {
+    const int64_t w = w0 + i;
+    return a.slots[(w * 2 + (b0 < w * a.per ? 0 : 1)) * op.cols + col];
+  });
+  if (threadIdx.x < kSumCols && col < op.cols) {
     float* to = a.grads.gate + g * op.cols + col;
-    *to = a.grads.accumulate ? *to + u : u;
+    *to = a.grads.accumulate ? *to + v : v;
   }
 }
 
@@ -457,45 +505,72 @@ NormPlan norm_plan(int64_t rows, int cols, bool backward) {
   p.lpr = lanes <= 16 ? 16 : lanes <= 32 ? 32 : lanes <= 64 ? 64 : 0;
   p.threads = p.lpr ? 256 : (lanes + 63) / 64 * 64;
   const int per_block = p.lpr ? 256 / p.lpr : 1;
-  // threads in flight: 256 CUs
-  const int64_t most = std::max<int64_t>(1, 256 * (backward ? 1024 : 2048) / p.threads) * per_block;
+  // as many blocks as run at a time on 256 CUs: by registers 20 waves of the
+  // forward fit a CU, 12 of the reverse (16 in blocks of 1024)
+  const int waves = p.threads / 64;
+  const int64_t most = 256 * std::max(1, (backward ? 12 : 20) / waves) * per_block;
   p.per = std::max<int64_t>(1, ceil_div(rows, most));
   p.blocks = ceil_div(ceil_div(rows, p.per), per_block);
   p.walkers = p.blocks * per_block;
   return p;
 }
 
-#define MGN_NG_LAUNCH(K, XT, BT)                                                                       \
-  do {                                                                                                 \
-    if (p.lpr == 16)                                                                                   \
-      hipLaunchKernelGGL((K<XT, BT, 16, 1>), dim3((unsigned)p.blocks), dim3(p.threads), lds, s, a);    \
-    else if (p.lpr == 32)                                                                              \
-      hipLaunchKernelGGL((K<XT, BT, 32, 1>), dim3((unsigned)p.blocks), dim3(p.threads), lds, s, a);    \
-    else if (p.lpr == 64)                                                                              \
-      hipLaunchKernelGGL((K<XT, BT, 64, 1>), dim3((unsigned)p.blocks), dim3(p.threads), lds, s, a);    \
-    else if (p.vpt == 8)                                                                               \
-      hipLaunchKernelGGL((K<XT, BT, 0, 1>), dim3((unsigned)p.blocks), dim3(p.threads), lds, s, a);     \
-    else                                                                                               \
-      hipLaunchKernelGGL((K<XT, BT, 0, 2>), dim3((unsigned)p.blocks), dim3(p.threads), lds, s, a);     \
+// The instantiation for a plan: K(lanes, runs of a lane, most threads).
+#define MGN_NG_PLAN(K)                   \
+  do {                                   \
+    if (p.lpr == 16)                     \
+      K(16, 1, 256);                     \
+    else if (p.lpr == 32)                \
+      K(32, 1, 256);                     \
+    else if (p.lpr == 64)                \
+      K(64, 1, 256);                     \
+    else if (p.vpt == 16)                \
+      K(0, 2, 1024);                     \
+    else if (p.threads <= 512)           \
+      K(0, 1, 512);                      \
+    else if (p.threads <= 640)           \
+      K(0, 1, 640);                      \
+    else                                 \
+      K(0, 1, 1024);                     \
   } while (0)
-#define MGN_NG_TYPES(K)                                           \
-  do {                                                            \
-    if (a.op.x_type == MGN_FP32 && a.op.b_type == MGN_FP32)       \
-      MGN_NG_LAUNCH(K, float, float);                             \
-    else if (a.op.x_type == MGN_FP32)                             \
-      MGN_NG_LAUNCH(K, float, bf16);                              \
-    else if (a.op.b_type == MGN_FP32)                             \
-      MGN_NG_LAUNCH(K, bf16, float);                              \
-    else                                                          \
-      MGN_NG_LAUNCH(K, bf16, bf16);                               \
+
+template <typename XT, typename BT>
+void launch_fwd(const NormGate& a, const NormPlan& p, hipStream_t s) {
+  const dim3 g((unsigned)p.blocks), t(p.threads);
+#define MGN_NG_FWD(L, NV, MAXT) hipLaunchKernelGGL((k_norm_gate_fwd<XT, BT, L, NV, MAXT>), g, t, 0, s, a)
+  MGN_NG_PLAN(MGN_NG_FWD);
+}
+template <typename XT, typename BT, bool MANY>
+void launch_bwd(const NormGate& a, const NormPlan& p, hipStream_t s) {
+  const dim3 g((unsigned)p.blocks), t(p.threads);
+  const size_t lds = p.lpr ? (size_t)(p.threads / p.lpr) * a.op.cols * 4 : 0;
+#define MGN_NG_BWD(L, NV, MAXT) hipLaunchKernelGGL((k_norm_gate_bwd<XT, BT, L, NV, MAXT, MANY>), g, t, lds, s, a)
+  MGN_NG_PLAN(MGN_NG_BWD);
+}
+template <typename XT, typename BT>
+void launch_bwd(const NormGate& a, const NormPlan& p, hipStream_t s) {
+  if (a.gmode == kGateRow || a.gmode == kGateGroup)
+    launch_bwd<XT, BT, true>(a, p, s);
+  else
+    launch_bwd<XT, BT, false>(a, p, s);
+}
+#define MGN_NG_TYPES(LAUNCH)                                \
+  do {                                                      \
+    if (a.op.x_type == MGN_FP32 && a.op.b_type == MGN_FP32) \
+      LAUNCH<float, float>(a, p, s);                        \
+    else if (a.op.x_type == MGN_FP32)                       \
+      LAUNCH<float, bf16>(a, p, s);                         \
+    else if (a.op.b_type == MGN_FP32)                       \
+      LAUNCH<bf16, float>(a, p, s);                         \
+    else                                                    \
+      LAUNCH<bf16, bf16>(a, p, s);                          \
   } while (0)
 
 hipError_t launch_norm_gate_forward(const NormGate& in, hipStream_t s) {
   NormGate a = in;
   const NormPlan p = norm_plan(a.op.rows, a.op.cols, false);
   a.per = p.per;
-  const size_t lds = 0;
-  MGN_NG_TYPES(k_norm_gate_fwd);
+  MGN_NG_TYPES(launch_fwd);
   return hipGetLastError();
 }
 
@@ -504,8 +579,7 @@ hipError_t launch_norm_gate_backward(const NormGate& in, hipStream_t s) {
   const NormPlan p = norm_plan(a.op.rows, a.op.cols, true);
   a.per = p.per;
   if (p.blocks > 0) {
-    const size_t lds = p.lpr ? (size_t)(p.threads / p.lpr) * a.op.cols * 4 : 0;
-    MGN_NG_TYPES(k_norm_gate_bwd);
+    MGN_NG_TYPES(launch_bwd);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
@@ -515,12 +589,12 @@ hipError_t launch_norm_gate_backward(const NormGate& in, hipStream_t s) {
                           {a.grads.post_gamma, a.grads.post_beta, a.grads.pre_gamma, a.grads.pre_beta,
                            one ? a.grads.gate : nullptr},
                           a.grads.accumulate};
-    hipLaunchKernelGGL(k_column_sums, dim3((a.op.cols + 63) / 64, 5), dim3(1024), 0, s, c);
+    hipLaunchKernelGGL(k_column_sums, dim3((a.op.cols + kSumCols - 1) / kSumCols, 5), dim3(1024), 0, s, c);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
   if (a.gmode == kGateGroup && a.grads.gate) {
-    hipLaunchKernelGGL(k_gate_slots, dim3((unsigned)a.op.n_gates, (a.op.cols + 63) / 64), dim3(1024), 0, s, a);
+    hipLaunchKernelGGL(k_gate_slots, dim3((unsigned)a.op.n_gates, (a.op.cols + kSumCols - 1) / kSumCols), dim3(1024), 0, s, a);
     return hipGetLastError();
   }
   return hipSuccess;
@@ -529,7 +603,7 @@ hipError_t launch_norm_gate_backward(const NormGate& in, hipStream_t s) {
 hipError_t launch_column_reduce(const float* part, int64_t nb, int64_t stride, int64_t cols, float* out,
                                 int32_t accumulate, hipStream_t s) {
   const ColumnSums c = {part, nb, stride, cols, {out, nullptr, nullptr, nullptr, nullptr}, accumulate};
-  hipLaunchKernelGGL(k_column_sums, dim3((unsigned)((cols + 63) / 64), 1), dim3(1024), 0, s, c);
+  hipLaunchKernelGGL(k_column_sums, dim3((unsigned)ceil_div(cols, kSumCols), 1), dim3(1024), 0, s, c);
   return hipGetLastError();
 }
 

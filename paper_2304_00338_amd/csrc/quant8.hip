@@ -58,31 +58,40 @@ __device__ __forceinline__ float scale_of(uint32_t amax, float& inv) {
   return s;
 }
 
-// x / s as a float that rounds to the format as the quotient itself does.
+// Whether t = x * inv may round to another number of the format than x / s.
 template <int F>
-__device__ __forceinline__ float quotient(float x, float s, float inv) {
+__device__ __forceinline__ bool unsure(float t) {
   constexpr uint32_t mask = (1u << Format<F>::low) - 1, half = 1u << (Format<F>::low - 1);
-  if (inv == 0.f) return 0.f;
-  float t = x * inv;
   const uint32_t b = abs_bits(t);
-  const bool unsure = ((b - half + 4) & mask) <= 8 || (t != 0.f && b < __float_as_uint(Format<F>::normal) + 8);
-  if (unsure) {
-    // rounded to odd: the last bit remembers what the quotient has beyond it
-    const double d = (double)x / (double)s;
-    t = (float)d;
-    const double e = (double)t;
-    uint32_t u = __float_as_uint(t);
-    if (e != d && (u & 1) == 0) u += fabs(e) < fabs(d) ? 1 : -1;
-    t = __uint_as_float(u);
-  }
-  return fminf(fmaxf(t, -Format<F>::most), Format<F>::most);
+  return ((b - half + 4) & mask) <= 8 || (t != 0.f && b < __float_as_uint(Format<F>::normal) + 8);
+}
+
+// x / s as a float that rounds to the format as the quotient itself does:
+// rounded to odd, so that the last bit remembers what the quotient has beyond it.
+__device__ __forceinline__ float quotient(float x, float s) {
+  const double d = (double)x / (double)s;
+  const float t = (float)d;
+  uint32_t u = __float_as_uint(t);
+  if ((double)t != d && (u & 1) == 0) u += fabs((double)t) < fabs(d) ? 1 : -1;
+  return __uint_as_float(u);
 }
 
 template <int F>
-__device__ __forceinline__ uint2 numbers8(const float (&v)[8], const float (&s)[8], const float (&inv)[8]) {
+__device__ __forceinline__ uint2 numbers8(const float (&v)[8], float s, float inv) {
   float t[8];
+  bool slow = false;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) t[e] = quotient<F>(v[e], s[e], inv[e]);
+  for (int e = 0; e < 8; ++e) {
+    t[e] = inv == 0.f ? 0.f : v[e] * inv;
+    slow |= unsure<F>(t[e]);
+  }
+  if (slow) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (unsure<F>(t[e])) t[e] = quotient(v[e], s);
+  }
+#pragma unroll
+  for (int e = 0; e < 8; ++e) t[e] = fminf(fmaxf(t[e], -Format<F>::most), Format<F>::most);
   uint2 r;
   r.x = Format<F>::pack(t[2], t[3], Format<F>::pack(t[0], t[1], 0, false), true);
   r.y = Format<F>::pack(t[6], t[7], Format<F>::pack(t[4], t[5], 0, false), true);
@@ -116,7 +125,7 @@ __global__ void __launch_bounds__(256) k_quant_rows(Quant8 a) {
 #pragma unroll
   for (int k = 0; k < kChunk; ++k) {
     const int64_t c = (k0 + k) * 128 + l * 8;
-    float v[8], s[8], inv[8];
+    float v[8], s, inv;
     uint32_t m = 0;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
@@ -124,19 +133,15 @@ __global__ void __launch_bounds__(256) k_quant_rows(Quant8 a) {
       m = max(m, abs_bits(v[e]));
     }
     m = max16(m);
-    s[0] = scale_of<F>(m, inv[0]);
-#pragma unroll
-    for (int e = 1; e < 8; ++e) {
-      s[e] = s[0];
-      inv[e] = inv[0];
-    }
+    s = scale_of<F>(m, inv);
     if (k0 + k >= cb) break;
     // 8 bytes: whole inside the row's zero padding to 16 bytes, or beyond it
     if (c < ((a.cols + 15) & ~15LL)) *(uint2*)(a.q + r * a.ldq + c) = numbers8<F>(v, s, inv);
-    if (l == 0) a.scale[(k0 + k) * a.rows + r] = s[0];
+    if (l == 0) a.scale[(k0 + k) * a.rows + r] = s;
   }
 }
 
+constexpr int64_t kTileBlocks = 1024;  // of k_quant_tile, four a CU
 constexpr int kColLd = 132;  // bytes of a column in LDS: 16 lanes' 8-byte pieces in distinct banks
 
 template <typename XT, int F>
@@ -144,119 +149,117 @@ __global__ void __launch_bounds__(256) k_quant_tile(Quant8 a) {
   __shared__ __align__(16) uint8_t turned[128 * kColLd];
   __shared__ uint32_t cmax[16][128];
   __shared__ float csum[16][128];
-  __shared__ uint32_t wmax[4];
+  __shared__ uint32_t wmax[2][4];  // in turn: a block of waves may be a tile ahead
   const int l = threadIdx.x & 15, g = threadIdx.x >> 4;
   const int64_t cbs = ceil_div(a.cols, 128), rbs = ceil_div(a.rows, 128);
-  const int64_t rb = blockIdx.x / cbs, cb = blockIdx.x % cbs;
-  const int64_t c0 = cb * 128 + l * 8, r0 = rb * 128 + g * 8;
-  const int n = (int)min(max(a.cols - c0, (int64_t)0), (int64_t)8);
+  const int64_t cb = blockIdx.x % cbs, run = blockIdx.x / cbs;
   const int64_t up_cols = (a.cols + 15) & ~15LL, up_rows = (a.rows + 15) & ~15LL;
-  Raw8<XT> raw[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int64_t r = min(r0 + i, a.rows - 1);
-    raw[i] = load8((const XT*)a.x + r * a.ldx + c0, r0 + i < a.rows ? n : 0);
-  }
-  uint32_t rmax[8], cm[8];
-  float cs[8];
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    cm[e] = 0;
-    cs[e] = 0.f;
-  }
-  uint32_t all = 0;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    rmax[i] = 0;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const float f = raw[i].get(e);
-      const uint32_t m = abs_bits(f);
-      rmax[i] = max(rmax[i], m);
-      cm[e] = max(cm[e], m);
-      cs[e] += f;
-    }
-    all = max(all, rmax[i]);
-  }
   const bool square = a.block_rows == 128, turn = a.qt != nullptr;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    if (turn && !square) cmax[g][l * 8 + e] = cm[e];
-    if (a.colsum != nullptr) csum[g][l * 8 + e] = cs[e];
-  }
-  if (square) {
-    all = max16(all);
-    uint32_t w = 0;
-#pragma unroll
-    for (int j = 0; j < 64; j += 16) w = max(w, (uint32_t)__builtin_amdgcn_readlane((int)all, j));
-    if ((threadIdx.x & 63) == 0) wmax[threadIdx.x >> 6] = w;
-  }
-  __syncthreads();
-  float s1 = 0.f, i1 = 0.f;
-  if (square) {
-    s1 = scale_of<F>(max(max(wmax[0], wmax[1]), max(wmax[2], wmax[3])), i1);
-    if (threadIdx.x == 0) {
-      if (a.q != nullptr) a.scale[cb * rbs + rb] = s1;
-      if (turn) a.scale_t[rb * cbs + cb] = s1;
-    }
-  }
-  if (a.colsum != nullptr && threadIdx.x < 128) {
-    const int64_t c = cb * 128 + threadIdx.x;
-    float t = 0.f;
-#pragma unroll
-    for (int j = 0; j < 16; ++j) t += csum[j][threadIdx.x];
-    if (c < a.cols) a.part[rb * a.cols + c] = t;
-  }
-  if (a.q != nullptr) {
+  float cs[8] = {};
+  for (int64_t rb = run * a.per; rb < min((run + 1) * a.per, rbs); ++rb) {
+    // the lane's columns are opaque, or the addresses of all its rows are kept
+    // in registers from tile to tile
+    int lc = l * 8;
+    asm volatile("" : "+v"(lc));
+    const int64_t r0 = rb * 128 + g * 8, c0 = cb * 128 + lc;
+    const int n = (int)min(max(a.cols - c0, (int64_t)0), (int64_t)8);
+    Raw8<XT> raw[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      float v[8], s[8], inv[8];
-      float rs = s1, ri = i1;
-      if (!square) rs = scale_of<F>(max16(rmax[i]), ri);
+      const int64_t r = min(r0 + i, a.rows - 1);
+      raw[i] = load8((const XT*)a.x + r * a.ldx + c0, r0 + i < a.rows ? n : 0);
+    }
+    uint32_t rmax[8], cm[8] = {};
+    uint32_t all = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      rmax[i] = 0;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        v[e] = raw[i].get(e);
-        s[e] = rs;
-        inv[e] = ri;
+        const float f = raw[i].get(e);
+        const uint32_t m = abs_bits(f);
+        rmax[i] = max(rmax[i], m);
+        cm[e] = max(cm[e], m);
+        cs[e] += f;
       }
-      if (r0 + i < a.rows) {
-        if (c0 < up_cols) *(uint2*)(a.q + (r0 + i) * a.ldq + c0) = numbers8<F>(v, s, inv);
-        if (!square && l == 0) a.scale[cb * a.rows + r0 + i] = rs;
+      all = max(all, rmax[i]);
+    }
+    if (turn && !square) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) cmax[g][l * 8 + e] = cm[e];
+    }
+    if (square) {
+      all = max16(all);
+      uint32_t w = 0;
+#pragma unroll
+      for (int j = 0; j < 64; j += 16) w = max(w, (uint32_t)__builtin_amdgcn_readlane((int)all, j));
+      if ((threadIdx.x & 63) == 0) wmax[rb & 1][threadIdx.x >> 6] = w;
+    }
+    __syncthreads();
+    float s1 = 0.f, i1 = 0.f;
+    if (square) {
+      const uint32_t* w = wmax[rb & 1];
+      s1 = scale_of<F>(max(max(w[0], w[1]), max(w[2], w[3])), i1);
+      if (threadIdx.x == 0) {
+        if (a.q != nullptr) a.scale[cb * rbs + rb] = s1;
+        if (turn) a.scale_t[rb * cbs + cb] = s1;
+      }
+    }
+    if (a.q != nullptr) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        float v[8], s = s1, inv = i1;
+        if (!square) s = scale_of<F>(max16(rmax[i]), inv);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = raw[i].get(e);
+        __builtin_amdgcn_sched_barrier(0);  // one row at a time, for the registers
+        if (r0 + i < a.rows) {
+          if (c0 < up_cols) *(uint2*)(a.q + (r0 + i) * a.ldq + c0) = numbers8<F>(v, s, inv);
+          if (!square && l == 0) a.scale[cb * a.rows + r0 + i] = s;
+        }
+      }
+    }
+    if (turn) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        float v[8], s = s1, inv = i1;
+        if (!square) {
+          uint32_t m = 0;
+#pragma unroll
+          for (int j = 0; j < 16; ++j) m = max(m, cmax[j][l * 8 + e]);
+          s = scale_of<F>(m, inv);
+          if (g == 0 && c0 + e < a.cols) a.scale_t[rb * a.cols + c0 + e] = s;
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = raw[i].get(e);
+        const uint2 p = numbers8<F>(v, s, inv);
+        uint32_t* to = (uint32_t*)(turned + (l * 8 + e) * kColLd + g * 8);
+        to[0] = p.x;
+        to[1] = p.y;
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      __syncthreads();
+      const int64_t c = cb * 128 + (threadIdx.x >> 1);
+      if (c < a.cols) {
+        const uint32_t* from = (const uint32_t*)(turned + (threadIdx.x >> 1) * kColLd + (threadIdx.x & 1) * 64);
+        const int64_t r = rb * 128 + (threadIdx.x & 1) * 64;
+        uint8_t* to = a.qt + c * a.ldqt + r;
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          if (r + 16 * k < up_rows) *(uint4*)(to + 16 * k) = uint4{from[4 * k], from[4 * k + 1], from[4 * k + 2], from[4 * k + 3]};
       }
     }
   }
-  if (turn) {
+  if (a.colsum != nullptr) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      float v[8], s[8], inv[8];
-      float es = s1, ei = i1;
-      if (!square) {
-        uint32_t m = 0;
-#pragma unroll
-        for (int j = 0; j < 16; ++j) m = max(m, cmax[j][l * 8 + e]);
-        es = scale_of<F>(m, ei);
-        if (g == 0 && c0 + e < a.cols) a.scale_t[rb * a.cols + c0 + e] = es;
-      }
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        v[i] = raw[i].get(e);
-        s[i] = es;
-        inv[i] = ei;
-      }
-      const uint2 p = numbers8<F>(v, s, inv);
-      uint32_t* to = (uint32_t*)(turned + (l * 8 + e) * kColLd + g * 8);
-      to[0] = p.x;
-      to[1] = p.y;
-    }
+    for (int e = 0; e < 8; ++e) csum[g][l * 8 + e] = cs[e];
     __syncthreads();
-    const int64_t c = cb * 128 + (threadIdx.x >> 1);
-    if (c < a.cols) {
-      const uint32_t* from = (const uint32_t*)(turned + (threadIdx.x >> 1) * kColLd + (threadIdx.x & 1) * 64);
-      const int64_t r = rb * 128 + (threadIdx.x & 1) * 64;
-      uint8_t* to = a.qt + c * a.ldqt + r;
+    const int64_t c = cb * 128 + threadIdx.x;
+    if (threadIdx.x < 128 && c < a.cols) {
+      float t = 0.f;
 #pragma unroll
-      for (int k = 0; k < 4; ++k)
-        if (r + 16 * k < up_rows) *(uint4*)(to + 16 * k) = uint4{from[4 * k], from[4 * k + 1], from[4 * k + 2], from[4 * k + 3]};
+      for (int j = 0; j < 16; ++j) t += csum[j][threadIdx.x];
+      a.part[run * a.cols + c] = t;
     }
   }
 }
@@ -265,8 +268,13 @@ __global__ void __launch_bounds__(256) k_quant_tile(Quant8 a) {
 
 using namespace dev;
 
-hipError_t launch_quant8(const Quant8& a, hipStream_t s) {
+hipError_t launch_quant8(const Quant8& in, hipStream_t s) {
+  Quant8 a = in;
   const int64_t cbs = ceil_div(a.cols, 128), rbs = ceil_div(a.rows, 128);
+  // blocks of k_quant_tile: with sums over the columns as many as run at a time,
+  // each leaving one row of partial sums
+  a.per = a.colsum ? std::max<int64_t>(1, rbs * cbs / kTileBlocks) : 1;
+  const int64_t runs = ceil_div(rbs, a.per);
 #define MGN_Q8(K, n)                                                                                 \
   do {                                                                                               \
     if (a.x_type == MGN_FP32 && a.format == MGN_E4M3)                                                \
@@ -282,11 +290,11 @@ hipError_t launch_quant8(const Quant8& a, hipStream_t s) {
     if (!a.qt && !a.colsum && a.block_rows == 1)
       MGN_Q8(k_quant_rows, ceil_div(a.rows, 16) * ceil_div(cbs, kChunk));
     else
-      MGN_Q8(k_quant_tile, rbs * cbs);
+      MGN_Q8(k_quant_tile, runs * cbs);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  if (a.colsum) return launch_column_reduce(a.part, rbs, a.cols, a.cols, a.colsum, a.accumulate, s);
+  if (a.colsum) return launch_column_reduce(a.part, runs, a.cols, a.cols, a.colsum, a.accumulate, s);
   return hipSuccess;
 }
 

@@ -21,8 +21,9 @@ struct Quant8 {
   int64_t ldq, ldqt;
   float *scale, *scale_t;
   float* colsum;  // nullable
-  float* part;    // [ceil(rows / 128)][cols] partial column sums
+  float* part;    // [at most ceil(rows / 128)][cols] partial column sums
   int32_t accumulate;
+  int64_t per;    // 128-row blocks that a block of k_quant_tile takes
 };
 hipError_t launch_quant8(const Quant8& a, hipStream_t s);
 
