@@ -5,15 +5,14 @@
 // Bound by memory: an element is read once (2 or 4 bytes) and written as one
 // byte a copy.  k_quant_rows (rows only, block_rows 1) gives 16 lanes to a
 // block of 128; k_quant_tile takes a tile of 128 x 128, lane (g, l) the rows
-// [8 g, 8 g + 8) of columns [8 l, 8 l + 8), so that a lane holds 8 consecutive
-// numbers of a row and of a column: rows are written from registers, the
-// transpose goes through LDS as 8-byte pieces of a column, and the column
-// maxima and sums need one step across the 16 row groups.
+// [4 g, 4 g + 4) of columns [8 l, 8 l + 8): rows are written from registers, the
+// transpose goes through LDS as 4-byte pieces of a column.  (With 8 rows a lane
+// the kernel needed 185 registers, two waves a SIMD.)
 //
-// The quotient is exact where it matters: x * fl(1 / scale) is within 2 ulp
-// of it, so it rounds as the quotient does unless it is that close to the
-// middle of two 8-bit numbers, or subnormal in the format; those elements
-// (some 2^-17 of all) are divided in double.
+// The quotient is exact where it matters: x times a reciprocal of the scale
+// is within 2 ulp of it, so it rounds as the quotient does unless it is that close to the
+// middle of two 8-bit numbers; groups of 4 or 8 with such an element (under 1 in
+// 10,000) are divided in double.
 #include "dev_common.hpp"
 #include "row_io.hpp"
 #include "row_ops.hpp"
@@ -21,8 +20,10 @@
 namespace mgn {
 namespace dev {
 
-__device__ __forceinline__ uint32_t abs_bits(float f) { return __float_as_uint(f) & 0x7fffffffu; }
-constexpr uint32_t kInfBits = 0x7f800000u;
+// The larger magnitude; a NaN wins.
+__device__ __forceinline__ float larger(float a, float b) {
+  return __builtin_elementwise_maximum(__builtin_fabsf(a), __builtin_fabsf(b));
+}
 
 template <int F>
 struct Format;
@@ -45,25 +46,23 @@ struct Format<MGN_E5M2> {
   }
 };
 
-// A block's scale and its reciprocal from the largest magnitude's bits (NaN
-// bits are above infinity's).  A block with a NaN or an infinity: inv 0.
+// A block's scale and a reciprocal of it (within an ulp) from its largest
+// magnitude.  A block with an infinity or a NaN: inv 0.  The division by the
+// constant F: with y the float nearest 1 / F, q = amax y and the exact remainder
+// r = amax - q F, q + r y rounds to the quotient's nearest float (Markstein); not
+// where r may be subnormal, so small values are divided as such.
 template <int F>
-__device__ __forceinline__ float scale_of(uint32_t amax, float& inv) {
-  if (amax >= kInfBits) {
+__device__ __forceinline__ float scale_of(float amax, float& inv) {
+  if (!(amax < __builtin_inff())) {
     inv = 0.f;
-    return __uint_as_float(0x7fc00000u);
+    return __builtin_nanf("");
   }
-  const float s = fmaxf(__uint_as_float(amax) / Format<F>::most, 0x1p-126f);
-  inv = 1.f / s;
+  constexpr float y = 1.f / Format<F>::most;
+  const float q = amax * y;
+  float s = __builtin_fmaf(__builtin_fmaf(-q, Format<F>::most, amax), y, q);
+  if (amax < 0x1p-90f) s = fmaxf(amax / Format<F>::most, 0x1p-126f);
+  inv = __builtin_amdgcn_rcpf(s);
   return s;
-}
-
-// Whether t = x * inv may round to another number of the format than x / s.
-template <int F>
-__device__ __forceinline__ bool unsure(float t) {
-  constexpr uint32_t mask = (1u << Format<F>::low) - 1, half = 1u << (Format<F>::low - 1);
-  const uint32_t b = abs_bits(t);
-  return ((b - half + 4) & mask) <= 8 || (t != 0.f && b < __float_as_uint(Format<F>::normal) + 8);
 }
 
 // x / s as a float that rounds to the format as the quotient itself does:
@@ -76,36 +75,48 @@ __device__ __forceinline__ float quotient(float x, float s) {
   return __uint_as_float(u);
 }
 
+// t: what rounds to the 8-bit numbers of v.  v * inv does for all N unless one
+// is within 4 ulp of the middle of two numbers; the smallest distance to that
+// (from -4 ulp on) is taken in units that wrap around at 2^32.  Below the
+// smallest normal number the numbers are spaced as between it and its double,
+// so it is added there.  No clamp: |v / s| is at most F (1 + 2^-23), which rounds
+// to F.
+template <int F, int N>
+__device__ __forceinline__ void to_numbers(float (&t)[N], const float (&v)[N], float s, float inv) {
+  constexpr int up = 32 - Format<F>::low;
+  constexpr uint32_t tie = 4u << up;
+  uint32_t near = ~0u;
+#pragma unroll
+  for (int e = 0; e < N; ++e) {
+    t[e] = v[e] * inv;
+    const float a = __builtin_fabsf(t[e]), w = a + (a < Format<F>::normal ? Format<F>::normal : 0.f);
+    near = min(near, (__float_as_uint(w) << up) + (0x80000000u + tie));
+  }
+  if (near <= 2 * tie || inv == 0.f) {
+#pragma unroll
+    for (int e = 0; e < N; ++e) t[e] = inv == 0.f ? 0.f : quotient(v[e], s);
+  }
+}
 template <int F>
-__device__ __forceinline__ uint2 numbers8(const float (&v)[8], float s, float inv) {
+__device__ __forceinline__ uint32_t numbers(const float (&v)[4], float s, float inv) {
+  float t[4];
+  to_numbers<F>(t, v, s, inv);
+  return Format<F>::pack(t[2], t[3], Format<F>::pack(t[0], t[1], 0, false), true);
+}
+template <int F>
+__device__ __forceinline__ uint2 numbers(const float (&v)[8], float s, float inv) {
   float t[8];
-  bool slow = false;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    t[e] = inv == 0.f ? 0.f : v[e] * inv;
-    slow |= unsure<F>(t[e]);
-  }
-  if (slow) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-      if (unsure<F>(t[e])) t[e] = quotient(v[e], s);
-  }
-#pragma unroll
-  for (int e = 0; e < 8; ++e) t[e] = fminf(fmaxf(t[e], -Format<F>::most), Format<F>::most);
-  uint2 r;
-  r.x = Format<F>::pack(t[2], t[3], Format<F>::pack(t[0], t[1], 0, false), true);
-  r.y = Format<F>::pack(t[6], t[7], Format<F>::pack(t[4], t[5], 0, false), true);
-  return r;
+  to_numbers<F>(t, v, s, inv);
+  return uint2{Format<F>::pack(t[2], t[3], Format<F>::pack(t[0], t[1], 0, false), true),
+               Format<F>::pack(t[6], t[7], Format<F>::pack(t[4], t[5], 0, false), true)};
 }
 
 // The largest of 16 lanes that share a DPP row.
-__device__ __forceinline__ uint32_t max16(uint32_t v) {
-  auto step = [](uint32_t a, float f) { return max(a, __float_as_uint(f)); };
-  v = step(v, dpp_f<0x128>(__uint_as_float(v)));
-  v = step(v, dpp_f<0x124>(__uint_as_float(v)));
-  v = step(v, dpp_f<0x122>(__uint_as_float(v)));
-  v = step(v, dpp_f<0x121>(__uint_as_float(v)));
-  return v;
+__device__ __forceinline__ float max16(float v) {
+  v = larger(v, dpp_f<0x128>(v));
+  v = larger(v, dpp_f<0x124>(v));
+  v = larger(v, dpp_f<0x122>(v));
+  return larger(v, dpp_f<0x121>(v));
 }
 
 constexpr int kChunk = 4;  // column blocks that a block of k_quant_rows takes from its 16 rows
@@ -126,80 +137,86 @@ __global__ void __launch_bounds__(256) k_quant_rows(Quant8 a) {
   for (int k = 0; k < kChunk; ++k) {
     const int64_t c = (k0 + k) * 128 + l * 8;
     float v[8], s, inv;
-    uint32_t m = 0;
+    float m = 0.f;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       v[e] = raw[k].get(e);
-      m = max(m, abs_bits(v[e]));
+      m = larger(m, v[e]);
     }
-    m = max16(m);
-    s = scale_of<F>(m, inv);
+    s = scale_of<F>(max16(m), inv);
     if (k0 + k >= cb) break;
     // 8 bytes: whole inside the row's zero padding to 16 bytes, or beyond it
-    if (c < ((a.cols + 15) & ~15LL)) *(uint2*)(a.q + r * a.ldq + c) = numbers8<F>(v, s, inv);
+    if (c < ((a.cols + 15) & ~15LL)) *(uint2*)(a.q + r * a.ldq + c) = numbers<F>(v, s, inv);
     if (l == 0) a.scale[(k0 + k) * a.rows + r] = s;
   }
 }
 
-constexpr int64_t kTileBlocks = 1024;  // of k_quant_tile, four a CU
-constexpr int kColLd = 132;  // bytes of a column in LDS: 16 lanes' 8-byte pieces in distinct banks
+// The largest of the four lanes l, l ^ 16, l ^ 32, l ^ 48.
+__device__ __forceinline__ float max_q(float f) {
+  const uint32_t v = __float_as_uint(f);
+  const auto a = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+  const uint32_t u = __float_as_uint(larger(__uint_as_float(a[0]), __uint_as_float(a[1])));
+  const auto b = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  return larger(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+
+constexpr int64_t kTileBlocks = 512;  // of k_quant_tile, two a CU
+constexpr int kColLd = 132;           // bytes of a column in LDS
 
 template <typename XT, int F>
-__global__ void __launch_bounds__(256) k_quant_tile(Quant8 a) {
+__global__ void __launch_bounds__(512) k_quant_tile(Quant8 a) {
   __shared__ __align__(16) uint8_t turned[128 * kColLd];
-  __shared__ uint32_t cmax[16][128];
-  __shared__ float csum[16][128];
-  __shared__ uint32_t wmax[2][4];  // in turn: a block of waves may be a tile ahead
-  const int l = threadIdx.x & 15, g = threadIdx.x >> 4;
+  __shared__ __align__(16) float cmax[8][128];
+  __shared__ __align__(16) float csum[8][128];
+  __shared__ float wmax[2][8];  // in turn: a wave may be a tile ahead
+  const int l = threadIdx.x & 15, g = threadIdx.x >> 4, w = threadIdx.x >> 6;
   const int64_t cbs = ceil_div(a.cols, 128), rbs = ceil_div(a.rows, 128);
   const int64_t cb = blockIdx.x % cbs, run = blockIdx.x / cbs;
   const int64_t up_cols = (a.cols + 15) & ~15LL, up_rows = (a.rows + 15) & ~15LL;
+  const int64_t c0 = cb * 128 + l * 8;
+  const int n = (int)min(max(a.cols - c0, (int64_t)0), (int64_t)8);
   const bool square = a.block_rows == 128, turn = a.qt != nullptr;
   float cs[8] = {};
   for (int64_t rb = run * a.per; rb < min((run + 1) * a.per, rbs); ++rb) {
-    // the lane's columns are opaque, or the addresses of all its rows are kept
-    // in registers from tile to tile
-    int lc = l * 8;
-    asm volatile("" : "+v"(lc));
-    const int64_t r0 = rb * 128 + g * 8, c0 = cb * 128 + lc;
-    const int n = (int)min(max(a.cols - c0, (int64_t)0), (int64_t)8);
-    Raw8<XT> raw[8];
+    const int64_t r0 = rb * 128 + g * 4;
+    Raw8<XT> raw[4];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < 4; ++i) {
       const int64_t r = min(r0 + i, a.rows - 1);
       raw[i] = load8((const XT*)a.x + r * a.ldx + c0, r0 + i < a.rows ? n : 0);
     }
-    uint32_t rmax[8], cm[8] = {};
-    uint32_t all = 0;
+    float rmax[4], cm[8] = {}, all = 0.f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      rmax[i] = 0;
+    for (int i = 0; i < 4; ++i) {
+      rmax[i] = 0.f;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const float f = raw[i].get(e);
-        const uint32_t m = abs_bits(f);
-        rmax[i] = max(rmax[i], m);
-        cm[e] = max(cm[e], m);
+        rmax[i] = larger(rmax[i], f);
+        cm[e] = larger(cm[e], f);
         cs[e] += f;
       }
-      all = max(all, rmax[i]);
+      all = larger(all, rmax[i]);
     }
     if (turn && !square) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) cmax[g][l * 8 + e] = cm[e];
+      for (int e = 0; e < 8; ++e) cm[e] = max_q(cm[e]);
+      if (g % 4 == 0) {
+        *(float4*)&cmax[w][l * 8] = float4{cm[0], cm[1], cm[2], cm[3]};
+        *(float4*)&cmax[w][l * 8 + 4] = float4{cm[4], cm[5], cm[6], cm[7]};
+      }
     }
     if (square) {
-      all = max16(all);
-      uint32_t w = 0;
-#pragma unroll
-      for (int j = 0; j < 64; j += 16) w = max(w, (uint32_t)__builtin_amdgcn_readlane((int)all, j));
-      if ((threadIdx.x & 63) == 0) wmax[rb & 1][threadIdx.x >> 6] = w;
+      all = max_q(max16(all));
+      if ((threadIdx.x & 63) == 0) wmax[rb & 1][w] = all;
     }
     __syncthreads();
     float s1 = 0.f, i1 = 0.f;
     if (square) {
-      const uint32_t* w = wmax[rb & 1];
-      s1 = scale_of<F>(max(max(w[0], w[1]), max(w[2], w[3])), i1);
+      float m = 0.f;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) m = larger(m, wmax[rb & 1][j]);
+      s1 = scale_of<F>(m, i1);
       if (threadIdx.x == 0) {
         if (a.q != nullptr) a.scale[cb * rbs + rb] = s1;
         if (turn) a.scale_t[rb * cbs + cb] = s1;
@@ -207,58 +224,65 @@ __global__ void __launch_bounds__(256) k_quant_tile(Quant8 a) {
     }
     if (a.q != nullptr) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
+      for (int i = 0; i < 4; ++i) {
         float v[8], s = s1, inv = i1;
         if (!square) s = scale_of<F>(max16(rmax[i]), inv);
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = raw[i].get(e);
-        __builtin_amdgcn_sched_barrier(0);  // one row at a time, for the registers
         if (r0 + i < a.rows) {
-          if (c0 < up_cols) *(uint2*)(a.q + (r0 + i) * a.ldq + c0) = numbers8<F>(v, s, inv);
+          if (c0 < up_cols) *(uint2*)(a.q + (r0 + i) * a.ldq + c0) = numbers<F>(v, s, inv);
           if (!square && l == 0) a.scale[cb * a.rows + r0 + i] = s;
         }
       }
     }
     if (turn) {
+      if (!square) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) cm[e] = 0.f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const float4 x = *(const float4*)&cmax[j][l * 8], y = *(const float4*)&cmax[j][l * 8 + 4];
+          const float m[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+#pragma unroll
+          for (int e = 0; e < 8; ++e) cm[e] = larger(cm[e], m[e]);
+        }
+      }
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        float v[8], s = s1, inv = i1;
+        float v[4], s = s1, inv = i1;
         if (!square) {
-          uint32_t m = 0;
-#pragma unroll
-          for (int j = 0; j < 16; ++j) m = max(m, cmax[j][l * 8 + e]);
-          s = scale_of<F>(m, inv);
-          if (g == 0 && c0 + e < a.cols) a.scale_t[rb * a.cols + c0 + e] = s;
+          s = scale_of<F>(cm[e], inv);
+          if (g == 0 && e < n) a.scale_t[rb * a.cols + c0 + e] = s;
         }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = raw[i].get(e);
-        const uint2 p = numbers8<F>(v, s, inv);
-        uint32_t* to = (uint32_t*)(turned + (l * 8 + e) * kColLd + g * 8);
-        to[0] = p.x;
-        to[1] = p.y;
-        __builtin_amdgcn_sched_barrier(0);
+        for (int i = 0; i < 4; ++i) v[i] = raw[i].get(e);
+        *(uint32_t*)(turned + (l * 8 + e) * kColLd + g * 4) = numbers<F>(v, s, inv);
       }
       __syncthreads();
-      const int64_t c = cb * 128 + (threadIdx.x >> 1);
+      // 32 bytes of a column a thread
+      const int64_t c = cb * 128 + (threadIdx.x >> 2), r = rb * 128 + (threadIdx.x & 3) * 32;
       if (c < a.cols) {
-        const uint32_t* from = (const uint32_t*)(turned + (threadIdx.x >> 1) * kColLd + (threadIdx.x & 1) * 64);
-        const int64_t r = rb * 128 + (threadIdx.x & 1) * 64;
+        const uint32_t* from = (const uint32_t*)(turned + (threadIdx.x >> 2) * kColLd + (threadIdx.x & 3) * 32);
         uint8_t* to = a.qt + c * a.ldqt + r;
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
+        for (int k = 0; k < 2; ++k)
           if (r + 16 * k < up_rows) *(uint4*)(to + 16 * k) = uint4{from[4 * k], from[4 * k + 1], from[4 * k + 2], from[4 * k + 3]};
       }
     }
   }
   if (a.colsum != nullptr) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) csum[g][l * 8 + e] = cs[e];
+    for (int e = 0; e < 8; ++e) cs[e] = sum_q(cs[e]);
+    if (g % 4 == 0) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) csum[w][l * 8 + e] = cs[e];
+    }
     __syncthreads();
     const int64_t c = cb * 128 + threadIdx.x;
     if (threadIdx.x < 128 && c < a.cols) {
       float t = 0.f;
 #pragma unroll
-      for (int j = 0; j < 16; ++j) t += csum[j][threadIdx.x];
+      for (int j = 0; j < 8; ++j) t += csum[j][threadIdx.x];
       a.part[run * a.cols + c] = t;
     }
   }
@@ -275,22 +299,22 @@ hipError_t launch_quant8(const Quant8& in, hipStream_t s) {
   // each leaving one row of partial sums
   a.per = a.colsum ? std::max<int64_t>(1, rbs * cbs / kTileBlocks) : 1;
   const int64_t runs = ceil_div(rbs, a.per);
-#define MGN_Q8(K, n)                                                                                 \
+#define MGN_Q8(K, n, threads)                                                                                 \
   do {                                                                                               \
     if (a.x_type == MGN_FP32 && a.format == MGN_E4M3)                                                \
-      hipLaunchKernelGGL((K<float, MGN_E4M3>), dim3((unsigned)(n)), dim3(256), 0, s, a);             \
+      hipLaunchKernelGGL((K<float, MGN_E4M3>), dim3((unsigned)(n)), dim3(threads), 0, s, a);             \
     else if (a.x_type == MGN_FP32)                                                                   \
-      hipLaunchKernelGGL((K<float, MGN_E5M2>), dim3((unsigned)(n)), dim3(256), 0, s, a);             \
+      hipLaunchKernelGGL((K<float, MGN_E5M2>), dim3((unsigned)(n)), dim3(threads), 0, s, a);             \
     else if (a.format == MGN_E4M3)                                                                   \
-      hipLaunchKernelGGL((K<bf16, MGN_E4M3>), dim3((unsigned)(n)), dim3(256), 0, s, a);              \
+      hipLaunchKernelGGL((K<bf16, MGN_E4M3>), dim3((unsigned)(n)), dim3(threads), 0, s, a);              \
     else                                                                                             \
-      hipLaunchKernelGGL((K<bf16, MGN_E5M2>), dim3((unsigned)(n)), dim3(256), 0, s, a);              \
+      hipLaunchKernelGGL((K<bf16, MGN_E5M2>), dim3((unsigned)(n)), dim3(threads), 0, s, a);              \
   } while (0)
   if (a.rows > 0) {
     if (!a.qt && !a.colsum && a.block_rows == 1)
-      MGN_Q8(k_quant_rows, ceil_div(a.rows, 16) * ceil_div(cbs, kChunk));
+      MGN_Q8(k_quant_rows, ceil_div(a.rows, 16) * ceil_div(cbs, kChunk), 256);
     else
-      MGN_Q8(k_quant_tile, runs * cbs);
+      MGN_Q8(k_quant_tile, runs * cbs, 512);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
