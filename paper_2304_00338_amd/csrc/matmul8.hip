@@ -453,10 +453,8 @@ __global__ void __launch_bounds__(512) k_matmul8_few(Job J) {
   const int64_t end = (p.a.cols + 15) & ~15LL;
   const int sha = p.a.block_rows == 128 ? 7 : 0, shb = p.b.block_rows == 128 ? 7 : 0;
   const int64_t Ra = ceil_div(p.a.rows, p.a.block_rows), Rb = ceil_div(p.b.rows, p.b.block_rows);
-  const uint8_t* rb = p.b.q + min(n0 + j, p.b.rows - 1) * p.b.ld + q * 32;
-  const uint8_t* ra[TM];
-  const float* psa[TM];
-  const float* psb[4];
+  const uint8_t *rb = p.b.q + min(n0 + j, p.b.rows - 1) * p.b.ld + q * 32, *ra[TM];
+  const float *psa[TM], *psb[4];
 #pragma unroll
   for (int i = 0; i < TM; ++i) {
     const int64_t m = min((int64_t)i * 16 + j, p.a.rows - 1);
@@ -466,24 +464,46 @@ __global__ void __launch_bounds__(512) k_matmul8_few(Job J) {
 #pragma unroll
   for (int r = 0; r < 4; ++r) psb[r] = p.b.scale + (min(n0 + 4 * q + r, p.b.rows - 1) >> shb);
   auto get = [&](const uint8_t* row, int64_t kb) {
-    const int64_t k = kb * 128;
+    const int64_t k = kb * 128, lim = end - q * 32;
     const uint8_t* z = (const uint8_t*)&zero16;
-    const uint4 lo = *(const uint4*)(k + q * 32 < end ? row + k : z);
-    const uint4 hi = *(const uint4*)(k + q * 32 + 16 < end ? row + k + 16 : z);
+    const uint4 lo = *(const uint4*)(k < lim ? row + k : z);
+    const uint4 hi = *(const uint4*)(k + 16 < lim ? row + k + 16 : z);
     return i32x8{(int)lo.x, (int)lo.y, (int)lo.z, (int)lo.w, (int)hi.x, (int)hi.y, (int)hi.z, (int)hi.w};
   };
-  f32x4 acc[TM] = {};
-  for (int64_t kb = kb0 + w; kb < kb1; kb += NWV) {
-    const i32x8 b = get(rb, kb);
-    float sb[4];
+  struct Step {
+    i32x8 a[TM], b;
+    float sa[TM], sb[4];
+  };
+  auto fetch = [&](Step& x, int64_t kb) {
+    x.b = get(rb, kb);
 #pragma unroll
-    for (int r = 0; r < 4; ++r) sb[r] = psb[r][kb * Rb];
+    for (int r = 0; r < 4; ++r) x.sb[r] = psb[r][kb * Rb];
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
-      const f32x4 part = mma16<WIDE, FB, FA>(b, get(ra[i], kb));
-      const float sa = psa[i][kb * Ra];
+      x.a[i] = get(ra[i], kb);
+      x.sa[i] = psa[i][kb * Ra];
+    }
+  };
+  f32x4 acc[TM] = {};
+  auto products = [&](const Step& x) {
 #pragma unroll
-      for (int r = 0; r < 4; ++r) acc[i][r] = __builtin_fmaf(part[r], sa * sb[r], acc[i][r]);
+    for (int i = 0; i < TM; ++i) {
+      const f32x4 part = mma16<WIDE, FB, FA>(x.b, x.a[i]);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) acc[i][r] = __builtin_fmaf(part[r], x.sa[i] * x.sb[r], acc[i][r]);
+    }
+  };
+  if (kb0 + w < kb1) {
+    Step x, y;
+    fetch(x, kb0 + w);
+    for (int64_t kb = kb0 + w; kb < kb1; kb += 2 * NWV) {
+      const bool more = kb + NWV < kb1;
+      if (more) fetch(y, kb + NWV);
+      products(x);
+      if (more) {
+        if (kb + 2 * NWV < kb1) fetch(x, kb + 2 * NWV);
+        products(y);
+      }
     }
   }
 #pragma unroll
@@ -504,7 +524,7 @@ using namespace dev;
 
 namespace {
 
-constexpr int64_t kFewRows = 64;
+constexpr int64_t kFewRows = 32;
 constexpr int64_t kCUs = 256;
 
 enum { kFew, kSmallTile, kBigTile };
@@ -522,7 +542,7 @@ Plan plan(int64_t m, int64_t n, int64_t k, bool big_ok) {
     r.kind = kFew;
     r.mt = 1;
     r.nt = ceil_div(n, 16);
-    want = std::min(2 * kCUs / std::max<int64_t>(r.nt, 1), kb / 16);
+    want = std::min(kCUs / std::max<int64_t>(r.nt, 1), kb / 16);
   } else {
     const int64_t big = ceil_div(m, 256) * ceil_div(n, 256);
     r.kind = big_ok && big >= kCUs * 3 / 4 ? kBigTile : kSmallTile;
@@ -545,10 +565,8 @@ void launch(const Job& J, const Plan& r, hipStream_t s) {
     const int64_t m = J.p.a.rows;
     if (m <= 16)
       hipLaunchKernelGGL((k_matmul8_few<WIDE, FA, FB, 1>), g, dim3(512), 0, s, J);
-    else if (m <= 32)
-      hipLaunchKernelGGL((k_matmul8_few<WIDE, FA, FB, 2>), g, dim3(512), 0, s, J);
     else
-      hipLaunchKernelGGL((k_matmul8_few<WIDE, FA, FB, 4>), g, dim3(512), 0, s, J);
+      hipLaunchKernelGGL((k_matmul8_few<WIDE, FA, FB, 2>), g, dim3(512), 0, s, J);
     return;
   }
   const bool brow = J.p.b.block_rows == 1;

@@ -9,7 +9,6 @@ raises, there is no fallback.
 from __future__ import annotations
 
 import collections
-import contextlib
 import ctypes as C
 import os
 
@@ -283,9 +282,15 @@ def patch_union(patches):
 
 
 # --------------------------------------------------------- device side
+_torch_module = None
+
+
 def _torch():
-    import torch
-    return torch
+    global _torch_module
+    if _torch_module is None:
+        import torch
+        _torch_module = torch
+    return _torch_module
 
 
 def _dptr(t, dtype=None, shape=None, name="tensor"):
@@ -536,57 +541,79 @@ def _row_type(t, name):
     torch = _torch()
     if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dim() != 2:
         raise MgnError(ERR_ARG, f"{name} must be a two-dimensional device tensor")
-    if t.dtype == torch.float32:
+    dt = t.dtype
+    if dt is torch.float32:
         return FP32
-    if t.dtype == torch.bfloat16:
+    if dt is torch.bfloat16:
         return BF16
-    raise MgnError(ERR_ARG, f"{name} must be float32 or bfloat16, got {t.dtype}")
+    raise MgnError(ERR_ARG, f"{name} must be float32 or bfloat16, got {dt}")
 
 
 def _row_ld(t, name, shape=None):
     """Leading dimension of a row tensor (its columns have to be adjacent)."""
-    if shape is not None and tuple(t.shape) != shape:
-        raise MgnError(ERR_ARG, f"{name} has shape {tuple(t.shape)}, expected {shape}")
     r, c = t.shape
-    if c > 1 and t.stride(1) != 1:
+    if shape is not None and (r, c) != shape:
+        raise MgnError(ERR_ARG, f"{name} has shape {(r, c)}, expected {shape}")
+    sr, sc = t.stride()
+    if c > 1 and sc != 1:
         raise MgnError(ERR_ARG, f"{name}: the columns of a row must be adjacent")
-    ld = t.stride(0) if r > 1 else c
-    if r > 1 and ld < c:
-        raise MgnError(ERR_ARG, f"{name}: rows overlap (stride {ld} for {c} columns)")
-    return max(ld, c)
+    if r <= 1:
+        return c
+    if sr < c:
+        raise MgnError(ERR_ARG, f"{name}: rows overlap (stride {sr} for {c} columns)")
+    return sr
 
 
 def _vector(t, name, n, device):
     torch = _torch()
     if t is None:
         return None
-    p = _dptr(t, torch.float32, name=name)
-    if t.numel() != n:
-        raise MgnError(ERR_ARG, f"{name} has {t.numel()} values, expected {n}")
-    if t.device != device:
-        raise MgnError(ERR_ARG, f"{name} is on {t.device}, expected {device}")
-    return p
+    if not isinstance(t, torch.Tensor) or t.dtype is not torch.float32 or t.device != device or t.numel() != n \
+            or not t.is_contiguous():
+        raise MgnError(ERR_ARG, f"{name} must be {n} contiguous float32 values on {device}")
+    return t.data_ptr()
 
 
-def _on(device, stream, *tensors):
-    """(context manager, stream pointer): the tensors' device made current,
-    and the tensors kept from reuse until a stream that is not the current one
-    has done its work."""
+_raw_stream = None  # device index -> the current stream's handle
+
+
+def _current_stream(device):
+    global _raw_stream
+    if _raw_stream is None:
+        torch = _torch()
+        # torch.cuda.current_stream builds an object: 1.9 us a call instead of 0.1
+        _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+            lambda i: torch.cuda.current_stream(i).cuda_stream)
+    return _raw_stream(device.index)
+
+
+def _run(device, stream, fn, args, tensors=()):
+    """fn(*args, stream) with the tensors' device current; with a stream that
+    is not the current one, the tensors are kept from reuse until it has done
+    its work."""
     torch = _torch()
-    guard = contextlib.nullcontext() if device.index == torch.cuda.current_device() else torch.cuda.device(device)
-    current = torch.cuda.current_stream(device)
-    if stream is None or stream == current:
-        return guard, current.cuda_stream
-    if stream.device != device:
-        raise MgnError(ERR_ARG, f"the stream is of {stream.device}, the tensors are on {device}")
-    for t in tensors:
-        if t is not None:
-            t.record_stream(stream)
-    return guard, stream.cuda_stream
+    if stream is None:
+        s = _current_stream(device)
+    else:
+        if stream.device != device:
+            raise MgnError(ERR_ARG, f"the stream is of {stream.device}, the tensors are on {device}")
+        s = stream.cuda_stream
+        if s != _current_stream(device):
+            for t in tensors:
+                if t is not None:
+                    t.record_stream(stream)
+    if device.index == torch.cuda.current_device():
+        rc = fn(*args, s)
+    else:
+        with torch.cuda.device(device):
+            rc = fn(*args, s)
+    if rc != OK:
+        _check(rc)
 
 
 def _scratch(nbytes, device):
-    return _torch().empty(nbytes, dtype=_torch().uint8, device=device) if nbytes else None
+    torch = _torch()
+    return torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
 
 
 def _at(t):
@@ -620,8 +647,12 @@ class Mat8:
         if not isinstance(scale, torch.Tensor) or scale.dtype != torch.float32 or tuple(scale.shape) != want \
                 or scale.device != q.device or not scale.is_contiguous():
             raise MgnError(ERR_ARG, f"scale must be a contiguous float32 tensor of shape {want} on {q.device}")
+        self._set(q, scale, rows, cols, ld, fmt, block_rows)
+
+    def _set(self, q, scale, rows, cols, ld, fmt, block_rows):
         self.q, self.scale, self.rows, self.cols, self.block_rows = q, scale, rows, cols, block_rows
         self.struct = CMat8(q.data_ptr(), scale.data_ptr(), rows, cols, ld, fmt, block_rows)
+        return self
 
 
 Quantised = collections.namedtuple("Quantised", "rows columns colsum")
@@ -635,19 +666,22 @@ def mgn_quant8(x, format="e4m3", block_rows=1, rowwise=True, transposed=False, c
     tensor with colsum=True, or the given one (added to with accumulate)."""
     torch = _torch()
     xt = _row_type(x, "x")
-    if format not in FORMATS:
+    fmt = FORMATS.get(format)
+    if fmt is None:
         raise MgnError(ERR_ARG, f"unknown 8-bit format {format!r}")
-    if block_rows not in (1, 128):
+    if block_rows != 1 and block_rows != 128:
         raise MgnError(ERR_ARG, f"blocks of {block_rows} rows (1 or 128)")
     r, c = x.shape
-    dev, f8 = x.device, torch.float8_e4m3fn if format == "e4m3" else torch.float8_e5m2
+    ldx = _row_ld(x, "x")
+    dev, f8 = x.device, torch.float8_e4m3fn if fmt == E4M3 else torch.float8_e5m2
     q = s = qt = st = sums = ws = None
+    rb, cb, ldq, ldqt, need = -(-r // 128), -(-c // 128), -(-c // 16) * 16, -(-r // 16) * 16, 0
     if rowwise:
-        q = torch.empty((r, -(-c // 16) * 16), dtype=f8, device=dev)
-        s = torch.empty((-(-c // 128), -(-r // block_rows)), dtype=torch.float32, device=dev)
+        q = torch.empty((r, ldq), dtype=f8, device=dev)
+        s = torch.empty((cb, r if block_rows == 1 else rb), dtype=torch.float32, device=dev)
     if transposed:
-        qt = torch.empty((c, -(-r // 16) * 16), dtype=f8, device=dev)
-        st = torch.empty((-(-r // 128), -(-c // block_rows)), dtype=torch.float32, device=dev)
+        qt = torch.empty((c, ldqt), dtype=f8, device=dev)
+        st = torch.empty((rb, c if block_rows == 1 else cb), dtype=torch.float32, device=dev)
     if isinstance(colsum, torch.Tensor):
         sums = colsum
         _vector(sums, "colsum", c, dev)
@@ -656,16 +690,14 @@ def mgn_quant8(x, format="e4m3", block_rows=1, rowwise=True, transposed=False, c
             raise MgnError(ERR_ARG, "accumulate needs the sums to add to")
         sums = torch.empty(c, dtype=torch.float32, device=dev)
     if sums is not None:
-        ws = _scratch(-(-r // 128) * c * 4, dev)
+        need = rb * c * 4
+        ws = _scratch(need, dev)
     if r > 0 and c > 0 or sums is not None:
-        guard, st_ptr = _on(dev, stream, x, q, s, qt, st, sums, ws)
-        with guard:
-            _check(lib().mgn_quant8(_at(x), xt, r, c, _row_ld(x, "x"), FORMATS[format], block_rows,
-                                    _at(q) or None, q.shape[1] if q is not None else 0, _at(s) if q is not None else None,
-                                    _at(qt), qt.shape[1] if qt is not None else 0, _at(st), _at(sums),
-                                    1 if accumulate else 0, _at(ws), ws.numel() if ws is not None else 0, st_ptr))
-    return Quantised(Mat8(q, s, c, block_rows) if rowwise else None,
-                     Mat8(qt, st, r, block_rows) if transposed else None, sums)
+        _run(dev, stream, lib().mgn_quant8,
+             (x.data_ptr(), xt, r, c, ldx, fmt, block_rows, _at(q) or None, ldq, _at(s) or None, _at(qt) or None, ldqt,
+              _at(st) or None, _at(sums), 1 if accumulate else 0, _at(ws), need), (x, q, s, qt, st, sums, ws))
+    return Quantised(Mat8.__new__(Mat8)._set(q, s, r, c, ldq, fmt, block_rows) if rowwise else None,
+                     Mat8.__new__(Mat8)._set(qt, st, c, r, ldqt, fmt, block_rows) if transposed else None, sums)
 
 
 def mgn_matmul8(a, b, bias=None, act="none", aux=None, out=None, dtype=None, accumulate=False, stream=None):
@@ -685,13 +717,22 @@ def mgn_matmul8(a, b, bias=None, act="none", aux=None, out=None, dtype=None, acc
     if out is None:
         if accumulate:
             raise MgnError(ERR_ARG, "accumulate needs an out to add to")
-        out = torch.empty((m, n), dtype=dtype or torch.float32, device=dev)
-    elif dtype is not None and out.dtype != dtype:
-        raise MgnError(ERR_ARG, f"out must be {dtype}, got {out.dtype}")
-    ct, ldc = _row_type(out, "out"), _row_ld(out, "out", (m, n))
-    if out.device != dev:
-        raise MgnError(ERR_ARG, f"out is on {out.device}, expected {dev}")
-    ep = Epilogue(bias=_vector(bias, "bias", n, dev), act=ACTS[act], accumulate=1 if accumulate else 0)
+        if dtype is None or dtype == torch.float32:
+            ct, out = FP32, torch.empty((m, n), dtype=torch.float32, device=dev)
+        elif dtype == torch.bfloat16:
+            ct, out = BF16, torch.empty((m, n), dtype=torch.bfloat16, device=dev)
+        else:
+            raise MgnError(ERR_ARG, f"out is float32 or bfloat16, not {dtype}")
+        ldc = n
+    else:
+        ct, ldc = _row_type(out, "out"), _row_ld(out, "out", (m, n))
+        if dtype is not None and out.dtype != dtype:
+            raise MgnError(ERR_ARG, f"out must be {dtype}, got {out.dtype}")
+        if out.device != dev:
+            raise MgnError(ERR_ARG, f"out is on {out.device}, expected {dev}")
+    ep = None
+    if bias is not None or act != "none" or accumulate:
+        ep = Epilogue(bias=_vector(bias, "bias", n, dev), act=ACTS[act], accumulate=1 if accumulate else 0)
     if act == "relu_grad":
         ep.aux_type, ep.ldaux = _row_type(aux, "aux"), _row_ld(aux, "aux", (m, n))
         if aux.device != dev:
@@ -701,13 +742,13 @@ def mgn_matmul8(a, b, bias=None, act="none", aux=None, out=None, dtype=None, acc
         raise MgnError(ERR_ARG, "aux is for relu_grad only")
     if m == 0 or n == 0:
         return out
+    L = lib()
     need = C.c_size_t()
-    _check(lib().mgn_matmul8_workspace(m, n, a.cols, C.byref(need)))
+    _check(L.mgn_matmul8_workspace(m, n, a.cols, C.byref(need)))
     ws = _scratch(need.value, dev)
-    guard, st_ptr = _on(dev, stream, a.q, a.scale, b.q, b.scale, bias, aux, out, ws)
-    with guard:
-        _check(lib().mgn_matmul8(C.byref(a.struct), C.byref(b.struct), C.byref(ep), ct, out.data_ptr(), ldc, _at(ws),
-                                 need.value, st_ptr))
+    _run(dev, stream, L.mgn_matmul8,
+         (C.byref(a.struct), C.byref(b.struct), None if ep is None else C.byref(ep), ct, out.data_ptr(), ldc, _at(ws),
+          need.value), (a.q, a.scale, b.q, b.scale, bias, aux, out, ws))
     return out
 
 
@@ -740,11 +781,17 @@ def _norm_gate(x, b, post, pre, post_gamma, post_beta, pre_gamma, pre_beta, gate
 def _as_rows(t, name, shape, dtype, device):
     if t is None:
         return Rows(None, 0)
-    if _row_type(t, name) is None or t.dtype != dtype:
+    _row_type(t, name)
+    if t.dtype != dtype:
         raise MgnError(ERR_ARG, f"{name} must be {dtype}, got {t.dtype}")
     if t.device != device:
         raise MgnError(ERR_ARG, f"{name} is on {t.device}, expected {device}")
     return Rows(t.data_ptr(), _row_ld(t, name, shape))
+
+
+def _new_rows(shape, dtype, device):
+    t = _torch().empty(shape, dtype=dtype, device=device)
+    return t, Rows(t.data_ptr(), shape[1])
 
 
 def mgn_norm_gate_forward(x, b, post="none", pre="none", post_gamma=None, post_beta=None, pre_gamma=None,
@@ -756,19 +803,17 @@ def mgn_norm_gate_forward(x, b, post="none", pre="none", post_gamma=None, post_b
     torch = _torch()
     op = _norm_gate(x, b, post, pre, post_gamma, post_beta, pre_gamma, pre_beta, gate, gate_ptr, skip, scale, eps)
     shape, dev = tuple(x.shape), x.device
-    if y is None:
-        y = torch.empty(shape, dtype=x.dtype, device=dev)
+    y, yr = _new_rows(shape, x.dtype, dev) if y is None else (y, _as_rows(y, "y", shape, x.dtype, dev))
     if pre == "none":
         if z is not None:
             raise MgnError(ERR_ARG, "z without a norm before the next block")
-    elif z is None:
-        z = torch.empty(shape, dtype=b.dtype, device=dev)
+        zr = Rows(None, 0)
+    else:
+        z, zr = _new_rows(shape, b.dtype, dev) if z is None else (z, _as_rows(z, "z", shape, b.dtype, dev))
     stats = torch.empty((shape[0], 4), dtype=torch.float32, device=dev) if save else None
-    xr, br = _as_rows(x, "x", shape, x.dtype, dev), _as_rows(b, "b", shape, b.dtype, dev)
-    yr, zr = _as_rows(y, "y", shape, x.dtype, dev), _as_rows(z, "z", shape, b.dtype, dev)
-    guard, st_ptr = _on(dev, stream, x, b, y, z, stats, gate, gate_ptr, post_gamma, post_beta, pre_gamma, pre_beta)
-    with guard:
-        _check(lib().mgn_norm_gate_forward(C.byref(op), xr, br, yr, zr, _at(stats), st_ptr))
+    xr, br = Rows(x.data_ptr(), _row_ld(x, "x")), Rows(b.data_ptr(), _row_ld(b, "b", shape))
+    _run(dev, stream, lib().mgn_norm_gate_forward, (C.byref(op), xr, br, yr, zr, _at(stats)),
+         (x, b, y, z, stats, gate, gate_ptr, post_gamma, post_beta, pre_gamma, pre_beta))
     return y, z, stats
 
 
@@ -786,8 +831,8 @@ def mgn_norm_gate_backward(x, b, stats, dy, dz, post="none", pre="none", post_ga
     op = _norm_gate(x, b, post, pre, post_gamma, post_beta, pre_gamma, pre_beta, gate, gate_ptr, skip, scale, eps)
     shape, dev = tuple(x.shape), x.device
     rows, cols = shape
-    dx = torch.empty(shape, dtype=x.dtype, device=dev) if dx is None else dx
-    db = torch.empty(shape, dtype=b.dtype, device=dev) if db is None else db
+    dx, dxr = _new_rows(shape, x.dtype, dev) if dx is None else (dx, _as_rows(dx, "dx", shape, x.dtype, dev))
+    db, dbr = _new_rows(shape, b.dtype, dev) if db is None else (db, _as_rows(db, "db", shape, b.dtype, dev))
     if not isinstance(stats, torch.Tensor) or tuple(stats.shape) != (rows, 4):
         raise MgnError(ERR_ARG, "stats must be the forward's, of shape (rows, 4)")
     _vector(stats, "stats", rows * 4, dev)
@@ -806,16 +851,14 @@ def mgn_norm_gate_backward(x, b, stats, dy, dz, post="none", pre="none", post_ga
         out[name] = g
     cg = CNormGateGrads(_at(out["dpost_gamma"]), _at(out["dpost_beta"]), _at(out["dpre_gamma"]), _at(out["dpre_beta"]),
                         _at(out["dgate"]), 0 if grads is None else 1)
-    rs = [_as_rows(t, n, shape, d.dtype, dev) for t, n, d in
-          ((x, "x", x), (b, "b", b), (dy, "dy", x), (dz, "dz", b), (dx, "dx", x), (db, "db", b))]
+    xr, br = Rows(x.data_ptr(), _row_ld(x, "x")), Rows(b.data_ptr(), _row_ld(b, "b", shape))
+    dyr, dzr = _as_rows(dy, "dy", shape, x.dtype, dev), _as_rows(dz, "dz", shape, b.dtype, dev)
     need = C.c_size_t()
     _check(lib().mgn_norm_gate_workspace(rows, cols, C.byref(need)))
     ws = _scratch(need.value, dev)
-    guard, st_ptr = _on(dev, stream, x, b, stats, dy, dz, dx, db, ws, gate, gate_ptr, post_gamma, post_beta, pre_gamma,
-                        pre_beta, *out.values())
-    with guard:
-        _check(lib().mgn_norm_gate_backward(C.byref(op), rs[0], rs[1], stats.data_ptr(), rs[2], rs[3], rs[4], rs[5],
-                                            C.byref(cg), _at(ws), need.value, st_ptr))
+    _run(dev, stream, lib().mgn_norm_gate_backward,
+         (C.byref(op), xr, br, stats.data_ptr(), dyr, dzr, dxr, dbr, C.byref(cg), _at(ws), need.value),
+         (x, b, stats, dy, dz, dx, db, ws, gate, gate_ptr, post_gamma, post_beta, pre_gamma, pre_beta, *out.values()))
     return NormGateGrads(dx, db, **out)
 
 
