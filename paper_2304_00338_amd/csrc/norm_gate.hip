@@ -170,7 +170,7 @@ __device__ __forceinline__ void gate_vectors(float (&ga)[NV][8], float (&gb)[NV]
 }
 
 template <typename XT, typename BT, int LPR, int NV, int MAXT>
-__global__ void __launch_bounds__(MAXT) k_norm_gate_fwd(NormGate a) {
+__global__ void __launch_bounds__(MAXT, LPR ? 5 : 1) k_norm_gate_fwd(NormGate a) {
   __shared__ float buf[64];
   const mgn_norm_gate& op = a.op;
   const Place<LPR, NV> at(op.rows, op.cols, a.per);
@@ -327,17 +327,27 @@ __global__ void __launch_bounds__(MAXT) k_norm_gate_bwd(NormGate a) {
     }
     if (!PRE) fetch(r);
     float x[NV][8], b[NV][8], t[NV][8], z[NV][8];
-    const float4 s = ns;
+    float4 s = ns;
+    if (LPR != 0 && !mine) {
+      // statistics and gradients 0: everything below is 0
+      s = float4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int k = 0; k < NV; ++k) {
+        ny[k] = Raw8<XT>{};
+        nz[k] = Raw8<BT>{};
+      }
+    }
 #pragma unroll
     for (int k = 0; k < NV; ++k)
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         x[k][e] = nx[k].get(e);
         b[k][e] = (nb[k].get(e) - s.x) * s.y;  // bhat (b itself without a norm: statistics 0 and 1)
-        t[k][e] = mine ? ny[k].get(e) : 0.f;
-        z[k][e] = mine ? nz[k].get(e) : 0.f;
+        t[k][e] = ny[k].get(e);
+        z[k][e] = nz[k].get(e);
       }
     if (PRE && i + 1 < a.per) fetch(r + 1);
+    if (LPR == 0 && !mine) continue;  // the whole block
     if (op.pre != MGN_NORM_NONE && a.dz.data != nullptr) {
       float s1 = 0.f, s2 = 0.f;
 #pragma unroll
@@ -345,7 +355,7 @@ __global__ void __launch_bounds__(MAXT) k_norm_gate_bwd(NormGate a) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           const float y = __builtin_fmaf(op.skip, x[k][e], __builtin_fmaf(b[k][e], ga[k][e], gb[k][e]));
-          x[k][e] = mine ? (y - s.z) * s.w : 0.f;  // yhat
+          x[k][e] = (y - s.z) * s.w;  // yhat
           dqb[k][e] += z[k][e];
           dqg[k][e] = __builtin_fmaf(z[k][e], x[k][e], dqg[k][e]);
           z[k][e] *= qg[k][e];
@@ -359,7 +369,7 @@ __global__ void __launch_bounds__(MAXT) k_norm_gate_bwd(NormGate a) {
       for (int k = 0; k < NV; ++k)
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-          t[k][e] = mine && e < at.n[k] ? __builtin_fmaf(s.w, z[k][e] - s1 - x[k][e] * s2, t[k][e]) : 0.f;
+          t[k][e] = __builtin_fmaf(s.w, z[k][e] - s1 - x[k][e] * s2, t[k][e]);
     }
     float s1 = 0.f, s2 = 0.f;
 #pragma unroll
@@ -368,10 +378,9 @@ __global__ void __launch_bounds__(MAXT) k_norm_gate_bwd(NormGate a) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         dx[e] = op.skip * t[k][e];
-        if (!mine) b[k][e] = 0.f;
         st[k][e] += t[k][e];
         sb[k][e] = __builtin_fmaf(t[k][e], b[k][e], sb[k][e]);
-        t[k][e] *= ga[k][e];  // gamma dp
+        t[k][e] *= ga[k][e];  // gamma dp; 0 beyond the row
         s1 += t[k][e];
         s2 = __builtin_fmaf(t[k][e], b[k][e], s2);
       }

@@ -13,7 +13,7 @@ template <>
 struct Raw8<float> {
   float v[8];
   __device__ __forceinline__ float get(int e) const { return v[e]; }
-  __device__ __forceinline__ void set(int e, float f) { v[e] = f; }
+  __device__ __forceinline__ void put(int e, float f) { v[e] = f; }
 };
 template <>
 struct Raw8<bf16> {
@@ -22,11 +22,25 @@ struct Raw8<bf16> {
     const uint32_t w = v[e >> 1];
     return __uint_as_float((e & 1) ? (w & 0xffff0000u) : (w << 16));
   }
-  __device__ __forceinline__ void set(int e, float f) {
-    const uint32_t h = (uint32_t)__builtin_bit_cast(uint16_t, (bf16)f);
-    v[e >> 1] = (e & 1) ? ((v[e >> 1] & 0xffffu) | (h << 16)) : ((v[e >> 1] & 0xffff0000u) | h);
-  }
+  __device__ __forceinline__ void put(int e, bf16 f) { v[e >> 1] |= (uint32_t)__builtin_bit_cast(uint16_t, f) << (16 * (e & 1)); }
 };
+
+__device__ __forceinline__ Raw8<float> raw8(const float (&f)[8], float) {
+  Raw8<float> r;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) r.v[e] = f[e];
+  return r;
+}
+// as vectors, for the instruction that rounds two at a time
+__device__ __forceinline__ Raw8<bf16> raw8(const float (&f)[8], bf16) {
+  typedef float f32x2 __attribute__((ext_vector_type(2)));
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  Raw8<bf16> r;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    r.v[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){f[2 * i], f[2 * i + 1]}, bf16x2));
+  return r;
+}
 
 // n: how many of the eight are inside the row (<= 0: none); the others are 0.
 template <typename T>
@@ -35,20 +49,18 @@ __device__ __forceinline__ Raw8<T> load8(const T* p, int n) {
   if (n >= 8) {
     __builtin_memcpy(&r, p, sizeof(r));
   } else {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) r.set(e, 0.f);
+    // bits, not values: a conversion here would be moved before the loads' wait
+    r = Raw8<T>{};
 #pragma unroll
     for (int e = 0; e < 7; ++e)
-      if (e < n) r.set(e, tof(p[e]));
+      if (e < n) r.put(e, p[e]);
   }
   return r;
 }
 template <typename T>
 __device__ __forceinline__ void store8(T* p, int n, const float (&f)[8]) {
   if (n >= 8) {
-    Raw8<T> r = {};
-#pragma unroll
-    for (int e = 0; e < 8; ++e) r.set(e, f[e]);
+    const Raw8<T> r = raw8(f, T());
     __builtin_memcpy(p, &r, sizeof(r));
   } else {
 #pragma unroll
