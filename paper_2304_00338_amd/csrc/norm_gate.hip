@@ -61,31 +61,52 @@ struct Reduce {
   }
 };
 
-// The walker's place: its lane, rows and columns.
+// The walker's place: its lane, rows and columns.  Runs of 8 columns start at
+// multiples of 8, but the last at cols - 8, so that every load is one of 16 or
+// 32 bytes inside the row; of that run a lane has the columns [lo, 8), of a run
+// behind the row none (lo 8), and what it has not counts as 0.  (With loads of
+// single elements for the last columns, each wait in their branch waited for the
+// next row's loads too: 16,384 x 5000 bf16 took 282 us in the reverse, 5120
+// columns 172.)  Rows of under 8 columns are one run [0, hi).
 template <int LPR, int NV>
 struct Place {
   int lane, lanes;
   int64_t walker, r0, r1;
-  int n[NV];  // columns of each run that are inside the row
+  int col[NV], lo[NV], hi;
+  bool tiny;
   __device__ __forceinline__ Place(int64_t rows, int cols, int64_t per) {
     lanes = LPR ? LPR : blockDim.x;
     lane = LPR ? threadIdx.x & (LPR - 1) : threadIdx.x;
     walker = LPR ? (int64_t)blockIdx.x * (blockDim.x / LPR) + threadIdx.x / LPR : blockIdx.x;
     r0 = min(walker * per, rows);
     r1 = min(r0 + per, rows);
+    tiny = cols < 8;
+    hi = min(cols, 8);
 #pragma unroll
-    for (int k = 0; k < NV; ++k) n[k] = cols - col(k);
+    for (int k = 0; k < NV; ++k) {
+      const int c = (k * lanes + lane) * 8;
+      col[k] = max(min(c, cols - 8), 0);
+      lo[k] = min(c - col[k], 8);
+    }
   }
-  __device__ __forceinline__ int col(int k) const { return (k * lanes + lane) * 8; }
+  __device__ __forceinline__ bool has(int k, int e) const { return e >= lo[k] && e < hi; }
+  template <typename T>
+  __device__ __forceinline__ Raw8<T> load(const mgn_rows& t, int64_t r, int k) const {
+    const T* p = (const T*)t.data + r * t.ld + col[k];
+    return load8(p, tiny ? hi : 8);
+  }
+  template <typename T>
+  __device__ __forceinline__ void store(const mgn_rows& t, int64_t r, int k, const float (&f)[8]) const {
+    store8((T*)t.data + r * t.ld + col[k], lo[k], hi, f);
+  }
 };
 
-template <int NV>
-__device__ __forceinline__ void load_vec(float (&v)[NV][8], const float* p, const int (&col)[NV], const int (&n)[NV],
-                                         float other) {
+template <int LPR, int NV>
+__device__ __forceinline__ void load_vec(float (&v)[NV][8], const float* p, const Place<LPR, NV>& at, float other) {
 #pragma unroll
   for (int k = 0; k < NV; ++k)
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[k][e] = p != nullptr ? (e < n[k] ? p[col[k] + e] : 0.f) : other;
+    for (int e = 0; e < 8; ++e) v[k][e] = p != nullptr ? (at.has(k, e) ? p[at.col[k] + e] : 0.f) : other;
 }
 
 // The gate group of a row: the largest g with ptr[g] <= r (0 if there is none).
@@ -103,7 +124,7 @@ __device__ __forceinline__ int64_t find_group(const int32_t* ptr, int64_t n, int
 
 // What a norm makes of a row: mean and 1 / sqrt(variance + eps).
 template <int LPR, int NV>
-__device__ __forceinline__ void statistics(const float (&v)[NV][8], const int (&n)[NV], int kind, float inv, float eps,
+__device__ __forceinline__ void statistics(const float (&v)[NV][8], const Place<LPR, NV>& at, int kind, float inv, float eps,
                                            Reduce<LPR>& red, float& mean, float& rstd) {
   mean = 0.f;
   if (kind == MGN_NORM_LAYER) {
@@ -119,7 +140,7 @@ __device__ __forceinline__ void statistics(const float (&v)[NV][8], const int (&
   for (int k = 0; k < NV; ++k)
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const float d = e < n[k] ? v[k][e] - mean : 0.f;
+      const float d = at.has(k, e) ? v[k][e] - mean : 0.f;
       q = __builtin_fmaf(d, d, q);
     }
   rstd = 1.f / __builtin_sqrtf(__builtin_fmaf(red.sum(q), inv, eps));
@@ -148,19 +169,19 @@ struct Gates {
 };
 
 // y = skip x + ga bhat + gb: ga = scale gate gamma, gb = scale gate beta.
-template <int NV>
+template <int LPR, int NV>
 __device__ __forceinline__ void gate_vectors(float (&ga)[NV][8], float (&gb)[NV][8], const NormGate& a, int64_t gate,
-                                             const int (&col)[NV], const int (&n)[NV]) {
+                                             const Place<LPR, NV>& at) {
   const mgn_norm_gate& op = a.op;
   const float* g = a.gmode == kGateNone ? nullptr : op.gate + gate * op.cols;
 #pragma unroll
   for (int k = 0; k < NV; ++k) {
     // opaque, or the addresses of all vectors are kept in registers from row to row
-    int c0 = col[k];
+    int c0 = at.col[k];
     asm volatile("" : "+v"(c0));
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const bool in = e < n[k];
+      const bool in = at.has(k, e);
       const int c = in ? c0 + e : 0;
       const float v = in ? op.scale * (g != nullptr ? g[c] : 1.f) : 0.f;
       ga[k][e] = v * (op.post_gamma != nullptr ? op.post_gamma[c] : 1.f);
@@ -170,20 +191,20 @@ __device__ __forceinline__ void gate_vectors(float (&ga)[NV][8], float (&gb)[NV]
 }
 
 template <typename XT, typename BT, int LPR, int NV, int MAXT>
-__global__ void __launch_bounds__(MAXT, LPR ? 5 : 1) k_norm_gate_fwd(NormGate a) {
+__global__ void __launch_bounds__(MAXT, LPR ? 4 : MAXT == 640 ? 5 : 1) k_norm_gate_fwd(NormGate a) {
   __shared__ float buf[64];
   const mgn_norm_gate& op = a.op;
   const Place<LPR, NV> at(op.rows, op.cols, a.per);
   Reduce<LPR> red{buf};
   const float inv = 1.f / (float)op.cols;
-  int col[NV];
-#pragma unroll
-  for (int k = 0; k < NV; ++k) col[k] = at.col(k);
   float ga[NV][8], gb[NV][8], qg[NV][8], qb[NV][8];
-  gate_vectors(ga, gb, a, 0, col, at.n);
-  load_vec(qg, op.pre_gamma, col, at.n, 1.f);
-  load_vec(qb, op.pre_beta, col, at.n, 0.f);
+  gate_vectors(ga, gb, a, 0, at);
+  load_vec(qg, op.pre_gamma, at, 1.f);
+  load_vec(qb, op.pre_beta, at, 0.f);
   const int64_t last = op.rows - 1;
+  // the last run's first columns are loaded by two lanes: where results replace
+  // inputs both have to be done before either stores, which a norm's sums see to
+  const bool plain = op.post == MGN_NORM_NONE && op.pre == MGN_NORM_NONE;
   Gates gates(a, at.r0);
   Raw8<XT> nx[NV];
   Raw8<BT> nb[NV];
@@ -191,8 +212,8 @@ __global__ void __launch_bounds__(MAXT, LPR ? 5 : 1) k_norm_gate_fwd(NormGate a)
     const int64_t rr = min(r, last);
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
-      nx[k] = load8((const XT*)a.x.data + rr * a.x.ld + col[k], at.n[k]);
-      nb[k] = load8((const BT*)a.b.data + rr * a.b.ld + col[k], at.n[k]);
+      nx[k] = at.template load<XT>(a.x, rr, k);
+      nb[k] = at.template load<BT>(a.b, rr, k);
     }
   };
   fetch(at.r0);
@@ -201,33 +222,39 @@ __global__ void __launch_bounds__(MAXT, LPR ? 5 : 1) k_norm_gate_fwd(NormGate a)
     const int64_t r = at.r0 + i;
     float x[NV][8], b[NV][8];
 #pragma unroll
-    for (int k = 0; k < NV; ++k)
+    for (int k = 0; k < NV; ++k) {
+      // (a branch around this, for rows that need none, took 226 us instead of
+      // 172 at 16,384 x 5120)
+      keep(nx[k], at.lo[k], at.hi);
+      keep(nb[k], at.lo[k], at.hi);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         x[k][e] = nx[k].get(e);
         b[k][e] = nb[k].get(e);
       }
+    }
+    if (LPR == 0 && plain) __syncthreads();
     if (i + 1 < a.per) fetch(r + 1);
     bool fresh = false;
     const bool mine = r < at.r1 && gates.at(a, r, fresh);
-    if (fresh) gate_vectors(ga, gb, a, gates.held, col, at.n);
+    if (fresh) gate_vectors(ga, gb, a, gates.held, at);
     float pm = 0.f, pr = 1.f, qm = 0.f, qr = 1.f;
-    if (op.post != MGN_NORM_NONE) statistics(b, at.n, op.post, inv, op.eps, red, pm, pr);
+    if (op.post != MGN_NORM_NONE) statistics(b, at, op.post, inv, op.eps, red, pm, pr);
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
       // beyond the row x, ga and gb are 0
 #pragma unroll
       for (int e = 0; e < 8; ++e)
         x[k][e] = __builtin_fmaf(op.skip, x[k][e], __builtin_fmaf((b[k][e] - pm) * pr, ga[k][e], gb[k][e]));
-      if (mine) store8((XT*)a.y.data + r * a.y.ld + col[k], at.n[k], x[k]);
+      if (mine) at.template store<XT>(a.y, r, k, x[k]);
     }
     if (op.pre != MGN_NORM_NONE) {
-      statistics(x, at.n, op.pre, inv, op.eps, red, qm, qr);
+      statistics(x, at, op.pre, inv, op.eps, red, qm, qr);
 #pragma unroll
       for (int k = 0; k < NV; ++k) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[k][e] = __builtin_fmaf((x[k][e] - qm) * qr, qg[k][e], qb[k][e]);
-        if (mine) store8((BT*)a.z.data + r * a.z.ld + col[k], at.n[k], x[k]);
+        if (mine) at.template store<BT>(a.z, r, k, x[k]);
       }
     }
     if (a.stats != nullptr && mine && at.lane == 0) ((float4*)a.stats)[r] = float4{pm, pr, qm, qr};
@@ -250,19 +277,20 @@ __global__ void __launch_bounds__(MAXT) k_norm_gate_bwd(NormGate a) {
   __shared__ float buf[64];
   extern __shared__ float sums[];  // LPR: [walkers of the block][cols]
   const mgn_norm_gate& op = a.op;
-  constexpr bool PRE = LPR == 0;  // the next row's loads under this one; else other walkers fill the wait
+  // the next row's loads under this one, where the registers hold them
+  constexpr bool PRE = LPR == 0 && NV == 1;
   const Place<LPR, NV> at(op.rows, op.cols, a.per);
   Reduce<LPR> red{buf};
   const float inv = 1.f / (float)op.cols;
-  int col[NV];
-#pragma unroll
-  for (int k = 0; k < NV; ++k) col[k] = at.col(k);
   float ga[NV][8], gb[NV][8], qg[NV][8];
-  gate_vectors(ga, gb, a, 0, col, at.n);
-  load_vec(qg, op.pre_gamma, col, at.n, 1.f);
+  gate_vectors(ga, gb, a, 0, at);
+  load_vec(qg, op.pre_gamma, at, 1.f);
   float st[NV][8] = {}, sb[NV][8] = {}, dqg[NV][8] = {}, dqb[NV][8] = {};
   float dpg[MANY ? NV : 1][8] = {}, dpb[MANY ? NV : 1][8] = {};
   const int64_t last = op.rows - 1;
+  // the last run's first columns are loaded by two lanes: where results replace
+  // inputs both have to be done before either stores, which a norm's sums see to
+  const bool plain = op.post == MGN_NORM_NONE && (op.pre == MGN_NORM_NONE || a.dz.data == nullptr);
   Gates gates(a, at.r0);
   auto vec = [&](const float* p, int c, float other) { return p != nullptr ? p[c] : other; };
   // The sums st and sb of a gate become those of the vectors.  dgate goes to
@@ -284,11 +312,11 @@ __global__ void __launch_bounds__(MAXT) k_norm_gate_bwd(NormGate a) {
     }
 #pragma unroll
     for (int k = 0; k < (MANY ? NV : 1); ++k) {
-      int c0 = col[k];
+      int c0 = at.col[k];
       asm volatile("" : "+v"(c0));  // as in gate_vectors
 #pragma unroll
       for (int e = 0; e < 8; ++e)
-        if (e < at.n[k]) {
+        if (at.has(k, e)) {
           const int c = c0 + e;
           const float v = op.scale * gate[c];
           const float d = op.scale * (vec(op.post_gamma, c, 1.f) * sb[k][e] + vec(op.post_beta, c, 0.f) * st[k][e]);
@@ -300,18 +328,18 @@ __global__ void __launch_bounds__(MAXT) k_norm_gate_bwd(NormGate a) {
         }
     }
   };
-  Raw8<XT> nx[NV], ny[NV];
-  Raw8<BT> nb[NV], nz[NV];
+  Raw8<XT> nx[NV], ny[NV] = {};
+  Raw8<BT> nb[NV], nz[NV] = {};
   float4 ns;
   auto fetch = [&](int64_t r) {
     const int64_t rr = min(r, last);
     ns = ((const float4*)a.stats)[rr];
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
-      nx[k] = load8((const XT*)a.x.data + rr * a.x.ld + col[k], at.n[k]);
-      nb[k] = load8((const BT*)a.b.data + rr * a.b.ld + col[k], at.n[k]);
-      ny[k] = load8((const XT*)a.dy.data + rr * a.dy.ld + col[k], a.dy.data ? at.n[k] : 0);
-      nz[k] = load8((const BT*)a.dz.data + rr * a.dz.ld + col[k], a.dz.data ? at.n[k] : 0);
+      nx[k] = at.template load<XT>(a.x, rr, k);
+      nb[k] = at.template load<BT>(a.b, rr, k);
+      if (a.dy.data != nullptr) ny[k] = at.template load<XT>(a.dy, rr, k);
+      if (a.dz.data != nullptr) nz[k] = at.template load<BT>(a.dz, rr, k);
     }
   };
   if (PRE) fetch(at.r0);
@@ -323,7 +351,7 @@ __global__ void __launch_bounds__(MAXT) k_norm_gate_bwd(NormGate a) {
     if (MANY && fresh) {
       if (open >= 0) settle(open);
       open = gates.held;
-      gate_vectors(ga, gb, a, open, col, at.n);
+      gate_vectors(ga, gb, a, open, at);
     }
     if (!PRE) fetch(r);
     float x[NV][8], b[NV][8], t[NV][8], z[NV][8];
@@ -338,7 +366,11 @@ __global__ void __launch_bounds__(MAXT) k_norm_gate_bwd(NormGate a) {
       }
     }
 #pragma unroll
-    for (int k = 0; k < NV; ++k)
+    for (int k = 0; k < NV; ++k) {
+      // bhat is not 0 beyond the lane's columns, but ga and the gradients are
+      keep(nx[k], at.lo[k], at.hi);
+      keep(ny[k], at.lo[k], at.hi);
+      keep(nz[k], at.lo[k], at.hi);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         x[k][e] = nx[k].get(e);
@@ -346,6 +378,8 @@ __global__ void __launch_bounds__(MAXT) k_norm_gate_bwd(NormGate a) {
         t[k][e] = ny[k].get(e);
         z[k][e] = nz[k].get(e);
       }
+    }
+    if (LPR == 0 && plain) __syncthreads();
     if (PRE && i + 1 < a.per) fetch(r + 1);
     if (LPR == 0 && !mine) continue;  // the whole block
     if (op.pre != MGN_NORM_NONE && a.dz.data != nullptr) {
@@ -384,7 +418,7 @@ __global__ void __launch_bounds__(MAXT) k_norm_gate_bwd(NormGate a) {
         s1 += t[k][e];
         s2 = __builtin_fmaf(t[k][e], b[k][e], s2);
       }
-      if (mine) store8((XT*)a.dx.data + r * a.dx.ld + col[k], at.n[k], dx);
+      if (mine) at.template store<XT>(a.dx, r, k, dx);
     }
     if (op.post != MGN_NORM_NONE) {
       red.sum2(s1, s2);
@@ -397,7 +431,7 @@ __global__ void __launch_bounds__(MAXT) k_norm_gate_bwd(NormGate a) {
     }
 #pragma unroll
     for (int k = 0; k < NV; ++k)
-      if (mine) store8((BT*)a.db.data + r * a.db.ld + col[k], at.n[k], t[k]);
+      if (mine) at.template store<BT>(a.db, r, k, t[k]);
   }
   if (MANY && open >= 0) settle(open);
   // the block's sums, one vector after the other
@@ -410,7 +444,7 @@ __global__ void __launch_bounds__(MAXT) k_norm_gate_bwd(NormGate a) {
       for (int k = 0; k < NV; ++k)
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-          if (e < at.n[k]) sums[w * op.cols + col[k] + e] = value(k, e, col[k] + e);
+          if (at.has(k, e)) sums[w * op.cols + at.col[k] + e] = value(k, e, at.col[k] + e);
       __syncthreads();
       for (int c = threadIdx.x; c < op.cols; c += blockDim.x) {
         float s = 0.f;
@@ -422,7 +456,7 @@ __global__ void __launch_bounds__(MAXT) k_norm_gate_bwd(NormGate a) {
       for (int k = 0; k < NV; ++k)
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-          if (e < at.n[k]) part[which * op.cols + col[k] + e] = value(k, e, col[k] + e);
+          if (at.has(k, e)) part[which * op.cols + at.col[k] + e] = value(k, e, at.col[k] + e);
     }
   };
   const float* one = a.gmode == kGateOne ? op.gate : nullptr;
@@ -509,15 +543,19 @@ using namespace dev;
 
 NormPlan norm_plan(int64_t rows, int cols, bool backward) {
   NormPlan p;
-  p.vpt = cols <= 8192 ? 8 : 16;
+  // in the reverse two runs a lane from 5121 columns on: blocks of more than 640
+  // threads have 128 registers, and with one run spilled (16,384 x 8192 bf16: 652
+  // us; two runs 305).  Above 8192 columns these are blocks of 1024 that do spill:
+  // 8192 x 16384 takes 1.75 ms.
+  p.vpt = cols <= (backward ? 5120 : 8192) ? 8 : 16;
   const int lanes = (cols + p.vpt - 1) / p.vpt;
   p.lpr = lanes <= 16 ? 16 : lanes <= 32 ? 32 : lanes <= 64 ? 64 : 0;
   p.threads = p.lpr ? 256 : (lanes + 63) / 64 * 64;
   const int per_block = p.lpr ? 256 / p.lpr : 1;
-  // as many blocks as run at a time on 256 CUs: by registers 20 waves of the
-  // forward fit a CU, 12 of the reverse (16 in blocks of 1024)
+  // as many blocks as run at a time on 256 CUs: by registers 16 waves of the
+  // forward fit a CU (20 in blocks of 640), 12 of the reverse (16 in blocks of 1024)
   const int waves = p.threads / 64;
-  const int64_t most = 256 * std::max(1, (backward ? 12 : 20) / waves) * per_block;
+  const int64_t most = 256 * std::max(1, (backward ? 12 : p.lpr ? 16 : 20) / waves) * per_block;
   p.per = std::max<int64_t>(1, ceil_div(rows, most));
   p.blocks = ceil_div(ceil_div(rows, p.per), per_block);
   p.walkers = p.blocks * per_block;
@@ -533,6 +571,8 @@ NormPlan norm_plan(int64_t rows, int cols, bool backward) {
       K(32, 1, 256);                     \
     else if (p.lpr == 64)                \
       K(64, 1, 256);                     \
+    else if (p.vpt == 16 && p.threads <= 512) \
+      K(0, 2, 512);                      \
     else if (p.vpt == 16)                \
       K(0, 2, 1024);                     \
     else if (p.threads <= 512)           \

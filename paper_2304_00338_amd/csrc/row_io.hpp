@@ -42,7 +42,8 @@ __device__ __forceinline__ Raw8<bf16> raw8(const float (&f)[8], bf16) {
   return r;
 }
 
-// n: how many of the eight are inside the row (<= 0: none); the others are 0.
+// The eight elements from p on, of which the first n are inside the row (<= 0:
+// none); the others are 0.
 template <typename T>
 __device__ __forceinline__ Raw8<T> load8(const T* p, int n) {
   Raw8<T> r;
@@ -57,16 +58,27 @@ __device__ __forceinline__ Raw8<T> load8(const T* p, int n) {
   }
   return r;
 }
+// Elements [lo, hi) of the eight.
 template <typename T>
-__device__ __forceinline__ void store8(T* p, int n, const float (&f)[8]) {
-  if (n >= 8) {
+__device__ __forceinline__ void store8(T* p, int lo, int hi, const float (&f)[8]) {
+  if (hi - lo == 8) {
     const Raw8<T> r = raw8(f, T());
     __builtin_memcpy(p, &r, sizeof(r));
   } else {
 #pragma unroll
-    for (int e = 0; e < 7; ++e)
-      if (e < n) p[e] = (T)f[e];
+    for (int e = 0; e < 8; ++e)
+      if (e >= lo && e < hi) p[e] = (T)f[e];
   }
+}
+// Elements outside of [lo, hi) become 0.
+__device__ __forceinline__ void keep(Raw8<float>& r, int lo, int hi) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) r.v[e] = e >= lo && e < hi ? r.v[e] : 0.f;
+}
+__device__ __forceinline__ void keep(Raw8<bf16>& r, int lo, int hi) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    r.v[i] &= (2 * i >= lo && 2 * i < hi ? 0xffffu : 0u) | (2 * i + 1 >= lo && 2 * i + 1 < hi ? 0xffff0000u : 0u);
 }
 
 }  // namespace dev
