@@ -430,7 +430,8 @@ typedef struct mgn_mat8 {
  * wanted).  colsum (nullable): [cols] sums of x over its rows (the gradient of
  * a bias), added to what is there with accumulate != 0.
  * The workspace is needed for colsum only (mgn_quant8_workspace).
- * Errors: ARG, SHAPE (2^31 rows or columns), WORKSPACE, DEVICE. */
+ * Errors: ARG, SHAPE (2^31 rows or columns, or rows x cols of 2^42), WORKSPACE,
+ * DEVICE. */
 int mgn_quant8_workspace(int64_t rows, int64_t cols, size_t* ws_bytes);
 int mgn_quant8(const void* x, int32_t x_type, int64_t rows, int64_t cols, int64_t ldx,
                int32_t format, int32_t block_rows, uint8_t* q, int64_t ldq, float* scale,
@@ -463,8 +464,8 @@ typedef struct mgn_epilogue {
  * transposes of dy and x, whose blocks run along the rows.  epilogue NULL: none.
  * cols 0 gives zero sums.  A workspace of mgn_matmul8_workspace bytes (which
  * may be 0) splits long sums over the device.
- * Errors: ARG, SHAPE (a->cols != b->cols, 2^31 rows or columns), WORKSPACE,
- * DEVICE. */
+ * Errors: ARG, SHAPE (a->cols != b->cols, 2^31 rows or columns, or c of 2^40
+ * elements), WORKSPACE, DEVICE. */
 int mgn_matmul8_workspace(int64_t a_rows, int64_t b_rows, int64_t cols, size_t* ws_bytes);
 int mgn_matmul8(const mgn_mat8* a, const mgn_mat8* b, const mgn_epilogue* epilogue,
                 int32_t c_type, void* c, int64_t ldc, void* workspace, size_t ws_bytes,

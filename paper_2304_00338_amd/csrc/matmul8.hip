@@ -178,24 +178,25 @@ __global__ void __launch_bounds__(WM * WN * 64, 2) k_matmul8_tile(Job J) {
   // XCD x (blocks go to the 8 XCDs in turn) takes an eighth of the tiles of all
   // splits, a split's tiles one after the other in groups of 8 rows of tiles, so
   // that the blocks it runs at a time share operands in its L2
-  const int64_t tiles = J.mt * J.nt, all = tiles * J.splits, chunk = ceil_div(all, 8);
-  const int64_t job = (int64_t)(blockIdx.x & 7) * chunk + (blockIdx.x >> 3);
+  const uint32_t nt = (uint32_t)J.nt, tiles = (uint32_t)J.mt * nt, all = tiles * J.splits, chunk = (all + 7) / 8;
+  const uint32_t job = (blockIdx.x & 7) * chunk + (blockIdx.x >> 3);
   if (job >= all) return;
-  const int split = (int)(job / tiles);
-  const int64_t t = job - split * tiles;
-  const int64_t group = t / (8 * J.nt), in = t - group * 8 * J.nt, gm = min(J.mt - group * 8, (int64_t)8);
-  const int64_t m0 = (group * 8 + in % gm) * BM, n0 = in / gm * BN;
+  const uint32_t split = job / tiles, t = job - split * tiles;
+  const uint32_t group = t / (8 * nt), in = t - group * 8 * nt, gm = min((uint32_t)J.mt - group * 8, 8u);
+  const uint32_t tn = in / gm;
+  const int64_t m0 = (int64_t)(group * 8 + in - tn * gm) * BM, n0 = (int64_t)tn * BN;
   const int64_t kb0 = split * J.per, kb1 = min(kb0 + J.per, J.kb);
   const int64_t end = (p.a.cols + 15) & ~15LL;
 
   // loads: of wave w the 8 rows from 8 (i NWV + w) on.  A wave's rows have a
-  // scalar base and 32-bit offsets (ld < 2^28).  At the matrices' ends a row that
-  // is not there is the last one again (its results are not stored), and what
-  // lies beyond the columns comes from the 16 zero bytes.  The offsets there are
-  // formed anew each time (opaque lane and wave): kept, they would spill.
+  // scalar base and 32-bit offsets.  At the matrices' ends, with an ld of 2^28 or
+  // more, and in a step that the columns end in, addresses are of 64 bits: a row
+  // that is not there is the last one again (its results are not stored), and
+  // what lies beyond the columns comes from the 16 zero bytes.  Those addresses
+  // are formed anew each time (opaque lane): kept, they would spill.
   const int lrow = l >> 3, lchunk = ((l & 7) ^ ((4 * (w & 1) + (l >> 4)) & 7)) * 16;
   const uint32_t ata = lrow * (uint32_t)p.a.ld + lchunk, atb = lrow * (uint32_t)p.b.ld + lchunk;
-  const bool inner = m0 + BM <= p.a.rows && n0 + BN <= p.b.rows;
+  const bool inner = m0 + BM <= p.a.rows && n0 + BN <= p.b.rows && max(p.a.ld, p.b.ld) < (1LL << 28);
   const uint8_t* const wa = p.a.q + (m0 + w * 8) * p.a.ld;
   const uint8_t* const wb = p.b.q + (n0 + w * 8) * p.b.ld;
   auto to_lds = [&](const uint8_t* src, uint8_t* buf, int i) {
@@ -524,7 +525,6 @@ using namespace dev;
 
 namespace {
 
-constexpr int64_t kFewRows = 32;
 constexpr int64_t kCUs = 256;
 
 enum { kFew, kSmallTile, kBigTile };
@@ -534,6 +534,21 @@ struct Plan {
   int splits;
 };
 
+// Which kernel, and into how many parts the sums are split; times in us of bf16
+// results (fp32 where marked).
+//  * Up to 32 rows of a the kernel for few rows, else tiles: 17 x 4096 x 4096 8.0
+//    (tiles 14.2), 32 x 1024 x 8192 9.3 (13.9), 24 x 10007 x 5000 19.0 (24.2), 32 x
+//    14336 x 4096 26.9 (24.6); 64 x 8192 x 8192 43.9 with four times 16 rows (27.9).
+//  * Tiles of 256 x 256 where they occupy three quarters of the CUs, need 8 steps
+//    or more and pad little; else of 128 x 128, two blocks a CU: 8192 x 4096 x 4096
+//    154 (small 167), 4096 x 3584 x 4096 72 (77), 16384 x 1000 x 5000 123 (158); but
+//    4096 x 2048 x 4096 66 (43), 100,000 x 512 x 512 75 (69), 434,558 x 128 x 384
+//    130 (76).  With a scale for each row of b, or for fp32 results, the large
+//    tiles spill.
+//  * Sums split so that two blocks a CU are busy: 128 x 256 x 852,640 to fp32 110
+//    (one block 119, four 121), 64 x 8192 x 8192 27.9 (35.7, 36.6).  For few rows one
+//    block of 8 waves a CU is enough: 1 x 4096 x 4096 6.9 whole, 10.2 in two parts.
+constexpr int64_t kFewRows = 32;
 Plan plan(int64_t m, int64_t n, int64_t k, bool big_ok) {
   Plan r;
   const int64_t kb = ceil_div(k, 128);
@@ -544,12 +559,12 @@ Plan plan(int64_t m, int64_t n, int64_t k, bool big_ok) {
     r.nt = ceil_div(n, 16);
     want = std::min(kCUs / std::max<int64_t>(r.nt, 1), kb / 16);
   } else {
-    const int64_t big = ceil_div(m, 256) * ceil_div(n, 256);
-    r.kind = big_ok && big >= kCUs * 3 / 4 ? kBigTile : kSmallTile;
-    const int64_t bm = r.kind == kBigTile ? 256 : 128;
-    r.mt = ceil_div(m, bm);
-    r.nt = ceil_div(n, bm);
-    want = r.kind == kBigTile ? 1 : std::min(2 * kCUs / (r.mt * r.nt), kb / 4);
+    const int64_t m2 = ceil_div(m, 256), n2 = ceil_div(n, 256), m1 = ceil_div(m, 128), n1 = ceil_div(n, 128);
+    const bool big = big_ok && m2 * n2 >= kCUs * 3 / 4 && kb >= 8 && 4 * m2 * n2 * 7 <= m1 * n1 * 8;
+    r.kind = big ? kBigTile : kSmallTile;
+    r.mt = big ? m2 : m1;
+    r.nt = big ? n2 : n1;
+    want = big ? 1 : std::min(2 * kCUs / (r.mt * r.nt), kb / 4);
   }
   r.splits = (int)std::max<int64_t>(want, 1);
   r.per = std::max<int64_t>(ceil_div(kb, r.splits), 1);
@@ -613,7 +628,7 @@ hipError_t launch_matmul8(const Matmul8& p, hipStream_t s) {
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || r.splits == 1) return e;
   const int64_t quads = p.a.rows * ceil_div(p.b.rows, 4);
-  if (r.splits >= 16)  // 256 splits of 128 x 256: 23 -> @ us
+  if (r.splits >= 16)  // 256 splits of 128 x 256: 8 us, with one thread 23
     hipLaunchKernelGGL((k_matmul8_join<16>), dim3((unsigned)ceil_div(quads, 16)), dim3(256), 0, s, J);
   else
     hipLaunchKernelGGL((k_matmul8_join<1>), dim3((unsigned)ceil_div(quads, 256)), dim3(256), 0, s, J);

@@ -124,8 +124,9 @@ constexpr int kChunk = 4;  // column blocks that a block of k_quant_rows takes f
 template <typename XT, int F>
 __global__ void __launch_bounds__(256) k_quant_rows(Quant8 a) {
   const int l = threadIdx.x & 15;
-  const int64_t cb = ceil_div(a.cols, 128), chunks = ceil_div(cb, (int64_t)kChunk);
-  const int64_t r = blockIdx.x / chunks * 16 + (threadIdx.x >> 4), k0 = blockIdx.x % chunks * kChunk;
+  const int64_t cb = ceil_div(a.cols, 128);
+  const uint32_t chunks = (uint32_t)ceil_div(cb, (int64_t)kChunk), group = blockIdx.x / chunks;
+  const int64_t r = (int64_t)group * 16 + (threadIdx.x >> 4), k0 = (int64_t)(blockIdx.x - group * chunks) * kChunk;
   if (r >= a.rows) return;  // all 16 lanes of the row
   Raw8<XT> raw[kChunk];
 #pragma unroll
@@ -171,13 +172,15 @@ __global__ void __launch_bounds__(512) k_quant_tile(Quant8 a) {
   __shared__ float wmax[2][8];  // in turn: a wave may be a tile ahead
   const int l = threadIdx.x & 15, g = threadIdx.x >> 4, w = threadIdx.x >> 6;
   const int64_t cbs = ceil_div(a.cols, 128), rbs = ceil_div(a.rows, 128);
-  const int64_t cb = blockIdx.x % cbs, run = blockIdx.x / cbs;
+  const uint32_t run = blockIdx.x / (uint32_t)cbs;
+  const int64_t cb = blockIdx.x - run * (uint32_t)cbs;
   const int64_t up_cols = (a.cols + 15) & ~15LL, up_rows = (a.rows + 15) & ~15LL;
   const int64_t c0 = cb * 128 + l * 8;
   const int n = (int)min(max(a.cols - c0, (int64_t)0), (int64_t)8);
   const bool square = a.block_rows == 128, turn = a.qt != nullptr;
   float cs[8] = {};
-  for (int64_t rb = run * a.per; rb < min((run + 1) * a.per, rbs); ++rb) {
+  const int64_t end = min((run + 1) * a.per, rbs);
+  for (int64_t rb = run * a.per; rb < end; ++rb) {
     const int64_t r0 = rb * 128 + g * 4;
     Raw8<XT> raw[4];
 #pragma unroll

@@ -112,6 +112,8 @@ int mgn_quant8(const void* x, int32_t x_type, int64_t rows, int64_t cols, int64_
     return fail(MGN_ERR_ARG, "%s: rows of qt have to start at multiples of 16 bytes", who);
   if (!aligned(scale, 4) || !aligned(scale_t, 4) || !aligned(colsum, 4))
     return fail(MGN_ERR_ARG, "%s: misaligned scales or sums", who);
+  if (ceil_div(rows, 16) * ceil_div(cols, 128) >= kMost)
+    return fail(MGN_ERR_SHAPE, "%s: x of %lld x %lld is too large for one call", who, (long long)rows, (long long)cols);
   if (colsum && need > 0 && (!ws || ws_bytes < need || !aligned(ws, 16)))
     return fail(MGN_ERR_WORKSPACE, "%s: workspace of %zu bytes, %zu needed", who, ws_bytes, need);
   if (!q && !qt && !colsum) return MGN_OK;
@@ -148,6 +150,9 @@ int mgn_matmul8(const mgn_mat8* a, const mgn_mat8* b, const mgn_epilogue* ep, in
       (!is_row_type(m.ep.aux_type) || !m.ep.aux || m.ep.ldaux < b->rows || !fits(a->rows, m.ep.ldaux) ||
        !aligned(m.ep.aux, elem(m.ep.aux_type))))
     return fail(MGN_ERR_ARG, "%s: null or misaligned aux, its type or leading dimension", who);
+  if (ceil_div(a->rows, 32) * ceil_div(b->rows, 16) >= kMost)
+    return fail(MGN_ERR_SHAPE, "%s: c of %lld x %lld is too large for one call", who, (long long)a->rows,
+                (long long)b->rows);
   const size_t need = matmul8_workspace(a->rows, b->rows, a->cols);
   if (need > 0 && (!ws || ws_bytes < need || !aligned(ws, 16)))
     return fail(MGN_ERR_WORKSPACE, "%s: workspace of %zu bytes, %zu needed", who, ws_bytes, need);

@@ -724,6 +724,30 @@ def test_far_offsets_of_numbers():
     assert torch.equal(mgn.mgn_matmul8(w, a), mgn.mgn_matmul8(w, m))
 
 
+def test_rows_far_apart():
+    """8-bit rows half a gigabyte apart: offsets within 8 rows pass 32 bits."""
+    ld, rows = 1 << 29, 40
+    base = torch.empty(rows * ld, dtype=torch.uint8, device="cuda").view(rows, ld)
+    m = mat8(rows, 1000)
+    far = base[:, :m.q.shape[1]]
+    far.copy_(m.q.view(torch.uint8))
+    a = mgn.Mat8(far.view(torch.float8_e4m3fn), m.scale, 1000)
+    w = mat8(300, 1000, block=128, seed=4)
+    for dtype in (torch.float32, torch.bfloat16):
+        assert torch.equal(mgn.mgn_matmul8(a, w, dtype=dtype), mgn.mgn_matmul8(m, w, dtype=dtype))
+        assert torch.equal(mgn.mgn_matmul8(w, a, dtype=dtype), mgn.mgn_matmul8(w, m, dtype=dtype))
+
+
+@pytest.mark.parametrize("m,n,k", [(4096, 3840, 1100), (4000, 3901, 1024), (16400, 1000, 5000)])
+def test_matmul8_large_tiles(m, n, k):
+    """Sizes that the tiles of 256 take, with edges in every dimension."""
+    for fa, bias, act in (("e4m3", True, "relu"), ("e5m2", False, "relu_grad")):
+        a, b = mat8(m, k, fa, 1, 1), mat8(n, k, "e4m3", 128, 2)
+        bv = randn(n, seed=3) * k ** 0.5 if bias else None
+        aux = randn(m, n, seed=4, dtype=torch.bfloat16) if act == "relu_grad" else None
+        check_product(mgn.mgn_matmul8(a, b, bias=bv, act=act, aux=aux, dtype=torch.bfloat16), a, b, bv, act, aux)
+
+
 def test_binding_refusals():
     x = randn(6, 40)
     q = mgn.mgn_quant8(x).rows

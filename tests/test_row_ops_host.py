@@ -27,6 +27,7 @@ def quant8(x=P, xt=0, rows=4, cols=130, ldx=130, fmt=mgn.E4M3, block=1, q=P, ldq
     (dict(fmt=1), mgn.ERR_ARG), (dict(block=2), mgn.ERR_ARG), (dict(block=64), mgn.ERR_ARG), (dict(s=NONE), mgn.ERR_ARG),
     (dict(q=NONE), mgn.ERR_ARG), (dict(st=NONE), mgn.ERR_ARG), (dict(ldq=143), mgn.ERR_ARG), (dict(ldq=128), mgn.ERR_ARG),
     (dict(ldq=136), mgn.ERR_ARG), (dict(q=P + 8), mgn.ERR_ARG), (dict(ldqt=0), mgn.ERR_ARG), (dict(qt=P + 4), mgn.ERR_ARG),
+    (dict(rows=1 << 30, cols=1 << 30, ldx=1 << 30, ldq=1 << 30, ldqt=1 << 30), mgn.ERR_SHAPE),
     (dict(cs=P), mgn.ERR_WORKSPACE), (dict(cs=P, ws=P, n=519), mgn.ERR_WORKSPACE),
     (dict(cs=P, ws=P + 4, n=520), mgn.ERR_WORKSPACE), (dict(cs=P + 2, ws=P, n=520), mgn.ERR_ARG),
 ])
@@ -61,6 +62,7 @@ def ep(bias=NONE, act=0, aux_type=0, aux=NONE, ldaux=0, acc=0):
     (dict(a=mat8(scale=P + 2)), mgn.ERR_ARG), (dict(a=mat8(ld=130)), mgn.ERR_ARG), (dict(a=mat8(ld=128)), mgn.ERR_ARG),
     (dict(a=mat8(fmt=0)), mgn.ERR_ARG), (dict(a=mat8(block=32)), mgn.ERR_ARG), (dict(a=mat8(rows=-1)), mgn.ERR_ARG),
     (dict(a=mat8(rows=1 << 31)), mgn.ERR_SHAPE), (dict(b=mat8(cols=131)), mgn.ERR_SHAPE),
+    (dict(a=mat8(rows=1 << 30), b=mat8(rows=1 << 30), ldc=1 << 30), mgn.ERR_SHAPE),
     (dict(b=mat8(q=NONE)), mgn.ERR_ARG), (dict(ct=2), mgn.ERR_ARG), (dict(c=NONE), mgn.ERR_ARG), (dict(ldc=4), mgn.ERR_ARG),
     (dict(c=P + 2), mgn.ERR_ARG), (dict(ep=ep(act=3)), mgn.ERR_ARG), (dict(ep=ep(act=-1)), mgn.ERR_ARG),
     (dict(ep=ep(bias=P + 2)), mgn.ERR_ARG), (dict(ep=ep(act=2)), mgn.ERR_ARG),
