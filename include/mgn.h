@@ -486,13 +486,13 @@ typedef struct mgn_norm_gate {
   int32_t post, pre; /* MGN_NORM_* (pre MGN_NORM_NONE: no z) */
   float eps;         /* > 0 */
   float skip, scale;
-  /* float32 [cols]; NULL: gamma 1, beta 0 */
+  /* float32 [cols]; NULL: gamma 1, beta 0; not used where the norm is NONE */
   const float *post_gamma, *post_beta, *pre_gamma, *pre_beta;
   /* gate: float32 [n_gates][cols].  n_gates 0: no gate (1); 1: one for all
    * rows; rows: one for each row; any number with gate_ptr (int32 device
    * [n_gates + 1], ascending): gate g for rows [gate_ptr[g], gate_ptr[g + 1]);
-   * rows outside of [gate_ptr[0], gate_ptr[n_gates]) are neither read nor
-   * written. */
+   * rows outside of [gate_ptr[0], gate_ptr[n_gates]) count for nothing, and
+   * their results are left as they were. */
   const float* gate;
   const int32_t* gate_ptr;
   int64_t n_gates;
@@ -512,7 +512,8 @@ int mgn_norm_gate_forward(const mgn_norm_gate* op, mgn_rows x, mgn_rows b, mgn_r
                           mgn_rows z, float* stats, void* stream);
 
 /* Gradients of the parameters, float32; each nullable; added to what is there
- * with accumulate != 0.  dgate is [n_gates][cols]. */
+ * with accumulate != 0.  dgate is [n_gates][cols].  Those of a norm that is NONE,
+ * and dgate without gates, are left as they were. */
 typedef struct mgn_norm_gate_grads {
   float *post_gamma, *post_beta, *pre_gamma, *pre_beta, *gate;
   int32_t accumulate;

@@ -202,9 +202,9 @@ __global__ void __launch_bounds__(MAXT, LPR ? 4 : MAXT == 640 ? 5 : 1) k_norm_ga
   load_vec(qg, op.pre_gamma, at, 1.f);
   load_vec(qb, op.pre_beta, at, 0.f);
   const int64_t last = op.rows - 1;
-  // the last run's first columns are loaded by two lanes: where results replace
-  // inputs both have to be done before either stores, which a norm's sums see to
-  const bool plain = op.post == MGN_NORM_NONE && op.pre == MGN_NORM_NONE;
+  // the last run's first columns are loaded by two lanes: where y replaces x both
+  // have to be done before either stores, which the sums of post see to
+  const bool plain = op.post == MGN_NORM_NONE;
   Gates gates(a, at.r0);
   Raw8<XT> nx[NV];
   Raw8<BT> nb[NV];
@@ -288,9 +288,9 @@ __global__ void __launch_bounds__(MAXT) k_norm_gate_bwd(NormGate a) {
   float st[NV][8] = {}, sb[NV][8] = {}, dqg[NV][8] = {}, dqb[NV][8] = {};
   float dpg[MANY ? NV : 1][8] = {}, dpb[MANY ? NV : 1][8] = {};
   const int64_t last = op.rows - 1;
-  // the last run's first columns are loaded by two lanes: where results replace
-  // inputs both have to be done before either stores, which a norm's sums see to
-  const bool plain = op.post == MGN_NORM_NONE && (op.pre == MGN_NORM_NONE || a.dz.data == nullptr);
+  // as in the forward: dx may replace what two lanes load; the sums of pre come
+  // before it is stored
+  const bool plain = op.pre == MGN_NORM_NONE || a.dz.data == nullptr;
   Gates gates(a, at.r0);
   auto vec = [&](const float* p, int c, float other) { return p != nullptr ? p[c] : other; };
   // The sums st and sb of a gate become those of the vectors.  dgate goes to

@@ -75,6 +75,9 @@ int check_norm_gate(const mgn_norm_gate* op, NormGate& a, const char* who) {
     return fail(MGN_ERR_ARG, "%s: %lld gates for %lld rows need gate_ptr", who, (long long)op->n_gates,
                 (long long)op->rows);
   a.op = *op;
+  // vectors of a norm that is not there
+  if (op->post == MGN_NORM_NONE) a.op.post_gamma = a.op.post_beta = nullptr;
+  if (op->pre == MGN_NORM_NONE) a.op.pre_gamma = a.op.pre_beta = nullptr;
   return MGN_OK;
 }
 
@@ -197,6 +200,9 @@ int mgn_norm_gate_backward(const mgn_norm_gate* op, mgn_rows x, mgn_rows b, cons
   int rc = check_norm_gate(op, a, who);
   if (rc != MGN_OK) return rc;
   if (grads) a.grads = *grads;
+  if (op->post == MGN_NORM_NONE) a.grads.post_gamma = a.grads.post_beta = nullptr;
+  if (op->pre == MGN_NORM_NONE) a.grads.pre_gamma = a.grads.pre_beta = nullptr;
+  if (op->n_gates == 0) a.grads.gate = nullptr;
   if (!aligned(a.grads.post_gamma, 4) || !aligned(a.grads.post_beta, 4) || !aligned(a.grads.pre_gamma, 4) ||
       !aligned(a.grads.pre_beta, 4) || !aligned(a.grads.gate, 4))
     return fail(MGN_ERR_ARG, "%s: misaligned parameter gradients", who);

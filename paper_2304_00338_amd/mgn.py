@@ -587,28 +587,36 @@ def _current_stream(device):
     return _raw_stream(device.index)
 
 
-def _run(device, stream, fn, args, tensors=()):
-    """fn(*args, stream) with the tensors' device current; with a stream that
-    is not the current one, the tensors are kept from reuse until it has done
-    its work."""
+def _run(device, fn, args):
+    """fn(*args, current stream) with the tensors' device current."""
     torch = _torch()
-    if stream is None:
-        s = _current_stream(device)
-    else:
-        if stream.device != device:
-            raise MgnError(ERR_ARG, f"the stream is of {stream.device}, the tensors are on {device}")
-        s = stream.cuda_stream
-        if s != _current_stream(device):
-            for t in tensors:
-                if t is not None:
-                    t.record_stream(stream)
     if device.index == torch.cuda.current_device():
-        rc = fn(*args, s)
+        rc = fn(*args, _current_stream(device))
     else:
         with torch.cuda.device(device):
-            rc = fn(*args, s)
+            rc = fn(*args, _current_stream(device))
     if rc != OK:
         _check(rc)
+
+
+def _elsewhere(fn, args):
+    """fn(**args) on args["stream"]: what it allocates belongs to that stream,
+    and the tensors it is given are kept from reuse until it is done with them."""
+    torch = _torch()
+    stream = args.pop("stream")
+    given = []
+    for v in args.values():
+        given += [v] if isinstance(v, torch.Tensor) else [v.q, v.scale] if isinstance(v, Mat8) else \
+            [t for t in v if isinstance(t, torch.Tensor)] if isinstance(v, tuple) else []
+    for t in given:
+        if t.is_cuda and t.device != stream.device:
+            raise MgnError(ERR_ARG, f"the stream is of {stream.device}, a tensor on {t.device}")
+    with torch.cuda.stream(stream):
+        out = fn(**args)
+    for t in given:
+        if t.is_cuda:
+            t.record_stream(stream)
+    return out
 
 
 def _scratch(nbytes, device):
@@ -664,6 +672,8 @@ def mgn_quant8(x, format="e4m3", block_rows=1, rowwise=True, transposed=False, c
     block_rows x 128 (see include/mgn.h).  Returns (rows, columns, colsum): x
     and its transpose as Mat8, or None, and the sums over x's rows: a new
     tensor with colsum=True, or the given one (added to with accumulate)."""
+    if stream is not None:
+        return _elsewhere(mgn_quant8, dict(locals()))
     torch = _torch()
     xt = _row_type(x, "x")
     fmt = FORMATS.get(format)
@@ -685,17 +695,17 @@ def mgn_quant8(x, format="e4m3", block_rows=1, rowwise=True, transposed=False, c
     if isinstance(colsum, torch.Tensor):
         sums = colsum
         _vector(sums, "colsum", c, dev)
+    elif accumulate:
+        raise MgnError(ERR_ARG, "accumulate needs the sums to add to")
     elif colsum:
-        if accumulate:
-            raise MgnError(ERR_ARG, "accumulate needs the sums to add to")
         sums = torch.empty(c, dtype=torch.float32, device=dev)
     if sums is not None:
         need = rb * c * 4
         ws = _scratch(need, dev)
     if r > 0 and c > 0 or sums is not None:
-        _run(dev, stream, lib().mgn_quant8,
+        _run(dev, lib().mgn_quant8,
              (x.data_ptr(), xt, r, c, ldx, fmt, block_rows, _at(q) or None, ldq, _at(s) or None, _at(qt) or None, ldqt,
-              _at(st) or None, _at(sums), 1 if accumulate else 0, _at(ws), need), (x, q, s, qt, st, sums, ws))
+              _at(st) or None, _at(sums), 1 if accumulate else 0, _at(ws), need))
     return Quantised(Mat8.__new__(Mat8)._set(q, s, r, c, ldq, fmt, block_rows) if rowwise else None,
                      Mat8.__new__(Mat8)._set(qt, st, c, r, ldqt, fmt, block_rows) if transposed else None, sums)
 
@@ -704,6 +714,8 @@ def mgn_matmul8(a, b, bias=None, act="none", aux=None, out=None, dtype=None, acc
     """act(a b^T + bias) of two Mat8 (see include/mgn.h): [a.rows][b.rows] in
     float32 or bfloat16 (dtype, default float32; out: written, or added to
     with accumulate)."""
+    if stream is not None:
+        return _elsewhere(mgn_matmul8, dict(locals()))
     torch = _torch()
     if not isinstance(a, Mat8) or not isinstance(b, Mat8):
         raise MgnError(ERR_ARG, "a and b must be Mat8")
@@ -746,9 +758,9 @@ def mgn_matmul8(a, b, bias=None, act="none", aux=None, out=None, dtype=None, acc
     need = C.c_size_t()
     _check(L.mgn_matmul8_workspace(m, n, a.cols, C.byref(need)))
     ws = _scratch(need.value, dev)
-    _run(dev, stream, L.mgn_matmul8,
+    _run(dev, L.mgn_matmul8,
          (C.byref(a.struct), C.byref(b.struct), None if ep is None else C.byref(ep), ct, out.data_ptr(), ldc, _at(ws),
-          need.value), (a.q, a.scale, b.q, b.scale, bias, aux, out, ws))
+          need.value))
     return out
 
 
@@ -800,6 +812,8 @@ def mgn_norm_gate_forward(x, b, post="none", pre="none", post_gamma=None, post_b
     """y = skip x + scale gate post(b), z = pre(y) (see include/mgn.h).
     Returns (y, z, stats): z None with pre="none", stats None without save.
     y may be x, z may be b."""
+    if stream is not None:
+        return _elsewhere(mgn_norm_gate_forward, dict(locals()))
     torch = _torch()
     op = _norm_gate(x, b, post, pre, post_gamma, post_beta, pre_gamma, pre_beta, gate, gate_ptr, skip, scale, eps)
     shape, dev = tuple(x.shape), x.device
@@ -812,8 +826,7 @@ def mgn_norm_gate_forward(x, b, post="none", pre="none", post_gamma=None, post_b
         z, zr = _new_rows(shape, b.dtype, dev) if z is None else (z, _as_rows(z, "z", shape, b.dtype, dev))
     stats = torch.empty((shape[0], 4), dtype=torch.float32, device=dev) if save else None
     xr, br = Rows(x.data_ptr(), _row_ld(x, "x")), Rows(b.data_ptr(), _row_ld(b, "b", shape))
-    _run(dev, stream, lib().mgn_norm_gate_forward, (C.byref(op), xr, br, yr, zr, _at(stats)),
-         (x, b, y, z, stats, gate, gate_ptr, post_gamma, post_beta, pre_gamma, pre_beta))
+    _run(dev, lib().mgn_norm_gate_forward, (C.byref(op), xr, br, yr, zr, _at(stats)))
     return y, z, stats
 
 
@@ -827,6 +840,8 @@ def mgn_norm_gate_backward(x, b, stats, dy, dz, post="none", pre="none", post_ga
     stats.  dy or dz None: zero.  Returns NormGateGrads; the gradients of the
     vectors and of the gate are those of the parameters that were given, new
     tensors, or those of grads (a NormGateGrads of an earlier call) added to."""
+    if stream is not None:
+        return _elsewhere(mgn_norm_gate_backward, dict(locals()))
     torch = _torch()
     op = _norm_gate(x, b, post, pre, post_gamma, post_beta, pre_gamma, pre_beta, gate, gate_ptr, skip, scale, eps)
     shape, dev = tuple(x.shape), x.device
@@ -856,9 +871,8 @@ def mgn_norm_gate_backward(x, b, stats, dy, dz, post="none", pre="none", post_ga
     need = C.c_size_t()
     _check(lib().mgn_norm_gate_workspace(rows, cols, C.byref(need)))
     ws = _scratch(need.value, dev)
-    _run(dev, stream, lib().mgn_norm_gate_backward,
-         (C.byref(op), xr, br, stats.data_ptr(), dyr, dzr, dxr, dbr, C.byref(cg), _at(ws), need.value),
-         (x, b, stats, dy, dz, dx, db, ws, gate, gate_ptr, post_gamma, post_beta, pre_gamma, pre_beta, *out.values()))
+    _run(dev, lib().mgn_norm_gate_backward,
+         (C.byref(op), xr, br, stats.data_ptr(), dyr, dzr, dxr, dbr, C.byref(cg), _at(ws), need.value))
     return NormGateGrads(dx, db, **out)
 
 

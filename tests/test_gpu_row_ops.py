@@ -507,6 +507,48 @@ def test_norm_gate_in_place():
         assert g2.dx is dy and torch.equal(dy, g.dx) and torch.equal(dz, g.db) and torch.equal(g2.dgate, g.dgate)
         mgn.mgn_norm_gate_forward(x, b, y=x, z=b, **kw)
         assert torch.equal(x, y) and torch.equal(b, z)
+    # odd widths: the last columns are read by two lanes
+    for cols in (131, 517, 1035, 4097, 6001, 8201):
+        for post, pre in (("none", "none"), ("none", "rms"), ("layer", "none"), ("rms", "layer")):
+            x, b = randn(600, cols, seed=1), randn(600, cols, seed=2)
+            dy = randn(600, cols, seed=3)
+            dz = randn(600, cols, seed=4) if pre != "none" else None
+            kw = dict(post=post, pre=pre, skip=0.5, scale=2.0)
+            y, z, st = mgn.mgn_norm_gate_forward(x, b, save=True, **kw)
+            g = mgn.mgn_norm_gate_backward(x, b, st, dy, dz, **kw)
+            h = mgn.mgn_norm_gate_backward(x, b, st, dy, None, **kw)
+            g2 = mgn.mgn_norm_gate_backward(x, b, st, dy.clone(), dz, dx=x.clone(), **kw)
+            assert torch.equal(g2.dx, g.dx)
+            x2, b2, dy2 = x.clone(), b.clone(), dy.clone()
+            h2 = mgn.mgn_norm_gate_backward(x2, b2, st, dy2, None, dx=dy2, db=b2, **kw)
+            assert h2.dx is dy2 and torch.equal(dy2, h.dx) and torch.equal(b2, h.db)
+            dz2 = dz.clone() if dz is not None else None
+            dy2 = dy.clone()
+            g3 = mgn.mgn_norm_gate_backward(x, b, st, dy2, dz2, dx=dy2, db=dz2, **kw)
+            assert torch.equal(dy2, g.dx) and torch.equal(g3.db, g.db)
+            mgn.mgn_norm_gate_forward(x, b, y=x, z=b if pre != "none" else None, **kw)
+            assert torch.equal(x, y) and (pre == "none" or torch.equal(b, z))
+
+
+def test_norm_gate_vectors_of_no_norm():
+    """Vectors of a norm that is not there change nothing and get no gradient."""
+    x, b, v = randn(30, 200, seed=1), randn(30, 200, seed=2), randn(200, seed=3)
+    y, z, st = mgn.mgn_norm_gate_forward(x, b, post_gamma=v, post_beta=v, pre_gamma=v, pre_beta=v, save=True)
+    assert z is None and torch.equal(y, x + b)
+    g = mgn.mgn_norm_gate_backward(x, b, st, x, None, post_gamma=v, post_beta=v, pre_gamma=v, pre_beta=v)
+    assert torch.equal(g.dx, x) and torch.equal(g.db, x) and g.dpost_gamma is None and g.dpre_beta is None
+    # and through the C ABI: the buffers stay as they were
+    op = mgn._norm_gate(x, b, "none", "none", v, v, v, v, None, None, 1.0, 1.0, 1e-5)
+    bufs = [dirty(200) for _ in range(5)]
+    cg = mgn.CNormGateGrads(*[t.data_ptr() for t in bufs], 0)
+    ws = torch.empty(1 << 22, dtype=torch.uint8, device="cuda")
+    R = lambda t: mgn.Rows(t.data_ptr(), 200)  # noqa: E731
+    dx, db = torch.empty_like(x), torch.empty_like(x)
+    import ctypes
+    assert mgn.lib().mgn_norm_gate_backward(ctypes.byref(op), R(x), R(b), st.data_ptr(), R(x), mgn.Rows(None, 0), R(dx), R(db),
+                                            ctypes.byref(cg), ws.data_ptr(), ws.numel(),
+                                            torch.cuda.current_stream().cuda_stream) == mgn.OK
+    assert torch.equal(dx, x) and all((t.view(torch.uint8) == 255).all() for t in bufs)
 
 
 def test_norm_gate_rows_apart():
@@ -683,9 +725,11 @@ def test_given_stream():
         q = mgn.mgn_quant8(x, stream=s).rows
         out = mgn.mgn_matmul8(q, w, stream=s)
         y, z, _ = mgn.mgn_norm_gate_forward(out, out, pre="rms", stream=s)
+        g = mgn.mgn_norm_gate_backward(out, out, None if z is None else mgn.mgn_norm_gate_forward(
+            out, out, pre="rms", save=True, stream=s)[2], out, z, pre="rms", stream=s)
         del q
         s.synchronize()
-        assert torch.equal(out, want) and torch.equal(y, want + want)
+        assert torch.equal(out, want) and torch.equal(y, want + want) and g.dx.isfinite().all()
 
 
 def test_far_offsets():
@@ -755,7 +799,7 @@ def test_binding_refusals():
     bad = [
         lambda: mgn.mgn_quant8(x, "e3m4"), lambda: mgn.mgn_quant8(x, block_rows=64), lambda: mgn.mgn_quant8(x.double()),
         lambda: mgn.mgn_quant8(x.t()), lambda: mgn.mgn_quant8(x[0]), lambda: mgn.mgn_quant8(x, colsum=randn(39)),
-        lambda: mgn.mgn_quant8(x, colsum=True, accumulate=True),
+        lambda: mgn.mgn_quant8(x, colsum=True, accumulate=True), lambda: mgn.mgn_quant8(x, accumulate=True),
         lambda: mgn.Mat8(f8, q.scale, 49), lambda: mgn.Mat8(f8[:, :40], q.scale, 40), lambda: mgn.Mat8(f8, q.scale[:, :3], 40),
         lambda: mgn.Mat8(x, q.scale, 40), lambda: mgn.Mat8(f8, q.scale, 40, 2), lambda: mgn.Mat8(f8[:, 8:], q.scale, 24) and
         mgn.mgn_matmul8(mgn.Mat8(f8[:, 8:], q.scale, 24), mgn.Mat8(f8[:, 8:], q.scale, 24)),
