@@ -12,7 +12,9 @@
  *     edge messages, Sec. 2.1), decoder; and its reverse mode;
  *   - one explicit integration step y' = y + sum_i b_i K_i with
  *     K_i = MGN(stage i), i.e. the update rule of Sec. 2.1 and the Heun forms
- *     of Sec. 2.3 / App. A (equation heun) generalised to a Butcher tableau.
+ *     of Sec. 2.3 / App. A (equation heun) generalised to a Butcher tableau;
+ *   - operators on rows for layers beside these: block-scaled 8-bit products and
+ *     the step norm, gate, residual, norm, with their gradients.
  *
  * Conventions
  *   - Every function returns an int status: MGN_OK (0) or a negative MGN_ERR_*.

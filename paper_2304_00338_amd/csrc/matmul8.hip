@@ -159,10 +159,16 @@ __global__ void __launch_bounds__(256) k_matmul8_join(Job J) {
 // that write LDS themselves (16 bytes a lane, 8 rows of 128 bytes a wave and
 // load), the next step's under the products of the current one, with one
 // barrier a step.  A row's 16-byte chunk c sits at place c ^ (row / 2 % 8), so
-// that 16 rows of a fragment read cover all 64 banks; the lanes'
-// source addresses are permuted to match.  What lies beyond the matrix comes
-// from 16 zero bytes.  The results go through the wave's own piece of LDS to be
+// that 16 rows of a fragment read cover all 64 banks; the lanes' source
+// addresses are permuted to match.  What lies beyond the matrix comes from 16
+// zero bytes.  The results go through the wave's own piece of LDS to be
 // stored as whole rows.
+//
+// Measured: 32,768 x 4096 x 4096 to bf16 563 us (1.95 PFLOP/s; the library's product
+// with one scale an operand reaches 2.5).  Without the loads 0.09 ms less, without
+// the scaled additions 0.05: a step's loads take longer than its 64 products a
+// SIMD, and the eight waves wait at its barrier.  434,558 x 128 x 384 to fp32 110 us
+// (3.6 TB/s), weight gradient 128 x 256 x 852,640 80 us (4.1 TB/s) and 8 to join.
 template <bool WIDE, int FA, int FB, bool BROW, int WM, int WN, int TM, int TN>
 __global__ void __launch_bounds__(WM * WN * 64, 2) k_matmul8_tile(Job J) {
   constexpr int BM = WM * TM * 32, BN = WN * TN * 32, NWV = WM * WN;
@@ -422,13 +428,17 @@ __global__ void __launch_bounds__(WM * WN * 64, 2) k_matmul8_tile(Job J) {
   }
 }
 
-// ---- few rows of a (up to TM times 16): the weights' bytes.
+// ---- few rows of a (up to TM times 16), bound by the weights' bytes.
 //
 // A block takes 16 rows of b, its 8 waves the steps of 128 columns in turn;
 // operands come straight from memory, 32 consecutive bytes a lane (four lanes
-// cover a row's 128), some steps ahead, and the waves' sums meet in LDS.  The
+// cover a row's 128), a step ahead, and the waves' sums meet in LDS.  The
 // instruction is 16x16x128: lane l holds row l & 15, bytes [32 (l >> 4), + 32);
 // result r is row 4 (l >> 4) + r of b, column l & 15 a row of a.
+//
+// Measured in a graph, weights from memory: 1 x 4096 x 4096 7.0 us, 1 x 4096 x 14336
+// 15.4 (3.8 TB/s), 23 x 10007 x 5000 25 (2.0 TB/s: every block reads a through L1,
+// twice the weights' bytes).
 template <bool WIDE, int FB, int FA>
 __device__ __forceinline__ f32x4 mma16(i32x8 b, i32x8 a) {
   f32x4 c = {0.f, 0.f, 0.f, 0.f};
