@@ -466,8 +466,8 @@ typedef struct mgn_epilogue {
  * transposes of dy and x, whose blocks run along the rows.  epilogue NULL: none.
  * cols 0 gives zero sums.  A workspace of mgn_matmul8_workspace bytes (which
  * may be 0) splits long sums over the device.
- * Errors: ARG, SHAPE (a->cols != b->cols, 2^31 rows or columns, or c of 2^40
- * elements), WORKSPACE, DEVICE. */
+ * Errors: ARG, SHAPE (a->cols != b->cols, 2^31 rows or columns, or c of about 2^24
+ * tiles of 128 x 128), WORKSPACE, DEVICE. */
 int mgn_matmul8_workspace(int64_t a_rows, int64_t b_rows, int64_t cols, size_t* ws_bytes);
 int mgn_matmul8(const mgn_mat8* a, const mgn_mat8* b, const mgn_epilogue* epilogue,
                 int32_t c_type, void* c, int64_t ldc, void* workspace, size_t ws_bytes,

@@ -458,8 +458,8 @@ __global__ void __launch_bounds__(512) k_matmul8_few(Job J) {
   __shared__ f32x4 sums[NWV][TM][64];
   const Matmul8& p = J.p;
   const int l = threadIdx.x & 63, w = threadIdx.x >> 6, j = l & 15, q = l >> 4;
-  const int64_t n0 = (int64_t)blockIdx.x * 16;
-  const int split = blockIdx.y;
+  const int64_t n0 = (blockIdx.y * kGridRow + blockIdx.x) * 16;
+  const int split = blockIdx.z;
   const int64_t kb0 = split * J.per, kb1 = min(kb0 + J.per, J.kb);
   const int64_t end = (p.a.cols + 15) & ~15LL;
   const int sha = p.a.block_rows == 128 ? 7 : 0, shb = p.b.block_rows == 128 ? 7 : 0;
@@ -586,7 +586,8 @@ template <bool WIDE, int FA, int FB>
 void launch(const Job& J, const Plan& r, hipStream_t s) {
   const dim3 grid((unsigned)(8 * ceil_div(r.mt * r.nt * r.splits, 8)));
   if (r.kind == kFew) {
-    const dim3 g((unsigned)r.nt, (unsigned)r.splits);
+    dim3 g = grid_of(r.nt);
+    g.z = (unsigned)r.splits;
     const int64_t m = J.p.a.rows;
     if (m <= 16)
       hipLaunchKernelGGL((k_matmul8_few<WIDE, FA, FB, 1>), g, dim3(512), 0, s, J);

@@ -512,10 +512,10 @@ struct ColumnSums {
   int32_t accumulate;
 };
 __global__ void __launch_bounds__(1024) k_column_sums(ColumnSums a) {
-  const int64_t col = (int64_t)blockIdx.x * kSumCols + threadIdx.x % kSumCols;
-  float* out = a.out[blockIdx.y];
+  const int64_t col = (blockIdx.y * kGridRow + blockIdx.x) * kSumCols + threadIdx.x % kSumCols;
+  float* out = a.out[blockIdx.z];
   if (out == nullptr) return;  // the whole block
-  const float* p = a.part + blockIdx.y * a.cols + col;
+  const float* p = a.part + blockIdx.z * a.cols + col;
   const float v = column_sum(a.nb, col < a.cols, [&](int64_t b) { return p[b * a.stride]; });
   if (threadIdx.x < kSumCols && col < a.cols) out[col] = a.accumulate ? out[col] + v : v;
 }
@@ -524,8 +524,10 @@ __global__ void __launch_bounds__(1024) k_column_sums(ColumnSums a) {
 // without rows.
 __global__ void __launch_bounds__(1024) k_gate_slots(NormGate a) {
   const mgn_norm_gate& op = a.op;
-  const int col = blockIdx.y * kSumCols + threadIdx.x % kSumCols;
-  const int64_t g = blockIdx.x, b0 = op.gate_ptr[g], b1 = op.gate_ptr[g + 1];
+  const int col = blockIdx.z * kSumCols + threadIdx.x % kSumCols;
+  const int64_t g = blockIdx.y * kGridRow + blockIdx.x;
+  if (g >= op.n_gates) return;
+  const int64_t b0 = op.gate_ptr[g], b1 = op.gate_ptr[g + 1];
   const int64_t p0 = max(b0, (int64_t)0), p1 = min(b1, op.rows);
   const bool none = p1 <= p0;
   const int64_t w0 = none ? 0 : p0 / a.per, w1 = none ? -1 : (p1 - 1) / a.per;
@@ -643,12 +645,16 @@ hipError_t launch_norm_gate_backward(const NormGate& in, hipStream_t s) {
                           {a.grads.post_gamma, a.grads.post_beta, a.grads.pre_gamma, a.grads.pre_beta,
                            one ? a.grads.gate : nullptr},
                           a.grads.accumulate};
-    hipLaunchKernelGGL(k_column_sums, dim3((a.op.cols + kSumCols - 1) / kSumCols, 5), dim3(1024), 0, s, c);
+    dim3 g = grid_of(ceil_div(a.op.cols, kSumCols));
+    g.z = 5;
+    hipLaunchKernelGGL(k_column_sums, g, dim3(1024), 0, s, c);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
   if (a.gmode == kGateGroup && a.grads.gate) {
-    hipLaunchKernelGGL(k_gate_slots, dim3((unsigned)a.op.n_gates, (a.op.cols + kSumCols - 1) / kSumCols), dim3(1024), 0, s, a);
+    dim3 g = grid_of(a.op.n_gates);
+    g.z = (unsigned)ceil_div(a.op.cols, kSumCols);
+    hipLaunchKernelGGL(k_gate_slots, g, dim3(1024), 0, s, a);
     return hipGetLastError();
   }
   return hipSuccess;
@@ -657,7 +663,7 @@ hipError_t launch_norm_gate_backward(const NormGate& in, hipStream_t s) {
 hipError_t launch_column_reduce(const float* part, int64_t nb, int64_t stride, int64_t cols, float* out,
                                 int32_t accumulate, hipStream_t s) {
   const ColumnSums c = {part, nb, stride, cols, {out, nullptr, nullptr, nullptr, nullptr}, accumulate};
-  hipLaunchKernelGGL(k_column_sums, dim3((unsigned)ceil_div(cols, kSumCols), 1), dim3(1024), 0, s, c);
+  hipLaunchKernelGGL(k_column_sums, grid_of(ceil_div(cols, kSumCols)), dim3(1024), 0, s, c);
   return hipGetLastError();
 }
 

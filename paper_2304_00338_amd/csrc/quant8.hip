@@ -130,8 +130,9 @@ template <typename XT, int F>
 __global__ void __launch_bounds__(256) k_quant_rows(Quant8 a) {
   const int l = threadIdx.x & 15;
   const int64_t cb = ceil_div(a.cols, 128);
-  const uint32_t chunks = (uint32_t)ceil_div(cb, (int64_t)kChunk), group = blockIdx.x / chunks;
-  const int64_t r = (int64_t)group * 16 + (threadIdx.x >> 4), k0 = (int64_t)(blockIdx.x - group * chunks) * kChunk;
+  const uint32_t chunks = (uint32_t)ceil_div(cb, (int64_t)kChunk), block = blockIdx.y * (uint32_t)kGridRow + blockIdx.x,
+                 group = block / chunks;
+  const int64_t r = (int64_t)group * 16 + (threadIdx.x >> 4), k0 = (int64_t)(block - group * chunks) * kChunk;
   if (r >= a.rows) return;  // all 16 lanes of the row
   Raw8<XT> raw[kChunk];
 #pragma unroll
@@ -177,8 +178,9 @@ __global__ void __launch_bounds__(512) k_quant_tile(Quant8 a) {
   __shared__ float wmax[2][8];  // in turn: a wave may be a tile ahead
   const int l = threadIdx.x & 15, g = threadIdx.x >> 4, w = threadIdx.x >> 6;
   const int64_t cbs = ceil_div(a.cols, 128), rbs = ceil_div(a.rows, 128);
-  const uint32_t run = blockIdx.x / (uint32_t)cbs;
-  const int64_t cb = blockIdx.x - run * (uint32_t)cbs;
+  const uint32_t block = blockIdx.y * (uint32_t)kGridRow + blockIdx.x, run = block / (uint32_t)cbs;
+  const int64_t cb = block - run * (uint32_t)cbs;
+  if (run * a.per >= rbs) return;  // behind the last block
   const int64_t up_cols = (a.cols + 15) & ~15LL, up_rows = (a.rows + 15) & ~15LL;
   const int64_t c0 = cb * 128 + l * 8;
   const int n = (int)min(max(a.cols - c0, (int64_t)0), (int64_t)8);
@@ -307,16 +309,16 @@ hipError_t launch_quant8(const Quant8& in, hipStream_t s) {
   // each leaving one row of partial sums
   a.per = a.colsum ? std::max<int64_t>(1, rbs * cbs / kTileBlocks) : 1;
   const int64_t runs = ceil_div(rbs, a.per);
-#define MGN_Q8(K, n, threads)                                                                                 \
-  do {                                                                                               \
-    if (a.x_type == MGN_FP32 && a.format == MGN_E4M3)                                                \
-      hipLaunchKernelGGL((K<float, MGN_E4M3>), dim3((unsigned)(n)), dim3(threads), 0, s, a);             \
-    else if (a.x_type == MGN_FP32)                                                                   \
-      hipLaunchKernelGGL((K<float, MGN_E5M2>), dim3((unsigned)(n)), dim3(threads), 0, s, a);             \
-    else if (a.format == MGN_E4M3)                                                                   \
-      hipLaunchKernelGGL((K<bf16, MGN_E4M3>), dim3((unsigned)(n)), dim3(threads), 0, s, a);              \
-    else                                                                                             \
-      hipLaunchKernelGGL((K<bf16, MGN_E5M2>), dim3((unsigned)(n)), dim3(threads), 0, s, a);              \
+#define MGN_Q8(K, n, threads)                                                                      \
+  do {                                                                                             \
+    if (a.x_type == MGN_FP32 && a.format == MGN_E4M3)                                              \
+      hipLaunchKernelGGL((K<float, MGN_E4M3>), grid_of(n), dim3(threads), 0, s, a);                \
+    else if (a.x_type == MGN_FP32)                                                                 \
+      hipLaunchKernelGGL((K<float, MGN_E5M2>), grid_of(n), dim3(threads), 0, s, a);                \
+    else if (a.format == MGN_E4M3)                                                                 \
+      hipLaunchKernelGGL((K<bf16, MGN_E4M3>), grid_of(n), dim3(threads), 0, s, a);                 \
+    else                                                                                           \
+      hipLaunchKernelGGL((K<bf16, MGN_E5M2>), grid_of(n), dim3(threads), 0, s, a);                 \
   } while (0)
   if (a.rows > 0) {
     if (!a.qt && !a.colsum && a.block_rows == 1)

@@ -153,7 +153,7 @@ int mgn_matmul8(const mgn_mat8* a, const mgn_mat8* b, const mgn_epilogue* ep, in
       (!is_row_type(m.ep.aux_type) || !m.ep.aux || m.ep.ldaux < b->rows || !fits(a->rows, m.ep.ldaux) ||
        !aligned(m.ep.aux, elem(m.ep.aux_type))))
     return fail(MGN_ERR_ARG, "%s: null or misaligned aux, its type or leading dimension", who);
-  if (ceil_div(a->rows, 32) * ceil_div(b->rows, 16) >= kMost)
+  if (a->rows > 32 && ceil_div(a->rows, 128) * ceil_div(b->rows, 128) > (1 << 24) - 8)  // 256 threads each
     return fail(MGN_ERR_SHAPE, "%s: c of %lld x %lld is too large for one call", who, (long long)a->rows,
                 (long long)b->rows);
   const size_t need = matmul8_workspace(a->rows, b->rows, a->cols);

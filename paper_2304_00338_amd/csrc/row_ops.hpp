@@ -12,6 +12,13 @@ namespace mgn {
 
 __host__ __device__ inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
+// n blocks of a launch as the rows of a grid (a dimension has under 2^32 threads):
+// block x + y * (blocks of a row), some of the last row being behind the last one.
+constexpr int64_t kGridRow = 1 << 20;
+inline dim3 grid_of(int64_t n) {
+  return dim3((unsigned)(n < kGridRow ? n : kGridRow), (unsigned)ceil_div(n, kGridRow));
+}
+
 // ---- quant8
 struct Quant8 {
   const void* x;

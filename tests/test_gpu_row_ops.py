@@ -821,3 +821,71 @@ def test_binding_refusals():
         with pytest.raises(mgn.MgnError):
             call()
             pytest.fail(f"call {i} was not refused")
+
+
+# ---------------------------------- more blocks than one dimension of a grid has
+def test_one_column_of_many_rows():
+    """2^28 + 17 rows of one value: each is its block's largest, so F or -F."""
+    n = 2 ** 28 + 17
+    x = torch.arange(n, device="cuda", dtype=torch.int32).remainder_(3).sub_(1).to(torch.bfloat16).view(n, 1)
+    m = mgn.mgn_quant8(x).rows
+    assert m.q.shape == (n, 16) and m.scale.shape == (1, n)
+    for r0 in range(0, n, 2 ** 26):
+        k = m.q[r0:r0 + 2 ** 26].view(torch.uint8)
+        v = x[r0:r0 + 2 ** 26, 0]
+        assert torch.equal(k[:, 0], torch.where(v == 0, 0, torch.where(v > 0, 0x7e, 0xfe)).to(torch.uint8))
+        assert not k[:, 1:].any()
+        s = torch.where(v == 0, 2.0 ** -126, float(np.float32(1) / np.float32(448))).to(torch.float32)
+        assert torch.equal(m.scale[0, r0:r0 + 2 ** 26], s)
+
+
+def test_one_row_of_many_columns():
+    n = 2 ** 30 + 200
+    x = torch.zeros((1, n), dtype=torch.bfloat16, device="cuda")
+    x[0, ::128] = 2.0
+    x[0, 1::128] = -1.0
+    m = mgn.mgn_quant8(x, "e5m2", block_rows=128).rows
+    k = m.q.view(torch.uint8)[0]
+    assert (k[:n:128] == 0x7b).all() and (k[1:n:128] == 0xf7).all()
+    assert int((k != 0).sum()) == 2 * (-(-n // 128))
+    assert (m.scale == float(np.float32(2) / np.float32(57344))).all()
+
+
+def test_column_sums_of_many_columns():
+    n = 2 ** 26 + 21
+    x = torch.arange(n, device="cuda", dtype=torch.int32).remainder_(251).to(torch.float32).view(1, n)
+    sums = mgn.mgn_quant8(torch.cat([x, x, x]), rowwise=False, colsum=True).colsum
+    assert torch.equal(sums, 3 * x[0])
+
+
+def test_matmul8_many_rows_of_b():
+    n = 2 ** 27 + 5
+    b = torch.arange(n, device="cuda", dtype=torch.int32).remainder_(13).float().to(torch.float8_e4m3fn)
+    q = torch.zeros((n, 16), dtype=torch.float8_e4m3fn, device="cuda")
+    q.view(torch.uint8)[:, 3] = b.view(torch.uint8)
+    b = mgn.Mat8(q, torch.full((1, -(-n // 128)), 0.5, device="cuda"), 16, 128)
+    a = torch.zeros((2, 16), dtype=torch.float8_e4m3fn, device="cuda")
+    a.view(torch.uint8)[:, 3] = 0x38  # 1
+    a = mgn.Mat8(a, torch.tensor([[1.0, -4.0]], device="cuda"))
+    c = mgn.mgn_matmul8(a, b, dtype=torch.bfloat16)
+    want = torch.arange(n, device="cuda", dtype=torch.int32).remainder_(13).to(torch.bfloat16) * 0.5
+    assert torch.equal(c[0], want) and torch.equal(c[1], -4 * want)
+
+
+def test_norm_gate_many_groups():
+    """2^22 + 9 gates of 600 rows: all but a few groups are empty."""
+    n, rows, cols = 2 ** 22 + 9, 600, 8
+    cut = torch.tensor([5, 2 ** 20 + 3, 2 ** 21, n - 2], device="cuda")
+    ptr = torch.bucketize(torch.arange(n + 1, device="cuda"), cut).to(torch.int32) * 150
+    x, b, dy = (randn(rows, cols, seed=s) for s in (1, 2, 3))
+    gate = randn(n, cols, seed=4)
+    y, _, stats = mgn.mgn_norm_gate_forward(x, b, gate=gate, gate_ptr=ptr, save=True)
+    group = cut.repeat_interleave(150)
+    want = x.double() + gate[group].double() * b.double()
+    assert ((y.double() - want).abs() <= 256 * U * (x.abs() + (gate[group] * b).abs()).double()).all()
+    g = mgn.mgn_norm_gate_backward(x, b, stats, dy, None, gate=gate, gate_ptr=ptr)
+    p = (dy.double() * b.double()).view(4, 150, cols)
+    assert ((g.dgate[cut].double() - p.sum(1)).abs() <= (150 + 512) * U * p.abs().sum(1)).all()
+    rest = torch.ones(n, dtype=torch.bool, device="cuda")
+    rest[cut] = False
+    assert not g.dgate[rest].any()

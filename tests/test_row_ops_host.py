@@ -163,3 +163,10 @@ def test_binding_refuses_host_tensors():
         with pytest.raises(mgn.MgnError) as e:
             call()
         assert e.value.code == mgn.ERR_ARG
+
+
+def test_matmul8_tiles_of_a_grid():
+    """2^24 tiles of 128 x 128 are refused, rows of b beside few rows of a are not tiles."""
+    tall = dict(cols=16, ld=16)
+    assert matmul8(a=mat8(rows=(1 << 31) - 1, **tall), b=mat8(rows=1, **tall), ldc=1) == mgn.ERR_SHAPE
+    assert "too large" in mgn.last_error()
