@@ -508,7 +508,7 @@ typedef struct mgn_rows {
 
 /* y and z from x and b; stats (nullable: inference) [rows][4] float32 keeps
  * mean and 1 / standard deviation of both norms for the reverse.  y may be x
- * and z may be b.  z is formed from the unrounded y.
+ * and z may be b (with the same ld).  z is formed from the unrounded y.
  * Errors: ARG, SHAPE, DEVICE. */
 int mgn_norm_gate_forward(const mgn_norm_gate* op, mgn_rows x, mgn_rows b, mgn_rows y,
                           mgn_rows z, float* stats, void* stream);

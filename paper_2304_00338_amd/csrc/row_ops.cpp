@@ -18,7 +18,7 @@ int64_t elem(int32_t t) { return t == MGN_BF16 ? 2 : 4; }
 int64_t up16(int64_t v) { return (v + 15) & ~(int64_t)15; }
 bool aligned(const void* p, int64_t a) { return ((uintptr_t)p & (uintptr_t)(a - 1)) == 0; }
 // every element's byte offset has to fit 63 bits
-bool fits(int64_t rows, int64_t ld) { return ld <= ((int64_t)1 << 40) && rows < kMost; }
+bool fits(int64_t rows, int64_t ld) { return ld <= ((int64_t)1 << 60) / (rows > 0 ? rows : 1); }
 
 int launched(hipError_t e, const char* who) {
   if (e != hipSuccess) return fail(MGN_ERR_DEVICE, "%s: %s", who, hipGetErrorString(e));
@@ -47,6 +47,14 @@ int check_rows(const mgn_rows& t, int64_t rows, int64_t cols, int32_t type, cons
   if (t.ld < cols || !fits(rows, t.ld) || !aligned(t.data, elem(type)))
     return fail(MGN_ERR_ARG, "%s: %s: leading dimension %lld for %lld columns, or a misaligned pointer", who, name,
                 (long long)t.ld, (long long)cols);
+  return MGN_OK;
+}
+
+// An output may stand in an input's place row for row, not in another output's.
+int check_in_place(const mgn_rows& out, const mgn_rows& in, int64_t rows, const char* who, const char* name) {
+  if (rows > 1 && out.data == in.data && out.ld != in.ld)
+    return fail(MGN_ERR_ARG, "%s: %s in place with another leading dimension (%lld, %lld)", who, name,
+                (long long)out.ld, (long long)in.ld);
   return MGN_OK;
 }
 
@@ -175,6 +183,10 @@ int mgn_norm_gate_forward(const mgn_norm_gate* op, mgn_rows x, mgn_rows b, mgn_r
     return rc;
   if (op->pre != MGN_NORM_NONE && (rc = check_rows(z, op->rows, op->cols, op->b_type, who, "z")) != MGN_OK) return rc;
   if (!aligned(stats, 16)) return fail(MGN_ERR_ARG, "%s: stats have to be 16-byte aligned", who);
+  if (op->pre != MGN_NORM_NONE && y.data == z.data) return fail(MGN_ERR_ARG, "%s: y and z are the same", who);
+  if ((rc = check_in_place(y, x, op->rows, who, "y")) != MGN_OK ||
+      (op->pre != MGN_NORM_NONE && (rc = check_in_place(z, b, op->rows, who, "z")) != MGN_OK))
+    return rc;
   a.x = x;
   a.b = b;
   a.y = y;
@@ -221,6 +233,14 @@ int mgn_norm_gate_backward(const mgn_norm_gate* op, mgn_rows x, mgn_rows b, cons
   if ((rc = mgn_norm_gate_workspace(op->rows, op->cols, &need)) != MGN_OK) return rc;
   if (need > 0 && (!ws || ws_bytes < need || !aligned(ws, 16)))
     return fail(MGN_ERR_WORKSPACE, "%s: workspace of %zu bytes, %zu needed", who, ws_bytes, need);
+  if (op->rows > 0) {
+    if (dx.data == db.data) return fail(MGN_ERR_ARG, "%s: dx and db are the same", who);
+    if ((rc = check_in_place(dx, x, op->rows, who, "dx")) != MGN_OK ||
+        (rc = check_in_place(dx, dy, op->rows, who, "dx")) != MGN_OK ||
+        (rc = check_in_place(db, b, op->rows, who, "db")) != MGN_OK ||
+        (rc = check_in_place(db, dz, op->rows, who, "db")) != MGN_OK)
+      return rc;
+  }
   const NormPlan p = norm_plan(op->rows, op->cols, true);
   a.x = x;
   a.b = b;

@@ -776,14 +776,18 @@ def _norm_gate(x, b, post, pre, post_gamma, post_beta, pre_gamma, pre_beta, gate
     if not 1 <= cols <= NORM_MAX_COLS:
         raise MgnError(ERR_SHAPE, f"{cols} columns (1 to {NORM_MAX_COLS})")
     if gate is not None:
-        if gate.dim() != 2 or gate.shape[1] != cols:
-            raise MgnError(ERR_ARG, f"gate has shape {tuple(gate.shape)}, expected (gates, {cols})")
+        if not isinstance(gate, torch.Tensor) or gate.dim() != 2 or gate.shape[1] != cols:
+            raise MgnError(ERR_ARG, f"gate must be a tensor of shape (gates, {cols})")
         n_gates = gate.shape[0]
+        if n_gates == 0 and rows > 0:
+            raise MgnError(ERR_ARG, f"no gates for {rows} rows (without a gate: None)")
         _vector(gate, "gate", n_gates * cols, dev)
     if gate_ptr is not None:
         _dptr(gate_ptr, torch.int32, (n_gates + 1,), "gate_ptr")
         if gate_ptr.device != dev:
             raise MgnError(ERR_ARG, f"gate_ptr is on {gate_ptr.device}, expected {dev}")
+        if gate is not None and n_gates == 0:
+            gate_ptr = None  # no groups and no rows
     return CNormGate(rows, cols, xt, bt, NORMS[post], NORMS[pre], eps, skip, scale,
                      _vector(post_gamma, "post_gamma", cols, dev), _vector(post_beta, "post_beta", cols, dev),
                      _vector(pre_gamma, "pre_gamma", cols, dev), _vector(pre_beta, "pre_beta", cols, dev), _at(gate),

@@ -889,3 +889,21 @@ def test_norm_gate_many_groups():
     rest = torch.ones(n, dtype=torch.bool, device="cuda")
     rest[cut] = False
     assert not g.dgate[rest].any()
+
+
+def test_norm_gate_no_gates():
+    """No gates for some rows are refused; an empty batch has none and no groups."""
+    x, gate = randn(6, 40), randn(0, 40)
+    ptr = torch.zeros(1, dtype=torch.int32, device="cuda")
+    for kw in (dict(gate=gate), dict(gate=gate, gate_ptr=ptr), dict(gate=[1.0])):
+        with pytest.raises(mgn.MgnError):
+            mgn.mgn_norm_gate_forward(x, x, **kw)
+    y, _, st = mgn.mgn_norm_gate_forward(x[:0], x[:0], gate=gate, gate_ptr=ptr, save=True)
+    g = mgn.mgn_norm_gate_backward(x[:0], x[:0], st, y, None, gate=gate, gate_ptr=ptr)
+    assert y.shape == (0, 40) and g.dgate.shape == (0, 40) and g.dx.shape == (0, 40)
+
+
+def test_norm_gate_in_place_of_another_layout():
+    x = randn(6, 80)
+    with pytest.raises(mgn.MgnError):  # rows 80 apart read, 40 apart written
+        mgn.mgn_norm_gate_forward(x[:, :40], randn(6, 40), y=x.view(12, 40)[:6])

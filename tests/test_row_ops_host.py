@@ -170,3 +170,31 @@ def test_matmul8_tiles_of_a_grid():
     tall = dict(cols=16, ld=16)
     assert matmul8(a=mat8(rows=(1 << 31) - 1, **tall), b=mat8(rows=1, **tall), ldc=1) == mgn.ERR_SHAPE
     assert "too large" in mgn.last_error()
+
+
+Q = P + (1 << 20)
+
+
+@pytest.mark.parametrize("kw", [
+    dict(x=R(ld=8), y=R(), z=R(Q), b=R(Q)), dict(x=R(), y=R(), b=R(Q), z=R(Q, 8)),  # in place, ld differs
+    dict(x=R(), b=R(Q), y=R(), z=R()),  # y and z the same
+])
+def test_norm_gate_forward_in_place_refusals(kw):
+    assert forward(**kw) == mgn.ERR_ARG
+    assert "in place" in mgn.last_error() or "same" in mgn.last_error()
+
+
+@pytest.mark.parametrize("kw", [
+    dict(x=R(ld=8), dx=R(), db=R(Q)), dict(dy=R(ld=8), dx=R(), db=R(Q)), dict(b=R(Q, 8), dx=R(), db=R(Q)),
+    dict(dz=R(Q, 8), b=R(Q), dx=R(), db=R(Q)), dict(dx=R(), db=R()),
+])
+def test_norm_gate_backward_in_place_refusals(kw):
+    assert backward(**kw) == mgn.ERR_ARG
+    assert "in place" in mgn.last_error() or "same" in mgn.last_error()
+
+
+def test_far_rows_refused():
+    far = 1 << 59  # 4 rows of it end past 63 bits of bytes
+    assert quant8(ldx=far) == mgn.ERR_ARG and quant8(ldq=far) == mgn.ERR_ARG
+    assert matmul8(a=mat8(ld=far)) == mgn.ERR_ARG and matmul8(ldc=far) == mgn.ERR_ARG
+    assert forward(x=R(ld=far)) == mgn.ERR_ARG
