@@ -129,7 +129,7 @@ int mgn_quant8(const void* x, int32_t x_type, int64_t rows, int64_t cols, int64_
     return fail(MGN_ERR_WORKSPACE, "%s: workspace of %zu bytes, %zu needed", who, ws_bytes, need);
   if (!q && !qt && !colsum) return MGN_OK;
   const Quant8 a = {x, x_type, format, block_rows, rows, cols, ldx, q, qt, ldq, ldqt, scale, scale_t, colsum, (float*)ws,
-                    accumulate, 1};
+                    accumulate};
   return launched(launch_quant8(a, (hipStream_t)stream), who);
 }
 

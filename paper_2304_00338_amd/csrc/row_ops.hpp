@@ -28,9 +28,8 @@ struct Quant8 {
   int64_t ldq, ldqt;
   float *scale, *scale_t;
   float* colsum;  // nullable
-  float* part;    // [at most ceil(rows / 128)][cols] partial column sums
+  float* part;    // [ceil(rows / 128)][cols] partial column sums
   int32_t accumulate;
-  int64_t per;    // 128-row blocks that a block of k_quant_tile takes
 };
 hipError_t launch_quant8(const Quant8& a, hipStream_t s);
 
@@ -72,8 +71,7 @@ NormPlan norm_plan(int64_t rows, int cols, bool backward);
 hipError_t launch_norm_gate_forward(const NormGate& a, hipStream_t s);
 hipError_t launch_norm_gate_backward(const NormGate& a, hipStream_t s);
 
-// out[c] (+)= sum over b < nb of part[b stride + c], in a fixed order.
-hipError_t launch_column_reduce(const float* part, int64_t nb, int64_t stride, int64_t cols, float* out,
-                                int32_t accumulate, hipStream_t s);
+// out[c] (+)= sum over b < nb of part[b cols + c], in a fixed order; part is overwritten.
+hipError_t launch_column_reduce(float* part, int64_t nb, int64_t cols, float* out, int32_t accumulate, hipStream_t s);
 
 }  // namespace mgn

@@ -907,3 +907,18 @@ def test_norm_gate_in_place_of_another_layout():
     x = randn(6, 80)
     with pytest.raises(mgn.MgnError):  # rows 80 apart read, 40 apart written
         mgn.mgn_norm_gate_forward(x[:, :40], randn(6, 40), y=x.view(12, 40)[:6])
+
+
+@pytest.mark.parametrize("rows,cols", [(1024 * 128, 5), (1024 * 128 + 1, 130), (300000, 33)])
+def test_column_sums_of_many_rows(rows, cols):
+    """A tile's 128 rows one after the other at worst, then the tiles: (rows + 512) u of the magnitudes."""
+    x = randn(rows, cols, seed=rows)
+    start = randn(cols, seed=7)
+    sums = mgn.mgn_quant8(x, rowwise=False, colsum=True).colsum
+    tol = (rows + 512) * U * x.abs().double().sum(0)
+    assert ((sums.double() - x.double().sum(0)).abs() <= tol).all()
+    assert torch.equal(sums, mgn.mgn_quant8(x, colsum=True).colsum)
+    more = mgn.mgn_quant8(x, rowwise=False, colsum=start.clone(), accumulate=True).colsum
+    assert torch.equal(more, start + sums)
+    ones = mgn.mgn_quant8(torch.ones_like(x), rowwise=False, colsum=True).colsum
+    assert (ones == rows).all()
