@@ -75,9 +75,9 @@ __device__ __forceinline__ float scale_of(float amax, float& inv) {
 
 // x / s as a float that rounds to the format as the quotient itself does: a float
 // beside it whose last bit is set where the quotient has more bits.  t is within
-// 2 ulp, the remainder x - t s is exact (s in [2^-46, 2^120], and where it is not, t is
-// so small that all its neighbours round to 0), and one correction leaves an
-// error under an ulp, whose side the second remainder tells.
+// 2 ulp, and one correction by the remainder x - t s leaves an error under an ulp,
+// whose side the next remainder tells: that one is exact (s in [2^-46, 2^120]; where
+// it is not, t is so small that all its neighbours round to 0).
 __device__ __forceinline__ float quotient(float x, float s, float inv) {
   const float a = __builtin_fabsf(x);
   float t = a * inv;
