@@ -922,3 +922,29 @@ def test_column_sums_of_many_rows(rows, cols):
     assert torch.equal(more, start + sums)
     ones = mgn.mgn_quant8(torch.ones_like(x), rowwise=False, colsum=True).colsum
     assert (ones == rows).all()
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "e5m2"])
+def test_quant8_middles_at_any_scale(fmt):
+    """Middles of neighbouring numbers, and floats up to three steps beside them, under scales from 2^-126 to 2^100."""
+    rng = np.random.default_rng(11)
+    tab = table(fmt)
+    mid = (tab[1:] + tab[:-1]) / 2
+    rows = []
+    for e in list(range(-126, -30, 3)) + list(range(-30, 101, 10)):
+        s = np.float32(2.0 ** e * (1 + rng.random()))
+        v = (rng.choice(mid, 127) * float(s)).astype(np.float32)
+        for _ in range(3):
+            to = rng.choice(np.array([-np.inf, 0, np.inf], dtype=np.float32), 127)
+            v = np.where(to == 0, v, np.nextafter(v, to))
+        rows.append(np.concatenate([[np.float32(F8[fmt][1] * float(s))], v]) * rng.choice([-1, 1], 128).astype(np.float32))
+    x = np.stack(rows).astype(np.float32)
+    out = mgn.mgn_quant8(torch.from_numpy(x).cuda(), fmt, 1, True)
+    check_mat8(out.rows, *oracle_quant(x, fmt, 1), "rows")
+    out = mgn.mgn_quant8(torch.from_numpy(np.ascontiguousarray(x.T)).cuda(), fmt, 1, False, True)
+    check_mat8(out.columns, *oracle_quant(x, fmt, 1), "columns")
+    for r in x:  # each a block of its own
+        out = mgn.mgn_quant8(torch.from_numpy(r[None]).cuda(), fmt, 128, True, True)
+        q, s = oracle_quant(r[None], fmt, 128)
+        check_mat8(out.rows, q, s, "square")
+        check_mat8(out.columns, np.ascontiguousarray(q.T), s.T, "square, turned")
