@@ -358,18 +358,13 @@ __global__ void __launch_bounds__(MAXT) k_norm_gate_bwd(NormGate a) {
       open = gates.held;
       gate_vectors(ga, gb, a, open, at);
     }
+    // A row that counts for nothing may hold anything, and the gate at hand may
+    // be of no row: the walker's lanes, which agree on it, form nothing of it (0
+    // times an infinity would be a NaN in all sums).
+    if (LPR != 0 && !mine) continue;
     if (!PRE) fetch(r);
     float x[NV][8], b[NV][8], t[NV][8], z[NV][8];
-    float4 s = ns;
-    if (LPR != 0 && !mine) {
-      // statistics and gradients 0: everything below is 0
-      s = float4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int k = 0; k < NV; ++k) {
-        ny[k] = Raw8<XT>{};
-        nz[k] = Raw8<BT>{};
-      }
-    }
+    const float4 s = ns;
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
       // bhat is not 0 beyond the lane's columns, but ga and the gradients are
@@ -423,7 +418,7 @@ __global__ void __launch_bounds__(MAXT) k_norm_gate_bwd(NormGate a) {
         s1 += t[k][e];
         s2 = __builtin_fmaf(t[k][e], b[k][e], s2);
       }
-      if (mine) at.template store<XT>(a.dx, r, k, dx);
+      at.template store<XT>(a.dx, r, k, dx);
     }
     if (op.post != MGN_NORM_NONE) {
       red.sum2(s1, s2);
@@ -435,8 +430,7 @@ __global__ void __launch_bounds__(MAXT) k_norm_gate_bwd(NormGate a) {
         for (int e = 0; e < 8; ++e) t[k][e] = s.y * (t[k][e] - s1 - b[k][e] * s2);
     }
 #pragma unroll
-    for (int k = 0; k < NV; ++k)
-      if (mine) at.template store<BT>(a.db, r, k, t[k]);
+    for (int k = 0; k < NV; ++k) at.template store<BT>(a.db, r, k, t[k]);
   }
   if (MANY && open >= 0) settle(open);
   // the block's sums, one vector after the other
