@@ -151,7 +151,9 @@ __device__ __forceinline__ void statistics(const float (&v)[NV][8], const Place<
   rstd = 1.f / __builtin_sqrtf(__builtin_fmaf(red.sum(q), inv, eps));
 }
 
-// Which gate a row has.  Groups are looked up once and followed from row to row.
+// Which gate a row has.  Groups are looked up once and followed from row to row: a
+// step to the next group, and behind that, where groups are empty, a search again
+// (any number of them can lie between two rows).
 struct Gates {
   int64_t g = 0, held = -1;
   __device__ __forceinline__ Gates(const NormGate& a, int64_t r0) {
@@ -164,7 +166,10 @@ struct Gates {
       fresh = true;
       held = r;
     } else if (a.gmode == kGateGroup) {
-      while (g + 1 < a.op.n_gates && r >= a.op.gate_ptr[g + 1]) ++g;
+      if (g + 1 < a.op.n_gates && r >= a.op.gate_ptr[g + 1]) {
+        ++g;
+        if (g + 1 < a.op.n_gates && r >= a.op.gate_ptr[g + 1]) g += find_group(a.op.gate_ptr + g, a.op.n_gates - g, r);
+      }
       if (r < a.op.gate_ptr[g] || r >= a.op.gate_ptr[g + 1]) return false;
       fresh = g != held;
       held = g;
