@@ -456,7 +456,9 @@ typedef struct mgn_epilogue {
 
 /* c[m][n] = act(sum_k a[m][k] b[n][k] + bias[n]), c [a->rows][b->rows] of type
  * MGN_FP32 or MGN_BF16.  A block of 128 products is summed, scaled, and added to
- * a float32 sum.  For an MGN_FP32 c the block is summed in float32.  For an
+ * a float32 sum; scales are of any size up to 2^124 (a quantised float32 has less
+ * than 2^120), and a result that float32 holds comes out so also where the product
+ * of two scales is none.  For an MGN_FP32 c the block is summed in float32.  For an
  * MGN_BF16 c it is summed by the 8-bit matrix instructions, twice as fast, which
  * add eight products at a time and cut each off 2^-13 below the largest of the
  * eight (1.5e-5 of a block's sum on normal values, a hundredth of the rounding

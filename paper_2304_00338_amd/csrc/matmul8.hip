@@ -31,19 +31,37 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 static_assert(MGN_E4M3 == 2 && MGN_E5M2 == 3, "8-bit formats in the order of the instruction's codes");
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
-// Eight 8-bit numbers as bf16: every one of them is a normal bf16 number or 0.
+// Scales.  Their product may leave the normal numbers where the result does not
+// (twice 2^70 before a sum of 2^-30, or before a sum of 0, which would become a NaN).
+// So half of each one's power of two, 2^floor(e / 2), goes into the matrix instruction
+// with the operand, or into its widening, and the sum is multiplied by the product of
+// the rests, which is a normal number for scales up to 2^124: what comes out of the
+// instruction lies between the plain sum and the result.  Both are exact, so a result
+// has the bits that it has by the product of the scales, where that is normal.
+// (Measured against that product: 32,768 x 4096 x 4096 1% more time, three steps of
+// 434,558 x 128 x 384 to fp32 3%, scales for each row of b 5%; with the halves and
+// rests formed by each wave for itself 10, 13 and 6.)
+__device__ __forceinline__ uint32_t half_of(float s) {  // last byte: 127 + floor(e / 2)
+  return (__float_as_uint(s) & 0x7fffffffu) + 0x3f800000u;
+}
+__device__ __forceinline__ float rest_of(float s) {
+  return __builtin_amdgcn_ldexpf(s, 127 - (int)(half_of(s) >> 24));
+}
+
+// Eight 8-bit numbers times a scale's half as bf16: exact, normal or 0.
 template <int F>
-__device__ __forceinline__ bf16x8 widen(int lo, int hi) {
+__device__ __forceinline__ bf16x8 widen(int lo, int hi, uint32_t half) {
+  const float s = __uint_as_float(half >> 1);  // its exponent is what counts
   bf16x2 v[4];
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     const int w = i ? hi : lo;
     if constexpr (F == MGN_E4M3) {
-      v[2 * i] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.f, false);
-      v[2 * i + 1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.f, true);
+      v[2 * i] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, s, false);
+      v[2 * i + 1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, s, true);
     } else {
-      v[2 * i] = __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(w, 1.f, false);
-      v[2 * i + 1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(w, 1.f, true);
+      v[2 * i] = __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(w, s, false);
+      v[2 * i + 1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(w, s, true);
     }
   }
   return bf16x8{v[0][0], v[0][1], v[1][0], v[1][1], v[2][0], v[2][1], v[3][0], v[3][1]};
@@ -177,7 +195,10 @@ __global__ void __launch_bounds__(WM * WN * 64, 2) k_matmul8_tile(Job J) {
   static_assert(NWV % 2 == 0, "a wave's groups of 8 rows have one parity");
   static_assert((BM + BN) * 128 >= NWV * 32 * TN * 32 * 4, "results fit a buffer");
   __shared__ __align__(16) uint8_t buf0[(BM + BN) * 128], buf1[(BM + BN) * 128];
-  __shared__ __align__(16) float sbuf[BROW ? 2 : 1][BROW ? BN : 4];
+  // scales of a's rows and (BROW) of b's, each as its half and its rest
+  constexpr int ROWS = BM + (BROW ? BN : 0);
+  __shared__ __align__(16) float rest[2][ROWS];
+  __shared__ uint32_t half[2][ROWS];
   const Matmul8& p = J.p;
   const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), j = l & 31, h = l >> 5;
   const int wm = w / WN, wn = w % WN;
@@ -241,26 +262,24 @@ __global__ void __launch_bounds__(WM * WN * 64, 2) k_matmul8_tile(Job J) {
       }
     }
   };
-  // scales: of the wave's rows of a one a lane and 32 rows; of b one for the
-  // wave's columns, which lie in one block of 128, or one for each of the tile's
+  // scales: a thread fetches that of one row of a, or (BROW) of b; what all waves need
+  // of it is formed once and goes through LDS.  Else one of b is all that a wave's
+  // columns have, which lie in one block of 128.
+  static_assert((ROWS & (ROWS - 1)) == 0 && ROWS <= NWV * 64, "threads for all rows");
   const int sha = p.a.block_rows == 128 ? 7 : 0, shb = p.b.block_rows == 128 ? 7 : 0;
   const int64_t Ra = ceil_div(p.a.rows, p.a.block_rows), Rb = ceil_div(p.b.rows, p.b.block_rows);
-  const int64_t ma = m0 + wm * TM * 32, ma0 = min(ma, p.a.rows - 1) >> sha;
-  uint32_t ia[TM];
-#pragma unroll
-  for (int i = 0; i < TM; ++i) ia[i] = (uint32_t)((min(ma + i * 32 + j, p.a.rows - 1) >> sha) - ma0);
-  const int64_t nb0 = BROW ? n0 : min(n0 + wn * TN * 32, p.b.rows - 1) >> shb;
-  const uint32_t ib = BROW ? (uint32_t)min((int64_t)(threadIdx.x & (BN - 1)), p.b.rows - 1 - n0) : 0;
-  float sa[TM], sb, na[TM], nb;
-  auto scales = [&](int64_t kb) {
-    const float* pa = p.a.scale + kb * Ra + ma0;
-#pragma unroll
-    for (int i = 0; i < TM; ++i) {
-      uint32_t at = ia[i];
-      asm volatile("" : "+v"(at));
-      na[i] = pa[at];
-    }
-    nb = (p.b.scale + kb * Rb + nb0)[ib];
+  const int srow = threadIdx.x & (ROWS - 1);
+  const bool ofb = BROW && srow >= BM;
+  const int64_t sstep = ofb ? Rb : Ra;
+  const float* sfrom = (ofb ? p.b.scale + min(n0 + srow - BM, p.b.rows - 1)
+                            : p.a.scale + (min(m0 + srow, p.a.rows - 1) >> sha)) + kb0 * sstep;
+  const int64_t nb0 = min(n0 + wn * TN * 32, p.b.rows - 1) >> shb;
+  uint32_t hb = 0;
+  float rb = 0.f, ns, nb = 0.f;
+  auto scales = [&](int64_t kb) {  // kb0, and the next one each time
+    ns = *sfrom;
+    sfrom += sstep;
+    if constexpr (!BROW) nb = (p.b.scale + kb * Rb)[nb0];
   };
 
   f32x16 acc[TM][TN] = {};
@@ -273,11 +292,12 @@ __global__ void __launch_bounds__(WM * WN * 64, 2) k_matmul8_tile(Job J) {
     const uint4 lo = *(const uint4*)(rows + off[s][0]), hi = *(const uint4*)(rows + off[s][1]);
     return i32x8{(int)lo.x, (int)lo.y, (int)lo.z, (int)lo.w, (int)hi.x, (int)hi.y, (int)hi.z, (int)hi.w};
   };
-  auto add = [&](f32x16& to, const f32x16& part, float fa, float fb, const float* sbn) {
+  // fa, fb, rests: of the scales
+  auto add = [&](f32x16& to, const f32x16& part, float fa, float fb, const float* rests) {
     if constexpr (BROW) {
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
-        const f32x4 s4 = *(const f32x4*)(sbn + 8 * g + 4 * h);
+        const f32x4 s4 = *(const f32x4*)(rests + 8 * g + 4 * h);
 #pragma unroll
         for (int e = 0; e < 4; ++e) to[4 * g + e] = __builtin_fmaf(part[4 * g + e], fa * s4[e], to[4 * g + e]);
       }
@@ -296,13 +316,20 @@ __global__ void __launch_bounds__(WM * WN * 64, 2) k_matmul8_tile(Job J) {
       for (int n = 0; n < TN; ++n) add(acc[TM - 1][n], open[n], open_a, open_b, nullptr);
     }
   };
-  auto products = [&](const uint8_t* buf, const float* sbn) {
+  auto products = [&](const uint8_t* buf, int at) {
     const uint8_t* rowsa = buf + wm * TM * 32 * 128;
     const uint8_t* rowsb = buf + (BM + wn * TN * 32) * 128;
-    sbn += BROW ? wn * TN * 32 : 0;
+    const float *const resta = rest[at] + wm * TM * 32 + j, *const restb = rest[at] + (BROW ? BM + wn * TN * 32 : 0);
+    const uint32_t *const halfa = half[at] + wm * TM * 32 + j, *const halfb = half[at] + (BROW ? BM + wn * TN * 32 : 0) + j;
+    uint32_t hbn[TN];
+#pragma unroll
+    for (int n = 0; n < TN; ++n) hbn[n] = BROW ? halfb[n * 32] : hb;
     if constexpr (WIDE) {
       // every operand is widened once: 16 columns of all TM + TN at a time
       f32x16 part[TM][TN] = {};
+      uint32_t han[TM];
+#pragma unroll
+      for (int m = 0; m < TM; ++m) han[m] = halfa[m * 32];
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
         i32x8 fa[TM], fb[TN];
@@ -312,26 +339,30 @@ __global__ void __launch_bounds__(WM * WN * 64, 2) k_matmul8_tile(Job J) {
         for (int n = 0; n < TN; ++n) fb[n] = frag(rowsb + n * 4096, s);
 #pragma unroll
         for (int i = 0; i < 8; i += 2) {
-          bf16x8 wa[TM], wb[TN];
+          bf16x8 va[TM], vb[TN];
 #pragma unroll
-          for (int m = 0; m < TM; ++m) wa[m] = widen<FA>(fa[m][i], fa[m][i + 1]);
+          for (int m = 0; m < TM; ++m) va[m] = widen<FA>(fa[m][i], fa[m][i + 1], han[m]);
 #pragma unroll
-          for (int n = 0; n < TN; ++n) wb[n] = widen<FB>(fb[n][i], fb[n][i + 1]);
+          for (int n = 0; n < TN; ++n) vb[n] = widen<FB>(fb[n][i], fb[n][i + 1], hbn[n]);
 #pragma unroll
           for (int m = 0; m < TM; ++m)
 #pragma unroll
             for (int n = 0; n < TN; ++n)
-              part[m][n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wb[n], wa[m], part[m][n], 0, 0, 0);
+              part[m][n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vb[n], va[m], part[m][n], 0, 0, 0);
         }
         __builtin_amdgcn_sched_barrier(0);
       }
 #pragma unroll
       for (int m = 0; m < TM; ++m)
 #pragma unroll
-        for (int n = 0; n < TN; ++n) add(acc[m][n], part[m][n], sa[m], sb, sbn + (BROW ? n * 32 : 0));
+        for (int n = 0; n < TN; ++n) add(acc[m][n], part[m][n], resta[m * 32], rb, restb + (BROW ? n * 32 : 0));
     } else {
       // the last 32 rows' products are added under the next step's first reads
       i32x8 fb[TN][2], fa[2][2];
+      uint32_t han[2];
+      float ran[2];
+      han[0] = halfa[0];
+      ran[0] = resta[0];
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
         fa[0][s] = frag(rowsa, s);
@@ -349,31 +380,37 @@ __global__ void __launch_bounds__(WM * WN * 64, 2) k_matmul8_tile(Job J) {
 #pragma unroll
           for (int n = 0; n < TN; ++n)
             part[n] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fb[n][s], fa[m & 1][s], s ? part[n] : f32x16{},
-                                                                      FB - MGN_E4M3, FA - MGN_E4M3, 0, 0, 0, 0);
+                                                                      FB - MGN_E4M3, FA - MGN_E4M3, 3, (int)hbn[n], 3,
+                                                                      (int)han[m & 1]);
         if (m + 1 < TM) {
 #pragma unroll
           for (int s = 0; s < 2; ++s) fa[(m + 1) & 1][s] = frag(rowsa + (m + 1) * 4096, s);
+          han[(m + 1) & 1] = halfa[(m + 1) * 32];
+          ran[(m + 1) & 1] = resta[(m + 1) * 32];
         }
         if (BROW || m + 1 < TM) {
 #pragma unroll
-          for (int n = 0; n < TN; ++n) add(acc[m][n], part[n], sa[m], sb, sbn + (BROW ? n * 32 : 0));
+          for (int n = 0; n < TN; ++n) add(acc[m][n], part[n], ran[m & 1], rb, restb + (BROW ? n * 32 : 0));
         } else {
 #pragma unroll
           for (int n = 0; n < TN; ++n) open[n] = part[n];
-          open_a = sa[m];
-          open_b = sb;
+          open_a = ran[m & 1];
+          open_b = rb;
         }
         // else the compiler has all reads and products of a step in registers at once
         __builtin_amdgcn_sched_barrier(0);
       }
     }
   };
-  auto take = [&](int to) {  // the fetched scales are the next step's
-#pragma unroll
-    for (int i = 0; i < TM; ++i) sa[i] = na[i];
-    sb = nb;
-    if constexpr (BROW) {
-      if ((int)threadIdx.x < BN) sbuf[to][threadIdx.x] = nb;
+  // The fetched scales are the next step's.  (Where there are more threads than rows two
+  // write the same value: a branch here moved products of the step behind it, and
+  // the large tiles spilled.)
+  auto take = [&](int to) {
+    half[to][srow] = half_of(ns);
+    rest[to][srow] = rest_of(ns);
+    if constexpr (!BROW) {  // one for the wave
+      hb = __builtin_amdgcn_readfirstlane(half_of(nb));
+      rb = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(rest_of(nb))));
     }
   };
 
@@ -388,15 +425,15 @@ __global__ void __launch_bounds__(WM * WN * 64, 2) k_matmul8_tile(Job J) {
         scales(kb + 1);
         fetch(buf1, kb + 1);
       }
-      products(buf0, sbuf[0]);
+      products(buf0, 0);
       if (left > 1) {
-        take(BROW ? 1 : 0);
+        take(1);
         __syncthreads();
         if (left > 2) {
           scales(kb + 2);
           fetch(buf0, kb + 2);
         }
-        products(buf1, sbuf[BROW ? 1 : 0]);
+        products(buf1, 1);
         take(0);
         __syncthreads();
       }
@@ -440,15 +477,16 @@ __global__ void __launch_bounds__(WM * WN * 64, 2) k_matmul8_tile(Job J) {
 // 15.4 (3.8 TB/s), 23 x 10007 x 5000 25 (2.0 TB/s: every block reads a through L1,
 // twice the weights' bytes).
 template <bool WIDE, int FB, int FA>
-__device__ __forceinline__ f32x4 mma16(i32x8 b, i32x8 a) {
+__device__ __forceinline__ f32x4 mma16(i32x8 b, i32x8 a, uint32_t hb, uint32_t ha) {
   f32x4 c = {0.f, 0.f, 0.f, 0.f};
   if constexpr (WIDE) {
 #pragma unroll
     for (int i = 0; i < 8; i += 2)
-      c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen<FB>(b[i], b[i + 1]), widen<FA>(a[i], a[i + 1]), c, 0, 0, 0);
+      c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen<FB>(b[i], b[i + 1], hb), widen<FA>(a[i], a[i + 1], ha), c, 0, 0, 0);
     return c;
   } else {
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b, a, c, FB - MGN_E4M3, FA - MGN_E4M3, 0, 0, 0, 0);
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b, a, c, FB - MGN_E4M3, FA - MGN_E4M3, 3, (int)hb, 3,
+                                                            (int)ha);
   }
 }
 
@@ -465,7 +503,7 @@ __global__ void __launch_bounds__(512) k_matmul8_few(Job J) {
   const int sha = p.a.block_rows == 128 ? 7 : 0, shb = p.b.block_rows == 128 ? 7 : 0;
   const int64_t Ra = ceil_div(p.a.rows, p.a.block_rows), Rb = ceil_div(p.b.rows, p.b.block_rows);
   const uint8_t *rb = p.b.q + min(n0 + j, p.b.rows - 1) * p.b.ld + q * 32, *ra[TM];
-  const float *psa[TM], *psb[4];
+  const float *psa[TM], *psb[4], *psj = p.b.scale + (min(n0 + j, p.b.rows - 1) >> shb);
 #pragma unroll
   for (int i = 0; i < TM; ++i) {
     const int64_t m = min((int64_t)i * 16 + j, p.a.rows - 1);
@@ -483,10 +521,11 @@ __global__ void __launch_bounds__(512) k_matmul8_few(Job J) {
   };
   struct Step {
     i32x8 a[TM], b;
-    float sa[TM], sb[4];
+    float sa[TM], sb[4], sj;
   };
   auto fetch = [&](Step& x, int64_t kb) {
     x.b = get(rb, kb);
+    x.sj = psj[kb * Rb];
 #pragma unroll
     for (int r = 0; r < 4; ++r) x.sb[r] = psb[r][kb * Rb];
 #pragma unroll
@@ -499,9 +538,10 @@ __global__ void __launch_bounds__(512) k_matmul8_few(Job J) {
   auto products = [&](const Step& x) {
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
-      const f32x4 part = mma16<WIDE, FB, FA>(x.b, x.a[i]);
+      const f32x4 part = mma16<WIDE, FB, FA>(x.b, x.a[i], half_of(x.sj), half_of(x.sa[i]));
 #pragma unroll
-      for (int r = 0; r < 4; ++r) acc[i][r] = __builtin_fmaf(part[r], x.sa[i] * x.sb[r], acc[i][r]);
+      for (int r = 0; r < 4; ++r)
+        acc[i][r] = __builtin_fmaf(part[r], rest_of(x.sa[i]) * rest_of(x.sb[r]), acc[i][r]);
     }
   };
   if (kb0 + w < kb1) {
