@@ -458,16 +458,18 @@ typedef struct mgn_epilogue {
  * MGN_FP32 or MGN_BF16.  A block of 128 products is summed, scaled, and added to
  * a float32 sum; scales are of any size up to 2^124 (a quantised float32 has less
  * than 2^120), and a result that float32 holds comes out so also where the product
- * of two scales is none.  For an MGN_FP32 c the block is summed in float32.  For an
- * MGN_BF16 c it is summed by the 8-bit matrix instructions, twice as fast, which
- * add eight products at a time and cut each off 2^-13 below the largest of the
- * eight (1.5e-5 of a block's sum on normal values, a hundredth of the rounding
- * of c).  A layer
- * y = x W^T takes a = rows of x, b = rows of W; its input gradient dy W takes
- * a = rows of dy, b = the transpose of W; its weight gradient dy^T x takes the
- * transposes of dy and x, whose blocks run along the rows.  epilogue NULL: none.
- * cols 0 gives zero sums.  A workspace of mgn_matmul8_workspace bytes (which
- * may be 0) splits long sums over the device.
+ * of two scales is none.
+ * For an MGN_FP32 c, and for up to 16 rows of a, the block is summed in float32.
+ * For an MGN_BF16 c of more rows it is summed by the 8-bit matrix instructions, up
+ * to twice as fast, which add eight products at a time and cut each off 2^-13
+ * below the largest of the eight (1.5e-5 of a block's sum on normal values, a
+ * hundredth of the rounding of c; more of a sum that is small because large
+ * products cancel).
+ * A layer y = x W^T takes a = rows of x, b = rows of W; its input gradient dy W
+ * takes a = rows of dy, b = the transpose of W; its weight gradient dy^T x takes
+ * the transposes of dy and x, whose blocks run along the rows.  epilogue NULL:
+ * none.  cols 0 gives zero sums.  A workspace of mgn_matmul8_workspace bytes
+ * (which may be 0) splits long sums over the device.
  * Errors: ARG, SHAPE (a->cols != b->cols, 2^31 rows or columns, or c of about 2^24
  * tiles of 128 x 128), WORKSPACE, DEVICE. */
 int mgn_matmul8_workspace(int64_t a_rows, int64_t b_rows, int64_t cols, size_t* ws_bytes);
