@@ -201,7 +201,7 @@ __device__ __forceinline__ void gate_vectors(float (&ga)[NV][8], float (&gb)[NV]
 }
 
 template <typename XT, typename BT, int LPR, int NV, int MAXT>
-__global__ void __launch_bounds__(MAXT, LPR ? 4 : MAXT == 640 ? 5 : 1) k_norm_gate_fwd(NormGate a) {
+__global__ void __launch_bounds__(MAXT, LPR ? 4 : 1) k_norm_gate_fwd(NormGate a) {
   __shared__ float buf[64];
   const mgn_norm_gate& op = a.op;
   const Place<LPR, NV> at(op.rows, op.cols, a.per);
@@ -576,39 +576,42 @@ NormPlan norm_plan(int64_t rows, int cols, bool backward) {
   return p;
 }
 
-// The instantiation for a plan: K(lanes, runs of a lane, most threads).
-#define MGN_NG_PLAN(K)                   \
-  do {                                   \
-    if (p.lpr == 16)                     \
-      K(16, 1, 256);                     \
-    else if (p.lpr == 32)                \
-      K(32, 1, 256);                     \
-    else if (p.lpr == 64)                \
-      K(64, 1, 256);                     \
-    else if (p.vpt == 16 && p.threads <= 512) \
-      K(0, 2, 512);                      \
-    else if (p.vpt == 16)                \
-      K(0, 2, 1024);                     \
-    else if (p.threads <= 512)           \
-      K(0, 1, 512);                      \
-    else if (p.threads <= 640)           \
-      K(0, 1, 640);                      \
-    else                                 \
-      K(0, 1, 1024);                     \
-  } while (0)
-
+// The instantiation for a plan: K(lanes, runs of a lane, most threads).  The forward's
+// with one run has 89 to 95 registers for any number of threads.
 template <typename XT, typename BT>
 void launch_fwd(const NormGate& a, const NormPlan& p, hipStream_t s) {
   const dim3 g((unsigned)p.blocks), t(p.threads);
 #define MGN_NG_FWD(L, NV, MAXT) hipLaunchKernelGGL((k_norm_gate_fwd<XT, BT, L, NV, MAXT>), g, t, 0, s, a)
-  MGN_NG_PLAN(MGN_NG_FWD);
+  if (p.lpr == 16)
+    MGN_NG_FWD(16, 1, 256);
+  else if (p.lpr == 32)
+    MGN_NG_FWD(32, 1, 256);
+  else if (p.lpr == 64)
+    MGN_NG_FWD(64, 1, 256);
+  else if (p.vpt == 8)
+    MGN_NG_FWD(0, 1, 1024);
+  else
+    MGN_NG_FWD(0, 2, 1024);
 }
 template <typename XT, typename BT, bool MANY>
 void launch_bwd(const NormGate& a, const NormPlan& p, hipStream_t s) {
   const dim3 g((unsigned)p.blocks), t(p.threads);
   const size_t lds = p.lpr ? (size_t)(p.threads / p.lpr) * a.op.cols * 4 : 0;
 #define MGN_NG_BWD(L, NV, MAXT) hipLaunchKernelGGL((k_norm_gate_bwd<XT, BT, L, NV, MAXT, MANY>), g, t, lds, s, a)
-  MGN_NG_PLAN(MGN_NG_BWD);
+  if (p.lpr == 16)
+    MGN_NG_BWD(16, 1, 256);
+  else if (p.lpr == 32)
+    MGN_NG_BWD(32, 1, 256);
+  else if (p.lpr == 64)
+    MGN_NG_BWD(64, 1, 256);
+  else if (p.vpt == 8 && p.threads <= 512)
+    MGN_NG_BWD(0, 1, 512);
+  else if (p.vpt == 8)
+    MGN_NG_BWD(0, 1, 640);
+  else if (p.threads <= 512)
+    MGN_NG_BWD(0, 2, 512);
+  else
+    MGN_NG_BWD(0, 2, 1024);
 }
 template <typename XT, typename BT>
 void launch_bwd(const NormGate& a, const NormPlan& p, hipStream_t s) {

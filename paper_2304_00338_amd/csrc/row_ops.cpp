@@ -150,7 +150,7 @@ int mgn_matmul8(const mgn_mat8* a, const mgn_mat8* b, const mgn_epilogue* ep, in
   if (a->cols != b->cols)
     return fail(MGN_ERR_SHAPE, "%s: a has %lld columns, b %lld", who, (long long)a->cols, (long long)b->cols);
   if (!is_row_type(c_type)) return fail(MGN_ERR_ARG, "%s: unknown type %d of c", who, c_type);
-  Matmul8 m = {*a, *b, {}, c_type, c, ldc, (float*)ws, ws_bytes};
+  Matmul8 m = {*a, *b, {}, c_type, c, ldc, (float*)ws};
   if (ep) m.ep = *ep;
   if (m.ep.act < MGN_ACT_NONE || m.ep.act > MGN_ACT_RELU_GRAD) return fail(MGN_ERR_ARG, "%s: unknown act %d", who, m.ep.act);
   if (a->rows == 0 || b->rows == 0) return MGN_OK;

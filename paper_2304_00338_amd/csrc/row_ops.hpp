@@ -41,7 +41,6 @@ struct Matmul8 {
   void* c;
   int64_t ldc;
   float* part;  // workspace
-  size_t part_bytes;
 };
 hipError_t launch_matmul8(const Matmul8& a, hipStream_t s);
 // Workspace that launch_matmul8 splits sums in.
