@@ -2,7 +2,7 @@
 
 The host-side C++ (graph construction, partition, patch extraction and
 union, tile schedule, context planning in api.cpp, the no-alloc entry's
-host checks) is compiled with AddressSanitizer and UndefinedBehaviorSanitizer
+host checks, the row operators' argument checks) is compiled with AddressSanitizer and UndefinedBehaviorSanitizer
 on the host side only; the device objects of the normal build are linked in
 unchanged (no GPU code is sanitized).  The library is written to
 _build/sanitized/libmgn.so; run_host_tests() runs the CPU host-library tests
@@ -57,7 +57,7 @@ def build() -> str:
     return LIB
 
 
-def run_host_tests(tests=("tests/test_host_lib.py",)) -> int:
+def run_host_tests(tests=("tests/test_host_lib.py", "tests/test_row_ops_host.py")) -> int:
     """Run the CPU host-library tests against the sanitized library (the ASan
     runtime preloaded into a child Python); returns its exit status."""
     env = dict(os.environ)
