@@ -483,6 +483,8 @@ int mgn_matmul8(const mgn_mat8* a, const mgn_mat8* b, const mgn_epilogue* epilog
 #define MGN_NORM_NONE 0
 #define MGN_NORM_LAYER 1 /* (v - mean) / sqrt(var + eps) * gamma + beta, biased variance */
 #define MGN_NORM_RMS 2   /* v / sqrt(mean(v^2) + eps) * gamma + beta */
+/* Statistics are float32: where the squares of a row add up to 2^128 or more
+ * (values of about 10^18) its 1 / standard deviation is 0. */
 #define MGN_NORM_MAX_COLS 16384
 typedef struct mgn_norm_gate {
   int64_t rows;
@@ -497,8 +499,8 @@ typedef struct mgn_norm_gate {
   /* gate: float32 [n_gates][cols].  n_gates 0: no gate (1); 1: one for all
    * rows; rows: one for each row; any number with gate_ptr (int32 device
    * [n_gates + 1], ascending): gate g for rows [gate_ptr[g], gate_ptr[g + 1]);
-   * rows outside of [gate_ptr[0], gate_ptr[n_gates]) count for nothing, and
-   * their results are left as they were. */
+   * rows outside of [gate_ptr[0], gate_ptr[n_gates]) count for nothing, whatever
+   * they hold, and their results are left as they were. */
   const float* gate;
   const int32_t* gate_ptr;
   int64_t n_gates;

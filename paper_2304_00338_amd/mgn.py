@@ -630,8 +630,8 @@ def _at(t):
 
 class Mat8:
     """An mgn_mat8 of include/mgn.h: q, a float8_e4m3fn or float8_e5m2 tensor
-    [rows][ld >= cols], and its scales [ceil(cols / 128)][ceil(rows /
-    block_rows)] in float32."""
+    [rows][ld >= cols] whose bytes from cols to the next multiple of 16 are
+    zero, and its scales [ceil(cols / 128)][ceil(rows / block_rows)] in float32."""
     __slots__ = ("q", "scale", "rows", "cols", "block_rows", "struct")
 
     def __init__(self, q, scale, cols=None, block_rows=1):
@@ -815,7 +815,8 @@ def mgn_norm_gate_forward(x, b, post="none", pre="none", post_gamma=None, post_b
                           z=None, stream=None):
     """y = skip x + scale gate post(b), z = pre(y) (see include/mgn.h).
     Returns (y, z, stats): z None with pre="none", stats None without save.
-    y may be x, z may be b."""
+    y may be x, z may be b.  Rows outside of the groups of gate_ptr are not
+    written: a y or z that is not given holds any bits there."""
     if stream is not None:
         return _elsewhere(mgn_norm_gate_forward, dict(locals()))
     torch = _torch()
@@ -843,7 +844,8 @@ def mgn_norm_gate_backward(x, b, stats, dy, dz, post="none", pre="none", post_ga
     """Reverse of mgn_norm_gate_forward (see include/mgn.h) from its inputs and
     stats.  dy or dz None: zero.  Returns NormGateGrads; the gradients of the
     vectors and of the gate are those of the parameters that were given, new
-    tensors, or those of grads (a NormGateGrads of an earlier call) added to."""
+    tensors, or those of grads (a NormGateGrads of an earlier call) added to.
+    Rows of dx and db outside of the groups of gate_ptr are not written."""
     if stream is not None:
         return _elsewhere(mgn_norm_gate_backward, dict(locals()))
     torch = _torch()
