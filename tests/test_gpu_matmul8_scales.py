@@ -117,3 +117,18 @@ def test_rows_apart(dtype, bb):
         got = mgn.mgn_matmul8(mgn.mgn_quant8(x).rows, b, dtype=dtype)
         assert torch.equal(got[~other], want[~other])
         assert (got[1::11] == 0).all() and got[7::11].isnan().all()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("bb", [1, 128])
+def test_zero_negative_and_subnormal_scales(dtype, bb):
+    """Scales that mgn_quant8 does not write, but a Mat8 may hold."""
+    for m, n, k in SIZES + [LARGE]:
+        a, b = matrix(m, k, "e4m3", 1, False, [-3, 0, 5], 1), matrix(n, k, "e4m3", bb, False, [-2, 1, 100], 2)
+        flat = a.scale.view(-1)
+        flat[0::5] = 0.0
+        flat[1::5] *= -1
+        flat[2::5] = 3 * 2.0 ** -149
+        flat[3::5] = -(2.0 ** -130)
+        b.scale.view(-1)[0::3] *= -1
+        check(a, b, dtype)
