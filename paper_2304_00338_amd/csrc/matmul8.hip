@@ -187,11 +187,11 @@ __global__ void __launch_bounds__(256) k_matmul8_join(Job J) {
 // zero bytes.  The results go through the wave's own piece of LDS to be
 // stored as whole rows.
 //
-// Measured: 32,768 x 4096 x 4096 to bf16 563 us (1.95 PFLOP/s; the library's product
-// with one scale an operand reaches 2.5).  Without the loads 0.09 ms less, without
-// the scaled additions 0.05: a step's loads take longer than its 64 products a
-// SIMD, and the eight waves wait at its barrier.  434,558 x 128 x 384 to fp32 110 us
-// (3.6 TB/s), weight gradient 128 x 256 x 852,640 80 us (4.1 TB/s) and 8 to join.
+// Measured: 32,768 x 4096 x 4096 to bf16 567 to 591 us on three cards (1.9 PFLOP/s; the
+// library's product with one scale an operand reaches 2.5).  Without the loads 0.09 ms
+// less, without the scaled additions 0.05: a step's loads take longer than its 64
+// products a SIMD, and the eight waves wait at its barrier.  434,558 x 128 x 384 to fp32
+// 117 us (3.4 TB/s), weight gradient 128 x 256 x 852,640 86 us (3.8 TB/s) and 8 to join.
 template <bool WIDE, int FA, int FB, bool BROW, int WM, int WN, int TM, int TN>
 __global__ void __launch_bounds__(WM * WN * 64, 2) k_matmul8_tile(Job J) {
   constexpr int BM = WM * TM * 32, BN = WN * TN * 32, NWV = WM * WN;
@@ -478,9 +478,10 @@ __global__ void __launch_bounds__(WM * WN * 64, 2) k_matmul8_tile(Job J) {
 // instruction is 16x16x128: lane l holds row l & 15, bytes [32 (l >> 4), + 32);
 // result r is row 4 (l >> 4) + r of b, column l & 15 a row of a.
 //
-// Measured in a graph, weights from memory: 1 x 4096 x 4096 7.0 us, 1 x 4096 x 14336
-// 15.4 (3.8 TB/s), 23 x 10007 x 5000 25 (2.0 TB/s: every block reads a through L1,
-// twice the weights' bytes).
+// Measured in a graph over weights of more bytes than the caches hold: 1 x 4096 x 4096
+// 7.0 us, 1 x 4096 x 14336 16.3 (3.6 TB/s), 23 x 10007 x 5000 25 (2.0 TB/s: every block
+// reads a through L1, 1.4 times the weights' bytes); the last one over weights of 150 MB
+// in turn, which the last-level cache holds, 18.7.
 template <bool WIDE, int FB, int FA>
 __device__ __forceinline__ f32x4 mma16(i32x8 b, i32x8 a, uint32_t hb, uint32_t ha) {
   f32x4 c = {0.f, 0.f, 0.f, 0.f};
@@ -589,16 +590,16 @@ struct Plan {
   int splits;
 };
 
-// Which kernel, and into how many parts the sums are split; times in us of bf16
-// results (fp32 where marked).
-//  * Up to 32 rows of a the kernel for few rows, else tiles: 17 x 4096 x 4096 8.0
-//    (tiles 14.2), 32 x 1024 x 8192 9.3 (13.9), 24 x 10007 x 5000 19.0 (24.2), 32 x
-//    14336 x 4096 26.9 (24.6); 64 x 8192 x 8192 43.9 with four times 16 rows (27.9).
+// Which kernel, and into how many parts the sums are split; us a call in a stream of
+// calls, bf16 results (fp32 where marked).
+//  * Up to 32 rows of a the kernel for few rows, else tiles: 17 x 4096 x 4096 12.6
+//    (tiles 16.7), 32 x 1024 x 8192 16.9 (17.3), 24 x 10007 x 5000 19.1 (24.4), 32 x
+//    14336 x 4096 27.0 (24.7); 64 x 8192 x 8192 43.9 with four times 16 rows (27.9).
 //  * Tiles of 256 x 256 where they occupy three quarters of the CUs, need 8 steps
 //    or more and pad little; else of 128 x 128, two blocks a CU: 8192 x 4096 x 4096
-//    154 (small 167), 4096 x 3584 x 4096 72 (77), 16384 x 1000 x 5000 123 (158); but
-//    4096 x 2048 x 4096 66 (43), 100,000 x 512 x 512 75 (69), 434,558 x 128 x 384
-//    130 (76).  With a scale for each row of b, or for fp32 results, the large
+//    146 (small 176), 4096 x 3584 x 4096 70.6 (82.5), 16384 x 1000 x 5000 110 (154);
+//    but 4096 x 2048 x 4096 66.9 (46.0), 100,000 x 512 x 512 77.0 (72.4), 434,558 x
+//    128 x 384 130 (80).  With a scale for each row of b, or for fp32 results, the large
 //    tiles spill.
 //  * Sums split so that two blocks a CU are busy: 128 x 256 x 852,640 to fp32 110
 //    (one block 119, four 121), 64 x 8192 x 8192 27.9 (35.7, 36.6).  For few rows one

@@ -10,10 +10,11 @@
 // column sums of the vectors' gradients; a block's sums are added over its
 // walkers, and the blocks' in a second launch, always in the same order.
 //
-// Measured, forward and reverse: 307,981 x 128 fp32 / bf16, 32 gates 122 and 182 us
-// (3.9 TB/s each), 16,384 x 5001 bf16 185 and 228 us (3.5 and 4.3), 16,384 x 4096 140
-// and 171 (3.8 and 4.7), one row of 4096 8.5 us.  Bound by memory at narrow rows; a
-// row of a whole block adds the barriers of its two to four sums.
+// Measured, forward and reverse: 307,981 x 128 fp32 / bf16, 32 gates 130 and 189 us
+// (3.6 and 3.8 TB/s), 16,384 x 5001 bf16 192 and 234 us (3.4 and 4.2), with 32 gates 276
+// and 284, 307,981 x 128 with a gate for each row 288 and 575, one row of 4096 8.8
+// us.  Bound by memory at narrow rows; a row of a whole block adds the barriers of its
+// two to four sums, another gate than the row's before the loads of its vectors.
 #include "dev_common.hpp"
 #include "row_io.hpp"
 #include "row_ops.hpp"
@@ -557,10 +558,16 @@ using namespace dev;
 
 NormPlan norm_plan(int64_t rows, int cols, bool backward) {
   NormPlan p;
-  // in the reverse two runs a lane from 5121 columns on: blocks of more than 640
-  // threads have 128 registers, and with one run spilled (16,384 x 8192 bf16: 652
-  // us; two runs 305).  Above 8192 columns these are blocks of 1024 that do spill:
-  // 8192 x 16384 takes 1.75 ms.
+  // In the reverse two runs a lane from 5121 columns on.  With one run blocks have up
+  // to 1024 threads, whose 128 registers do not hold it: forward and reverse of 16,384
+  // rows of 8192 bf16 924 us (two runs 607), of 7168 856 (544).  Blocks of 704 and 768
+  // threads would still have 168: compiled for 768, one run takes 455 us at 6144
+  // columns (two 497) and 421 at 5632 (484).
+  // What spills: with gates of rows or groups one run from 4097 columns on 6 to 11
+  // registers, two runs 37 to 86, each for three of the four pairs of types (reverse of
+  // 16,384 x 8192 bf16 with 32 gates 583 us, without 354); above 8192 columns, in blocks of
+  // 1024, the reverse 173 to 412 and the forward 84 to 102 (8192 x 16,384 1.69 ms and
+  // 390 us).
   p.vpt = cols <= (backward ? 5120 : 8192) ? 8 : 16;
   const int lanes = (cols + p.vpt - 1) / p.vpt;
   p.lpr = lanes <= 16 ? 16 : lanes <= 32 ? 32 : lanes <= 64 ? 64 : 0;
