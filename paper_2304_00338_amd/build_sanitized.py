@@ -2,9 +2,10 @@
 
 The host-side C++ (graph construction, partition, patch extraction and
 union, tile schedule, context planning in api.cpp, the no-alloc entry's
-host checks, the row operators' argument checks) is compiled with AddressSanitizer and UndefinedBehaviorSanitizer
-on the host side only; the device objects of the normal build are linked in
-unchanged (no GPU code is sanitized).  The library is written to
+host checks, the row operators' argument checks) is compiled with
+AddressSanitizer and UndefinedBehaviorSanitizer on the host side only; the
+device objects of the normal build are linked in unchanged (no GPU code is
+sanitized).  The library is written to
 _build/sanitized/libmgn.so; run_host_tests() runs the CPU host-library tests
 against it in a child process with the ASan runtime preloaded.
 """
