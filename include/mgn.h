@@ -13,8 +13,10 @@
  *   - one explicit integration step y' = y + sum_i b_i K_i with
  *     K_i = MGN(stage i), i.e. the update rule of Sec. 2.1 and the Heun forms
  *     of Sec. 2.3 / App. A (equation heun) generalised to a Butcher tableau;
- *   - operators on rows for layers beside these: block-scaled 8-bit products and
- *     the step norm, gate, residual, norm, with their gradients.
+ *   - operators on rows for layers beside these: products of 8-bit and 4-bit
+ *     matrices with block scales, the step norm, gate, residual, norm, and the group
+ *     norm with an activation, with their gradients; the norm of many gradients and
+ *     its clipping.
  *
  * Conventions
  *   - Every function returns an int status: MGN_OK (0) or a negative MGN_ERR_*.
@@ -396,8 +398,9 @@ int mgn_pec_step(mgn_ctx* ctx, const mgn_dgraph* g, const float* params,
 /* ---- row operators ------------------------------------------------------ */
 /* Building blocks for layers that a model adds beside the MGN processor's own
  * fused MLPs (wider MLPs on the latents, steps between the blocks of a
- * residual stream): an 8-bit quantiser, the product of block-scaled 8-bit
- * matrices, and the step norm -> gate -> residual -> norm with its reverse.
+ * residual stream): an 8-bit and a 4-bit quantiser, the products of such
+ * matrices, the step norm -> gate -> residual -> norm and the group norm with their
+ * reverses, and the clipping of gradients by their norm.
  * They need no context; like the calls above they are asynchronous on
  * `stream`, run on the current device, allocate nothing and have fixed
  * summation orders (results are bitwise reproducible).  Row tensors are
@@ -537,6 +540,128 @@ int mgn_norm_gate_backward(const mgn_norm_gate* op, mgn_rows x, mgn_rows b,
                            const float* stats, mgn_rows dy, mgn_rows dz, mgn_rows dx,
                            mgn_rows db, const mgn_norm_gate_grads* grads, void* workspace,
                            size_t ws_bytes, void* stream);
+
+/* A matrix of 4-bit numbers (sign, 2 exponent bits, 1 mantissa bit: 0, 0.5, 1, 1.5, 2,
+ * 3, 4, 6) with one power of two for each 32 columns of a row.  Value (r, c) is the
+ * number in byte q[r ld + c / 2] (the lower half byte for even c) times 2^(s - 127), s =
+ * scale[((c / 128) rows + r) 4 + c / 32 % 4]; s = 255 makes all 32 NaN.  q is 16-byte
+ * aligned, ld a multiple of 16, and the numbers from cols to the next multiple of 32 are
+ * zero, as are the scales behind the last one of the columns (mgn_quant4 writes them
+ * so); scale is 4-byte aligned and has 4 rows ceil(cols / 128) bytes. */
+typedef struct mgn_mat4 {
+  const uint8_t* q;
+  const uint8_t* scale;
+  int64_t rows, cols, ld; /* ld in bytes */
+} mgn_mat4;
+
+/* Quantises x [rows][cols] (MGN_FP32 or MGN_BF16).  The scale X of 32 columns is the
+ * power of two that puts their largest magnitude in [3.5, 7) (4 or 6 to the nearest
+ * number), from 2^-127 on (for smaller ones, and for zeros, 2^-127); a value becomes the
+ * number nearest x / X, ties to the even mantissa.  Where one of the 32 is an infinity or
+ * a NaN, s is 255 and the numbers are zero.
+ * q, scale: x as an mgn_mat4 (NULL: not wanted).  qt, scale_t: the transpose
+ * [cols][rows], whose scales are of 32 rows of one column of x (NULL: not wanted).
+ * colsum (nullable): [cols] sums of x over its rows (the gradient of a bias), added to
+ * what is there with accumulate != 0; the workspace is needed for it only.
+ * Errors: ARG, SHAPE (2^31 rows or columns, or rows x cols of 2^42), WORKSPACE,
+ * DEVICE. */
+int mgn_quant4_workspace(int64_t rows, int64_t cols, size_t* ws_bytes);
+int mgn_quant4(const void* x, int32_t x_type, int64_t rows, int64_t cols, int64_t ldx, uint8_t* q,
+               int64_t ldq, uint8_t* scale, uint8_t* qt, int64_t ldqt, uint8_t* scale_t,
+               float* colsum, int32_t accumulate, void* workspace, size_t ws_bytes, void* stream);
+
+/* The values of a as rows of y_type (MGN_FP32, MGN_BF16), [a->rows][ldy].  Exact in both
+ * (but for 6 times 2^127 and 4 times 2^127, which are infinities).
+ * Errors: ARG, SHAPE, DEVICE. */
+int mgn_dequant4(const mgn_mat4* a, int32_t y_type, void* y, int64_t ldy, void* stream);
+
+/* c[m][n] = act(sum_k a[m][k] b[n][k] + bias[n]) as mgn_matmul8 with its epilogue, of
+ * 4-bit matrices.  Products are exact and summed in float32 (32 products, all of one
+ * scale, without loss).
+ * Errors: ARG, SHAPE (a->cols != b->cols, 2^31 rows or columns, or c of about 2^24
+ * tiles of 128 x 128), WORKSPACE, DEVICE. */
+int mgn_matmul4_workspace(int64_t a_rows, int64_t b_rows, int64_t cols, size_t* ws_bytes);
+int mgn_matmul4(const mgn_mat4* a, const mgn_mat4* b, const mgn_epilogue* epilogue,
+                int32_t c_type, void* c, int64_t ldc, void* workspace, size_t ws_bytes,
+                void* stream);
+
+/* Group norm with an activation.  x [rows][cols], rows being nodes or pixels and columns
+ * channels; a sample is a run of rows, a group cols / groups neighbouring channels:
+ *   xhat = (x - mean) / sqrt(var + eps) over a sample's rows and a group's channels
+ *   (biased variance),  z = gamma xhat + beta,  y = act(z).
+ * act is MGN_ACT_NONE, MGN_ACT_RELU or */
+#define MGN_ACT_SILU 3 /* z / (1 + exp(-z)) (mgn_group_norm only) */
+typedef struct mgn_group_norm {
+  int64_t rows;
+  int32_t cols;   /* 1 .. MGN_NORM_MAX_COLS */
+  int32_t groups; /* divides cols */
+  int32_t type;   /* of x, y, dy, dx: MGN_FP32 or MGN_BF16 */
+  int32_t act;
+  float eps;      /* > 0 */
+  const float *gamma, *beta; /* float32 [cols]; NULL: 1, 0 */
+  /* sample s has rows [sample_ptr[s], sample_ptr[s + 1]) (int32 device [n_samples + 1],
+   * ascending; rows outside of all count for nothing, whatever they hold, and their
+   * results are left as they were), or with sample_ptr NULL rows / n_samples rows each
+   * (n_samples divides rows). */
+  const int32_t* sample_ptr;
+  int64_t n_samples;
+} mgn_group_norm;
+
+/* y from x; stats (nullable: inference) [n_samples][groups][2] float32 keeps mean and
+ * 1 / sqrt(var + eps) for the reverse (of a sample without rows: 0 and 1 / sqrt(eps)).
+ * Sums are of 64 bits.  y may be x (with the same ld).
+ * Errors: ARG, SHAPE, WORKSPACE, DEVICE. */
+int mgn_group_norm_workspace(const mgn_group_norm* op, int32_t backward, size_t* ws_bytes);
+int mgn_group_norm_forward(const mgn_group_norm* op, mgn_rows x, mgn_rows y, float* stats,
+                           void* workspace, size_t ws_bytes, void* stream);
+
+/* Reverse: from x, the forward's stats and the gradient dy of y the gradient dx, and
+ * (each nullable, float32 [cols], added to what is there with accumulate != 0) dgamma
+ * and dbeta, summed over all samples.  dx may be dy or x (with the same ld).
+ * Errors: ARG, SHAPE, WORKSPACE, DEVICE. */
+int mgn_group_norm_backward(const mgn_group_norm* op, mgn_rows x, const float* stats, mgn_rows dy,
+                            mgn_rows dx, float* dgamma, float* dbeta, int32_t accumulate,
+                            void* workspace, size_t ws_bytes, void* stream);
+
+/* Clipping of gradients by the norm over all of them (before mgn_adam_step).  The
+ * gradients are a list of n tensors of any sizes, each a contiguous run of `n` elements
+ * of in_type (MGN_FP32 or MGN_BF16), with a place of as many elements of out_type for
+ * the clipped ones, which may be the gradient itself (same type). */
+typedef struct mgn_tensor {
+  const void* in;
+  void* out; /* NULL: the list is for norms only */
+  int64_t n;
+  int32_t in_type, out_type;
+} mgn_tensor;
+
+/* The list cut into pieces of at most mgn_grad_piece() elements, as the kernels take it:
+ * fills pieces (host, room for *n_pieces of them; NULL: only the count is given back).
+ * The caller copies them to the device once and keeps them while the tensors stay where
+ * they are.  A place may not overlap another place, or another tensor's gradient.
+ * Errors: ARG, SHAPE (2^31 pieces). */
+typedef struct mgn_piece {
+  const void* in;
+  void* out;
+  int32_t n;
+  int32_t types; /* in_type + 2 out_type */
+} mgn_piece;
+int32_t mgn_grad_piece(void);
+int mgn_grad_pieces(const mgn_tensor* tensors, int64_t n, mgn_piece* pieces, int64_t* n_pieces);
+
+/* norm (one device float) = sqrt(sum of squares of all elements), summed in 64 bits, so that
+ * it is right at any magnitude; more than float32 holds gives infinity.  pieces: on the
+ * device.  Errors: ARG, WORKSPACE, DEVICE. */
+int mgn_grad_norm_workspace(int64_t n_pieces, size_t* ws_bytes);
+int mgn_grad_norm(const mgn_piece* pieces, int64_t n_pieces, float* norm, void* workspace,
+                  size_t ws_bytes, void* stream);
+
+/* out = in * min(1, max_norm / norm), rounded once.  given == 0: norm is formed first, as by
+ * mgn_grad_norm (and the factor from its 64 bits), and written; given != 0: norm is read
+ * (say after a sum over processes).  A norm that is no finite number (of the given float,
+ * or of the 64-bit sum) clips nothing: out = in, and the caller sees it in norm.
+ * max_norm >= 0, may be infinite.  Errors: ARG, WORKSPACE, DEVICE. */
+int mgn_grad_clip(const mgn_piece* pieces, int64_t n_pieces, double max_norm, float* norm,
+                  int32_t given, void* workspace, size_t ws_bytes, void* stream);
 
 /* Per-kernel timing for benchmarks.  While enabled, every kernel launch of
  * the context is bracketed by two HIP events recorded on the caller's stream.

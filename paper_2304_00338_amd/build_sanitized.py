@@ -58,7 +58,7 @@ def build() -> str:
     return LIB
 
 
-def run_host_tests(tests=("tests/test_host_lib.py", "tests/test_row_ops_host.py")) -> int:
+def run_host_tests(tests=("tests/test_host_lib.py", "tests/test_row_ops_host.py", "tests/test_more_row_ops_host.py")) -> int:
     """Run the CPU host-library tests against the sanitized library (the ASan
     runtime preloaded into a child Python); returns its exit status."""
     env = dict(os.environ)

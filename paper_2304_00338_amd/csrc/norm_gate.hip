@@ -677,20 +677,24 @@ hipError_t launch_norm_gate_backward(const NormGate& in, hipStream_t s) {
   return hipSuccess;
 }
 
-hipError_t launch_column_reduce(float* part, int64_t nb, int64_t cols, float* out, int32_t accumulate, hipStream_t s) {
-  dim3 g = grid_of(ceil_div(cols, kSumCols));
-  int64_t stride = cols;
+hipError_t launch_column_reduce(float* part, int64_t nb, int64_t cols, float* const* out, int n, int32_t accumulate,
+                                hipStream_t s) {
+  const int64_t all = cols * n;
+  int64_t stride = all;
   if (nb > 1024) {  // 6662 x 128: 10.2 us in two steps, 16.4 in one, whose 8 blocks wait for memory
+    dim3 g = grid_of(ceil_div(all, kSumCols));
     const int64_t per = std::max<int64_t>(256, ceil_div(nb, 32768));
     g.z = (unsigned)ceil_div(nb, per);
-    hipLaunchKernelGGL(k_column_fold, g, dim3(1024), 0, s, part, nb, cols, per);
+    hipLaunchKernelGGL(k_column_fold, g, dim3(1024), 0, s, part, nb, all, per);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     nb = g.z;
-    stride = per * cols;
-    g.z = 1;
+    stride = per * all;
   }
-  const ColumnSums c = {part, nb, stride, cols, {out, nullptr, nullptr, nullptr, nullptr}, accumulate};
+  ColumnSums c = {part, nb, stride, cols, {}, accumulate};
+  for (int i = 0; i < n; ++i) c.out[i] = out[i];
+  dim3 g = grid_of(ceil_div(cols, kSumCols));
+  g.z = (unsigned)n;
   hipLaunchKernelGGL(k_column_sums, g, dim3(1024), 0, s, c);
   return hipGetLastError();
 }

@@ -1,0 +1,251 @@
+// 4-bit quantisation with one power of two for each 32 columns of a row, and the
+// way back (see include/mgn.h).
+//
+// With u the bits of the largest magnitude, X = 2^(b - 127), b = max(0, ((u + 2^21) >>
+// 23) - 2): the exponent of u less 2, one more where its mantissa is 1.75 or more. x / X
+// is exact, and the conversion instruction, which takes X as a float's exponent, rounds
+// it to the nearest number, ties to even (checked for every bf16 below 7 X and for the
+// float neighbours of the middles, at X from 2^-127 to 2^126).
+//
+// Bound by memory: an element is read once (2 or 4 bytes) and written as half a
+// byte a copy.  k_quant4_rows (rows only) gives 16 lanes to 128 columns, four to a
+// block; k_quant4_tile takes 128 x 128, a thread 8 rows x 8 columns, so that a wave
+// has the 32 rows of a column's block and the column maxima stay in it; the
+// transpose and the scales go through LDS to be stored in whole pieces.
+#include "dev_common.hpp"
+#include "row_io.hpp"
+#include "row_ops.hpp"
+
+namespace mgn {
+namespace dev {
+
+constexpr int kChunk4 = 4;  // blocks of 128 columns that a block of k_quant4_rows takes from its 16 rows
+
+// Magnitudes as bits: their order is that of the values, a NaN is the largest.
+__device__ __forceinline__ uint32_t magnitude(float f) { return __float_as_uint(f) & 0x7fffffffu; }
+template <int CTRL>
+__device__ __forceinline__ uint32_t dpp_u(uint32_t v) {
+  return (uint32_t)__builtin_amdgcn_mov_dpp((int)v, CTRL, 0xf, 0xf, false);
+}
+// The largest of the four lanes 4 i .. 4 i + 3.
+__device__ __forceinline__ uint32_t max_quad(uint32_t v) {
+  v = max(v, dpp_u<0xb1>(v));  // lanes 1 0 3 2
+  return max(v, dpp_u<0x4e>(v));  // lanes 2 3 0 1
+}
+// The largest of the lanes l, l ^ 16, l ^ 32, l ^ 48.
+__device__ __forceinline__ uint32_t max_rows(uint32_t v) {
+  const auto a = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+  const uint32_t u = max(a[0], a[1]);
+  const auto b = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  return max(b[0], b[1]);
+}
+
+// The scale's byte for a largest magnitude.
+__device__ __forceinline__ uint32_t scale4(uint32_t u) {
+  return u >= 0x7f800000u ? 255u : (uint32_t)max((int)((u + 0x200000u) >> 23) - 2, 0);
+}
+// 2^(b - 127) as a float.
+__device__ __forceinline__ float power(uint32_t b) { return __uint_as_float(max(b << 23, 0x400000u)); }
+
+// Eight numbers, the first in the lowest half byte.
+__device__ __forceinline__ uint32_t numbers4(const float (&v)[8], uint32_t b) {
+  const float s = power(b);
+  uint32_t w = 0;
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[0], v[1], s, 0);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[2], v[3], s, 1);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[4], v[5], s, 2);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[6], v[7], s, 3);
+  return b == 255u ? 0u : w;
+}
+
+template <typename XT>
+__global__ void __launch_bounds__(256) k_quant4_rows(Quant4 a) {
+  const int l = threadIdx.x & 15;
+  const int64_t cb = ceil_div(a.cols, 128), end = (a.cols + 31) & ~31LL;
+  const uint32_t chunks = (uint32_t)ceil_div(cb, (int64_t)kChunk4), block = blockIdx.y * (uint32_t)kGridRow + blockIdx.x,
+                 group = block / chunks;
+  const int64_t r = (int64_t)group * 16 + (threadIdx.x >> 4), k0 = (int64_t)(block - group * chunks) * kChunk4;
+  if (r >= a.rows) return;  // all 16 lanes of the row
+  Raw8<XT> raw[kChunk4];
+#pragma unroll
+  for (int k = 0; k < kChunk4; ++k) {
+    const int64_t c = (k0 + k) * 128 + l * 8;
+    raw[k] = load8((const XT*)a.x + r * a.ldx + c, (int)min(a.cols - c, (int64_t)8));
+  }
+#pragma unroll
+  for (int k = 0; k < kChunk4; ++k) {
+    const int64_t c = (k0 + k) * 128 + l * 8;
+    if (k0 + k >= cb) break;
+    float v[8];
+    uint32_t m = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      v[e] = raw[k].get(e);
+      m = max(m, magnitude(v[e]));
+    }
+    const uint32_t b = scale4(max_quad(m));
+    if (c < end) *(uint32_t*)(a.q + r * a.ldq + c / 2) = numbers4(v, b);
+    // the four bytes meet in lane 0
+    uint32_t w = b << (8 * (l >> 2));
+    w |= dpp_u<0x128>(w);
+    w |= dpp_u<0x124>(w);
+    if (l == 0) ((uint32_t*)a.scale)[(k0 + k) * a.rows + r] = w;
+  }
+}
+
+constexpr int kCol4Ld = 68;  // bytes of a column of 128 rows in LDS
+
+template <typename XT, bool SUMS>
+__global__ void __launch_bounds__(256) k_quant4_tile(Quant4 a) {
+  __shared__ __align__(16) uint8_t turned[128 * kCol4Ld];
+  __shared__ __align__(16) uint8_t cscale[128][4];
+  __shared__ uint32_t rscale[128];
+  __shared__ float csum[SUMS ? 4 : 1][128];
+  const int l = threadIdx.x & 15, g = threadIdx.x >> 4, w = threadIdx.x >> 6;
+  const int64_t cbs = ceil_div(a.cols, 128), rbs = ceil_div(a.rows, 128);
+  const uint32_t block = blockIdx.y * (uint32_t)kGridRow + blockIdx.x;
+  const int64_t rb = block / (uint32_t)cbs, cb = block - rb * cbs;
+  if (rb >= rbs) return;  // behind the last block
+  const int64_t up_cols = (a.cols + 31) & ~31LL, up_rows = (a.rows + 31) & ~31LL;
+  const int64_t c0 = cb * 128 + l * 8, r0 = rb * 128 + g * 8;
+  const int n = (int)min(max(a.cols - c0, (int64_t)0), (int64_t)8);
+  const bool turn = a.qt != nullptr;
+  Raw8<XT> raw[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int64_t r = min(r0 + i, a.rows - 1);
+    raw[i] = load8((const XT*)a.x + r * a.ldx + c0, r0 + i < a.rows ? n : 0);
+  }
+  uint32_t cm[8] = {};
+  float cs[8] = {};
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    float v[8];
+    uint32_t m = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      v[e] = raw[i].get(e);
+      const uint32_t u = magnitude(v[e]);
+      m = max(m, u);
+      cm[e] = max(cm[e], u);
+      if (SUMS) cs[e] += v[e];
+    }
+    if (a.q != nullptr) {
+      const uint32_t b = scale4(max_quad(m));
+      if (r0 + i < a.rows && c0 < up_cols) *(uint32_t*)(a.q + (r0 + i) * a.ldq + c0 / 2) = numbers4(v, b);
+      uint32_t s = b << (8 * (l >> 2));
+      s |= dpp_u<0x128>(s);
+      s |= dpp_u<0x124>(s);
+      if (l == 0) rscale[g * 8 + i] = s;
+    }
+  }
+  if (turn) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const uint32_t b = scale4(max_rows(cm[e]));
+      float v[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = raw[i].get(e);
+      *(uint32_t*)(turned + (l * 8 + e) * kCol4Ld + g * 4) = numbers4(v, b);
+      if (g % 4 == 0) cscale[l * 8 + e][w] = (uint8_t)b;
+    }
+  }
+  if constexpr (SUMS) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) cs[e] = sum_q(cs[e]);
+    if (g % 4 == 0) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) csum[w][l * 8 + e] = cs[e];
+    }
+  }
+  __syncthreads();
+  if (turn) {
+    // 32 bytes of a column a thread
+    const int64_t c = cb * 128 + (threadIdx.x >> 1), r = rb * 128 + (threadIdx.x & 1) * 64;
+    if (c < a.cols) {
+      const uint32_t* from = (const uint32_t*)(turned + (threadIdx.x >> 1) * kCol4Ld + (threadIdx.x & 1) * 32);
+      uint8_t* to = a.qt + c * a.ldqt + r / 2;
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+        if (r + 32 * k < up_rows) *(uint4*)(to + 16 * k) = uint4{from[4 * k], from[4 * k + 1], from[4 * k + 2], from[4 * k + 3]};
+    }
+  }
+  const int t = threadIdx.x & 127;
+  if (threadIdx.x < 128) {
+    if (a.q != nullptr && rb * 128 + t < a.rows) ((uint32_t*)a.scale)[cb * a.rows + rb * 128 + t] = rscale[t];
+  } else if (cb * 128 + t < a.cols) {
+    if (turn) ((uint32_t*)a.scale_t)[rb * a.cols + cb * 128 + t] = *(const uint32_t*)cscale[t];
+    if constexpr (SUMS) a.part[rb * a.cols + cb * 128 + t] = ((csum[0][t] + csum[1][t]) + csum[2][t]) + csum[3][t];
+  }
+}
+
+// Back: 16 lanes to 128 columns, 4 blocks of 128 of a row a thread.
+template <typename YT>
+__global__ void __launch_bounds__(256) k_dequant4(Dequant4 a) {
+  typedef float f32x2 __attribute__((ext_vector_type(2)));
+  const int l = threadIdx.x & 15;
+  const int64_t cb = ceil_div(a.a.cols, 128), end = (a.a.cols + 31) & ~31LL;
+  const uint32_t chunks = (uint32_t)ceil_div(cb, (int64_t)kChunk4), block = blockIdx.y * (uint32_t)kGridRow + blockIdx.x,
+                 group = block / chunks;
+  const int64_t r = (int64_t)group * 16 + (threadIdx.x >> 4), k0 = (int64_t)(block - group * chunks) * kChunk4;
+  if (r >= a.a.rows) return;
+  uint32_t w[kChunk4];
+  uint8_t s[kChunk4];
+#pragma unroll
+  for (int k = 0; k < kChunk4; ++k) {
+    const int64_t c = (k0 + k) * 128 + l * 8;
+    const bool in = c < end;
+    w[k] = in ? *(const uint32_t*)(a.a.q + r * a.a.ld + c / 2) : 0;
+    s[k] = in ? a.a.scale[((k0 + k) * a.a.rows + r) * 4 + (l >> 2)] : 0;
+  }
+#pragma unroll
+  for (int k = 0; k < kChunk4; ++k) {
+    const int64_t c = (k0 + k) * 128 + l * 8;
+    const float x = power(s[k]);
+    const f32x2 v[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[k], x, 0), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[k], x, 1),
+                        __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[k], x, 2), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[k], x, 3)};
+    float f[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f[e] = s[k] == 255 ? __builtin_nanf("") : v[e >> 1][e & 1];
+    const int n = (int)min(a.a.cols - c, (int64_t)8);
+    if (n > 0) store8((YT*)a.y + r * a.ldy + c, 0, n, f);
+  }
+}
+
+}  // namespace dev
+
+using namespace dev;
+
+hipError_t launch_quant4(const Quant4& a, hipStream_t s) {
+  const int64_t cbs = ceil_div(a.cols, 128), rbs = ceil_div(a.rows, 128);
+#define MGN_Q4(n, K, ...)                                                                        \
+  do {                                                                                           \
+    if (a.x_type == MGN_FP32)                                                                    \
+      hipLaunchKernelGGL((K<float __VA_ARGS__>), grid_of(n), dim3(256), 0, s, a);                \
+    else                                                                                         \
+      hipLaunchKernelGGL((K<bf16 __VA_ARGS__>), grid_of(n), dim3(256), 0, s, a);                 \
+  } while (0)
+  if (a.rows > 0) {
+    if (!a.qt && !a.colsum)
+      MGN_Q4(ceil_div(a.rows, 16) * ceil_div(cbs, kChunk4), k_quant4_rows, );
+    else if (a.colsum)
+      MGN_Q4(rbs * cbs, k_quant4_tile, , true);
+    else
+      MGN_Q4(rbs * cbs, k_quant4_tile, , false);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  if (a.colsum) return launch_column_reduce(a.part, rbs, a.cols, &a.colsum, 1, a.accumulate, s);
+  return hipSuccess;
+}
+
+hipError_t launch_dequant4(const Dequant4& a, hipStream_t s) {
+  const dim3 g = grid_of(ceil_div(a.a.rows, 16) * ceil_div(ceil_div(a.a.cols, 128), kChunk4));
+  if (a.y_type == MGN_FP32)
+    hipLaunchKernelGGL((k_dequant4<float>), g, dim3(256), 0, s, a);
+  else
+    hipLaunchKernelGGL((k_dequant4<bf16>), g, dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
+}  // namespace mgn

@@ -362,7 +362,7 @@ hipError_t launch_quant8(const Quant8& a, hipStream_t s) {
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  if (a.colsum) return launch_column_reduce(a.part, rbs, a.cols, a.colsum, a.accumulate, s);
+  if (a.colsum) return launch_column_reduce(a.part, rbs, a.cols, &a.colsum, 1, a.accumulate, s);
   return hipSuccess;
 }
 

@@ -24,6 +24,7 @@ FP32, BF16, E4M3, E5M2 = 0, 1, 2, 3
 FORMATS = {"e4m3": E4M3, "e5m2": E5M2}
 ACTS = {"none": 0, "relu": 1, "relu_grad": 2}
 NORMS = {"none": 0, "layer": 1, "rms": 2}
+GROUP_ACTS = {"none": 0, "relu": 1, "silu": 3}
 NORM_MAX_COLS = 16384  # MGN_NORM_MAX_COLS of include/mgn.h
 EULER, HEUN2, MIDPOINT, HEUN3, RK4, RALSTON2, RALSTON3 = 0, 1, 2, 3, 4, 5, 6
 SCHEMES = {"euler": EULER, "heun2": HEUN2, "midpoint": MIDPOINT, "heun3": HEUN3, "rk4": RK4,
@@ -90,6 +91,25 @@ class CNormGateGrads(C.Structure):
                 ("pre_beta", C.c_void_p), ("gate", C.c_void_p), ("accumulate", C.c_int32)]
 
 
+class CMat4(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("scale", C.c_void_p), ("rows", C.c_int64), ("cols", C.c_int64), ("ld", C.c_int64)]
+
+
+class CGroupNorm(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("cols", C.c_int32), ("groups", C.c_int32), ("type", C.c_int32), ("act", C.c_int32),
+                ("eps", C.c_float), ("gamma", C.c_void_p), ("beta", C.c_void_p), ("sample_ptr", C.c_void_p),
+                ("n_samples", C.c_int64)]
+
+
+class CTensor(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("out", C.c_void_p), ("n", C.c_int64), ("in_type", C.c_int32),
+                ("out_type", C.c_int32)]
+
+
+class CPiece(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("out", C.c_void_p), ("n", C.c_int32), ("types", C.c_int32)]
+
+
 _lib = None
 
 EXPORTS = [
@@ -100,6 +120,9 @@ EXPORTS = [
     "mgn_pec_step", "mgn_patch_step", "mgn_adam_lr", "mgn_adam_step", "mgn_train_step", "mgn_scheme_stages", "mgn_version", "mgn_last_error", "mgn_profile_enable",
     "mgn_profile_collect", "mgn_quant8_workspace", "mgn_quant8", "mgn_matmul8_workspace", "mgn_matmul8",
     "mgn_norm_gate_forward", "mgn_norm_gate_workspace", "mgn_norm_gate_backward",
+    "mgn_quant4_workspace", "mgn_quant4", "mgn_dequant4", "mgn_matmul4_workspace", "mgn_matmul4",
+    "mgn_group_norm_workspace", "mgn_group_norm_forward", "mgn_group_norm_backward", "mgn_grad_piece",
+    "mgn_grad_pieces", "mgn_grad_norm_workspace", "mgn_grad_norm", "mgn_grad_clip",
 ]
 
 
@@ -151,6 +174,19 @@ def lib():
         "mgn_norm_gate_workspace": (C.c_int, [i64, i32, P(C.c_size_t)]),
         "mgn_norm_gate_backward": (C.c_int, [P(CNormGate), Rows, Rows, vp, Rows, Rows, Rows, Rows, P(CNormGateGrads),
                                              vp, C.c_size_t, vp]),
+        "mgn_quant4_workspace": (C.c_int, [i64, i64, P(C.c_size_t)]),
+        "mgn_quant4": (C.c_int, [vp, i32, i64, i64, i64, vp, i64, vp, vp, i64, vp, vp, i32, vp, C.c_size_t, vp]),
+        "mgn_dequant4": (C.c_int, [P(CMat4), i32, vp, i64, vp]),
+        "mgn_matmul4_workspace": (C.c_int, [i64, i64, i64, P(C.c_size_t)]),
+        "mgn_matmul4": (C.c_int, [P(CMat4), P(CMat4), P(Epilogue), i32, vp, i64, vp, C.c_size_t, vp]),
+        "mgn_group_norm_workspace": (C.c_int, [P(CGroupNorm), i32, P(C.c_size_t)]),
+        "mgn_group_norm_forward": (C.c_int, [P(CGroupNorm), Rows, Rows, vp, vp, C.c_size_t, vp]),
+        "mgn_group_norm_backward": (C.c_int, [P(CGroupNorm), Rows, vp, Rows, Rows, vp, vp, i32, vp, C.c_size_t, vp]),
+        "mgn_grad_piece": (i32, []),
+        "mgn_grad_pieces": (C.c_int, [P(CTensor), i64, P(CPiece), P(i64)]),
+        "mgn_grad_norm_workspace": (C.c_int, [i64, P(C.c_size_t)]),
+        "mgn_grad_norm": (C.c_int, [vp, i64, vp, vp, C.c_size_t, vp]),
+        "mgn_grad_clip": (C.c_int, [vp, i64, C.c_double, vp, i32, vp, C.c_size_t, vp]),
     }
     for name, (res, args) in sig.items():
         f = getattr(L, name)
@@ -606,7 +642,8 @@ def _elsewhere(fn, args):
     stream = args.pop("stream")
     given = []
     for v in args.values():
-        given += [v] if isinstance(v, torch.Tensor) else [v.q, v.scale] if isinstance(v, Mat8) else \
+        given += [v] if isinstance(v, torch.Tensor) else [v.q, v.scale] if isinstance(v, (Mat8, Mat4)) else \
+            v.tensors() if isinstance(v, TensorList) else \
             [t for t in v if isinstance(t, torch.Tensor)] if isinstance(v, tuple) else []
     for t in given:
         if t.is_cuda and t.device != stream.device:
@@ -880,6 +917,312 @@ def mgn_norm_gate_backward(x, b, stats, dy, dz, post="none", pre="none", post_ga
     _run(dev, lib().mgn_norm_gate_backward,
          (C.byref(op), xr, br, stats.data_ptr(), dyr, dzr, dxr, dbr, C.byref(cg), _at(ws), need.value))
     return NormGateGrads(dx, db, **out)
+
+
+class Mat4:
+    """An mgn_mat4 of include/mgn.h: q, a uint8 tensor [rows][ld] of 4-bit numbers,
+    two a byte, those from cols to the next multiple of 32 zero, and its scales
+    [ceil(cols / 128)][rows][4] in float8_e8m0fnu (or uint8), those behind the
+    last 32 columns zero bytes."""
+    __slots__ = ("q", "scale", "rows", "cols", "struct")
+
+    def __init__(self, q, scale, cols):
+        torch = _torch()
+        if not isinstance(q, torch.Tensor) or not q.is_cuda or q.dim() != 2 or q.dtype != torch.uint8:
+            raise MgnError(ERR_ARG, "q must be a two-dimensional uint8 device tensor")
+        rows, width = q.shape
+        cols = int(cols)
+        need = -(-cols // 32) * 16
+        ld = _row_ld(q, "q") if rows > 1 else -(-width // 16) * 16
+        if cols < 0 or (width < need and rows > 0):
+            raise MgnError(ERR_ARG, f"q has {width} bytes a row for {cols} columns: {need} are needed")
+        want = (-(-cols // 128), rows, 4)
+        if not isinstance(scale, torch.Tensor) or scale.dtype not in (torch.float8_e8m0fnu, torch.uint8) \
+                or tuple(scale.shape) != want or scale.device != q.device or not scale.is_contiguous():
+            raise MgnError(ERR_ARG, f"scale must be a contiguous float8_e8m0fnu tensor of shape {want} on {q.device}")
+        self._set(q, scale, rows, cols, ld)
+
+    def _set(self, q, scale, rows, cols, ld):
+        self.q, self.scale, self.rows, self.cols = q, scale, rows, cols
+        self.struct = CMat4(q.data_ptr(), scale.data_ptr(), rows, cols, ld)
+        return self
+
+
+def mgn_quant4(x, rowwise=True, transposed=False, colsum=False, accumulate=False, stream=None):
+    """Quantises x [rows][cols] to 4 bits with a power of two for each 32 columns
+    of a row (see include/mgn.h).  Returns (rows, columns, colsum): x and its
+    transpose as Mat4, or None, and the sums over x's rows: a new tensor with
+    colsum=True, or the given one (added to with accumulate)."""
+    if stream is not None:
+        return _elsewhere(mgn_quant4, dict(locals()))
+    torch = _torch()
+    xt = _row_type(x, "x")
+    r, c = x.shape
+    ldx = _row_ld(x, "x")
+    dev = x.device
+    q = s = qt = st = sums = ws = None
+    rb, cb, ldq, ldqt, need = -(-r // 128), -(-c // 128), -(-c // 32) * 16, -(-r // 32) * 16, 0
+    if rowwise:
+        q = torch.empty((r, ldq), dtype=torch.uint8, device=dev)
+        s = torch.empty((cb, r, 4), dtype=torch.float8_e8m0fnu, device=dev)
+    if transposed:
+        qt = torch.empty((c, ldqt), dtype=torch.uint8, device=dev)
+        st = torch.empty((rb, c, 4), dtype=torch.float8_e8m0fnu, device=dev)
+    if isinstance(colsum, torch.Tensor):
+        sums = colsum
+        _vector(sums, "colsum", c, dev)
+    elif accumulate:
+        raise MgnError(ERR_ARG, "accumulate needs the sums to add to")
+    elif colsum:
+        sums = torch.empty(c, dtype=torch.float32, device=dev)
+    if sums is not None:
+        need = rb * c * 4
+        ws = _scratch(need, dev)
+    if r > 0 and c > 0 or sums is not None:
+        _run(dev, lib().mgn_quant4,
+             (x.data_ptr(), xt, r, c, ldx, _at(q) or None, ldq, _at(s) or None, _at(qt) or None, ldqt, _at(st) or None,
+              _at(sums), 1 if accumulate else 0, _at(ws), need))
+    return Quantised(Mat4.__new__(Mat4)._set(q, s, r, c, ldq) if rowwise else None,
+                     Mat4.__new__(Mat4)._set(qt, st, c, r, ldqt) if transposed else None, sums)
+
+
+def mgn_dequant4(a, dtype=None, out=None, stream=None):
+    """The values of a Mat4 as rows in float32 or bfloat16 (dtype, default
+    float32, or those of out)."""
+    if stream is not None:
+        return _elsewhere(mgn_dequant4, dict(locals()))
+    if not isinstance(a, Mat4):
+        raise MgnError(ERR_ARG, "a must be a Mat4")
+    yt, ldy, out = _result(out, dtype, (a.rows, a.cols), a.q.device)
+    if a.rows > 0 and a.cols > 0:
+        _run(a.q.device, lib().mgn_dequant4, (C.byref(a.struct), yt, out.data_ptr(), ldy))
+    return out
+
+
+def _result(out, dtype, shape, device):
+    """(type, leading dimension, tensor) of a result: out, or a new one of dtype."""
+    torch = _torch()
+    if out is None:
+        if dtype is None or dtype == torch.float32:
+            return FP32, shape[1], torch.empty(shape, dtype=torch.float32, device=device)
+        if dtype == torch.bfloat16:
+            return BF16, shape[1], torch.empty(shape, dtype=torch.bfloat16, device=device)
+        raise MgnError(ERR_ARG, f"out is float32 or bfloat16, not {dtype}")
+    t, ld = _row_type(out, "out"), _row_ld(out, "out", shape)
+    if dtype is not None and out.dtype != dtype:
+        raise MgnError(ERR_ARG, f"out must be {dtype}, got {out.dtype}")
+    if out.device != device:
+        raise MgnError(ERR_ARG, f"out is on {out.device}, expected {device}")
+    return t, ld, out
+
+
+def mgn_matmul4(a, b, bias=None, act="none", aux=None, out=None, dtype=None, accumulate=False, stream=None):
+    """act(a b^T + bias) of two Mat4 (see include/mgn.h): [a.rows][b.rows] in
+    float32 or bfloat16 (dtype, default float32; out: written, or added to
+    with accumulate)."""
+    if stream is not None:
+        return _elsewhere(mgn_matmul4, dict(locals()))
+    if not isinstance(a, Mat4) or not isinstance(b, Mat4):
+        raise MgnError(ERR_ARG, "a and b must be Mat4")
+    if a.cols != b.cols:
+        raise MgnError(ERR_SHAPE, f"a has {a.cols} columns, b {b.cols}")
+    if act not in ACTS:
+        raise MgnError(ERR_ARG, f"unknown act {act!r}")
+    dev, m, n = a.q.device, a.rows, b.rows
+    if b.q.device != dev:
+        raise MgnError(ERR_ARG, f"b is on {b.q.device}, expected {dev}")
+    if out is None and accumulate:
+        raise MgnError(ERR_ARG, "accumulate needs an out to add to")
+    ct, ldc, out = _result(out, dtype, (m, n), dev)
+    ep = None
+    if bias is not None or act != "none" or accumulate:
+        ep = Epilogue(bias=_vector(bias, "bias", n, dev), act=ACTS[act], accumulate=1 if accumulate else 0)
+    if act == "relu_grad":
+        ep.aux_type, ep.ldaux = _row_type(aux, "aux"), _row_ld(aux, "aux", (m, n))
+        if aux.device != dev:
+            raise MgnError(ERR_ARG, f"aux is on {aux.device}, expected {dev}")
+        ep.aux = aux.data_ptr()
+    elif aux is not None:
+        raise MgnError(ERR_ARG, "aux is for relu_grad only")
+    if m == 0 or n == 0:
+        return out
+    L = lib()
+    need = C.c_size_t()
+    _check(L.mgn_matmul4_workspace(m, n, a.cols, C.byref(need)))
+    ws = _scratch(need.value, dev)
+    _run(dev, L.mgn_matmul4,
+         (C.byref(a.struct), C.byref(b.struct), None if ep is None else C.byref(ep), ct, out.data_ptr(), ldc, _at(ws),
+          need.value))
+    return out
+
+
+def _group_norm(x, groups, gamma, beta, act, samples, sample_ptr, eps):
+    xt = _row_type(x, "x")
+    rows, cols = x.shape
+    dev = x.device
+    if act not in GROUP_ACTS:
+        raise MgnError(ERR_ARG, f"unknown act {act!r}")
+    if sample_ptr is None:
+        n = 1 if samples is None else int(samples)
+    else:
+        torch = _torch()
+        if not isinstance(sample_ptr, torch.Tensor) or sample_ptr.dim() != 1 or sample_ptr.numel() < 1:
+            raise MgnError(ERR_ARG, "sample_ptr must be a tensor of one number more than there are samples")
+        n = sample_ptr.numel() - 1
+        if samples is not None and samples != n:
+            raise MgnError(ERR_ARG, f"sample_ptr is of {n} samples, not {samples}")
+        _dptr(sample_ptr, torch.int32, (n + 1,), "sample_ptr")
+        if sample_ptr.device != dev:
+            raise MgnError(ERR_ARG, f"sample_ptr is on {sample_ptr.device}, expected {dev}")
+    return CGroupNorm(rows, cols, int(groups), xt, GROUP_ACTS[act], eps, _vector(gamma, "gamma", cols, dev),
+                      _vector(beta, "beta", cols, dev), _at(sample_ptr), n)
+
+
+def mgn_group_norm_forward(x, groups, gamma=None, beta=None, act="none", samples=None, sample_ptr=None, eps=1e-5,
+                           save=False, y=None, stream=None):
+    """y = act(gamma xhat + beta), xhat being x normed over each sample's rows and
+    each of the groups of columns (see include/mgn.h).  Samples: as many runs of
+    equal length (default 1), or the runs of sample_ptr (int32, one number more
+    than there are samples).  Returns (y, stats): stats None without save.  y
+    may be x.  Rows outside of sample_ptr's are not written: a y that is not given
+    holds any bits there."""
+    if stream is not None:
+        return _elsewhere(mgn_group_norm_forward, dict(locals()))
+    torch = _torch()
+    op = _group_norm(x, groups, gamma, beta, act, samples, sample_ptr, eps)
+    shape, dev = tuple(x.shape), x.device
+    need = C.c_size_t()
+    _check(lib().mgn_group_norm_workspace(C.byref(op), 0, C.byref(need)))
+    y, yr = _new_rows(shape, x.dtype, dev) if y is None else (y, _as_rows(y, "y", shape, x.dtype, dev))
+    stats = torch.empty((op.n_samples, op.groups, 2), dtype=torch.float32, device=dev) if save else None
+    ws = _scratch(need.value, dev)
+    _run(dev, lib().mgn_group_norm_forward,
+         (C.byref(op), Rows(x.data_ptr(), _row_ld(x, "x")), yr, _at(stats), _at(ws), need.value))
+    return y, stats
+
+
+GroupNormGrads = collections.namedtuple("GroupNormGrads", "dx dgamma dbeta")
+
+
+def mgn_group_norm_backward(x, stats, dy, groups, gamma=None, beta=None, act="none", samples=None, sample_ptr=None,
+                            eps=1e-5, dx=None, grads=None, stream=None):
+    """Reverse of mgn_group_norm_forward (see include/mgn.h) from its input and
+    stats.  Returns GroupNormGrads; dgamma and dbeta are those of the parameters
+    that were given, new tensors, or those of grads (a GroupNormGrads of an
+    earlier call) added to.  dx may be dy or x.  Rows of dx outside of
+    sample_ptr's are not written."""
+    if stream is not None:
+        return _elsewhere(mgn_group_norm_backward, dict(locals()))
+    torch = _torch()
+    op = _group_norm(x, groups, gamma, beta, act, samples, sample_ptr, eps)
+    shape, dev = tuple(x.shape), x.device
+    need = C.c_size_t()
+    _check(lib().mgn_group_norm_workspace(C.byref(op), 1, C.byref(need)))
+    dx, dxr = _new_rows(shape, x.dtype, dev) if dx is None else (dx, _as_rows(dx, "dx", shape, x.dtype, dev))
+    if not isinstance(stats, torch.Tensor) or tuple(stats.shape) != (op.n_samples, op.groups, 2):
+        raise MgnError(ERR_ARG, "stats must be the forward's, of shape (samples, groups, 2)")
+    _vector(stats, "stats", stats.numel(), dev)
+    if dy is None:
+        raise MgnError(ERR_ARG, "dy is needed")
+    dyr = _as_rows(dy, "dy", shape, x.dtype, dev)
+    out = {}
+    for name, p in (("dgamma", gamma), ("dbeta", beta)):
+        g = getattr(grads, name) if grads is not None else None
+        if p is None:
+            if g is not None:
+                raise MgnError(ERR_ARG, f"{name} without its parameter")
+        elif grads is None:
+            g = torch.empty(p.shape, dtype=torch.float32, device=dev)
+        elif g is not None:
+            _vector(g, name, p.numel(), dev)
+        out[name] = g
+    ws = _scratch(need.value, dev)
+    _run(dev, lib().mgn_group_norm_backward,
+         (C.byref(op), Rows(x.data_ptr(), _row_ld(x, "x")), stats.data_ptr(), dyr, dxr, _at(out["dgamma"]),
+          _at(out["dbeta"]), 0 if grads is None else 1, _at(ws), need.value))
+    return GroupNormGrads(dx, **out)
+
+
+class TensorList:
+    """The list of gradients that mgn_grad_norm and mgn_grad_clip take: contiguous
+    float32 or bfloat16 tensors of one device and any sizes, and, for clipping,
+    the places of the clipped ones, as many tensors of the same sizes (out;
+    None: the gradients themselves).  A program makes it once and keeps it; it
+    keeps its tensors, whose values may change but not their places."""
+
+    def __init__(self, tensors, out=None):
+        torch = _torch()
+        self._given, self._out = list(tensors), None if out is None else list(out)
+        if not self._given:
+            raise MgnError(ERR_ARG, "a list of no tensors")
+        places = self._given if self._out is None else self._out
+        if len(places) != len(self._given):
+            raise MgnError(ERR_ARG, f"{len(places)} places for {len(self._given)} gradients")
+        types = {torch.float32: FP32, torch.bfloat16: BF16}
+        self.device = None
+        table = (CTensor * len(places))()
+        for i, (t, o) in enumerate(zip(self._given, places)):
+            for v in (t, o):
+                if not isinstance(v, torch.Tensor) or not v.is_cuda or v.dtype not in types or not v.is_contiguous():
+                    raise MgnError(ERR_ARG, f"tensor {i} must be contiguous, float32 or bfloat16, on the device")
+                if self.device is None:
+                    self.device = v.device
+                if v.device != self.device:
+                    raise MgnError(ERR_ARG, f"tensor {i} is on {v.device}, expected {self.device}")
+            if t.numel() != o.numel():
+                raise MgnError(ERR_ARG, f"tensor {i}: a place of {o.numel()} elements for {t.numel()}")
+            table[i] = CTensor(t.data_ptr(), o.data_ptr(), t.numel(), types[t.dtype], types[o.dtype])
+        n = C.c_int64()
+        _check(lib().mgn_grad_pieces(table, len(places), None, C.byref(n)))
+        pieces = (CPiece * n.value)()
+        _check(lib().mgn_grad_pieces(table, len(places), pieces, C.byref(n)))
+        self.n = n.value
+        # on the device once it is made, whatever stream uses it first
+        self.pieces = torch.frombuffer(bytearray(pieces), dtype=torch.uint8).to(self.device) if self.n else None
+        torch.cuda.current_stream(self.device).synchronize()
+        need = C.c_size_t()
+        _check(lib().mgn_grad_norm_workspace(self.n, C.byref(need)))
+        self.ws_bytes = need.value
+
+    def tensors(self):
+        return self._given + (self._out or []) + ([self.pieces] if self.n else [])
+
+
+def _list(tensors):
+    if not isinstance(tensors, TensorList):
+        raise MgnError(ERR_ARG, "a TensorList is needed")
+    return tensors.device
+
+
+def mgn_grad_norm(tensors, stream=None):
+    """The norm over all elements of a TensorList, a float32 tensor of one."""
+    if stream is not None:
+        return _elsewhere(mgn_grad_norm, dict(locals()))
+    dev = _list(tensors)
+    norm = _torch().empty(1, dtype=_torch().float32, device=dev)
+    ws = _scratch(tensors.ws_bytes, dev)
+    _run(dev, lib().mgn_grad_norm, (_at(tensors.pieces), tensors.n, norm.data_ptr(), _at(ws), tensors.ws_bytes))
+    return norm
+
+
+def mgn_grad_clip(tensors, max_norm, norm=None, stream=None):
+    """Scales a TensorList's gradients, into their places, by min(1, max_norm /
+    norm) (see include/mgn.h).  norm: of all of them, or the given float32 tensor
+    of one element (say of a norm over several processes).  Returns the norm.  One
+    that is not finite leaves the values as they are."""
+    if stream is not None:
+        return _elsewhere(mgn_grad_clip, dict(locals()))
+    dev = _list(tensors)
+    given = norm is not None
+    if given:
+        _vector(norm, "norm", 1, dev)
+    else:
+        norm = _torch().empty(1, dtype=_torch().float32, device=dev)
+    need = 0 if given else tensors.ws_bytes
+    ws = _scratch(need, dev)
+    _run(dev, lib().mgn_grad_clip,
+         (_at(tensors.pieces), tensors.n, float(max_norm), norm.data_ptr(), 1 if given else 0, _at(ws), need))
+    return norm
 
 
 # short aliases

@@ -1,0 +1,393 @@
+"""The 4-bit quantiser, its reading back and the product on the GPU against plain
+implementations in 64 bits.
+
+Quantisation and its reading back are compared for equality: scales and numbers are
+defined to the bit (see include/mgn.h).  The product's tolerance counts roundings
+of u = 2^-24: products of two numbers and the sums of 32 of them are exact, and the
+K / 32 block sums are added in float32 along at most K / 32 + 24 additions (eight waves
+or the splits' sums among them), each off by at most one step 2u of the magnitudes'
+sum; a bias adds one more, a result stored in bfloat16 is off by 2^-8 of itself.
+"""
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+from paper_2304_00338_amd import mgn  # noqa: E402
+
+U = 2.0 ** -24
+T = {"fp32": torch.float32, "bf16": torch.bfloat16}
+NUMBERS = np.array([0, .5, 1, 1.5, 2, 3, 4, 6])
+
+
+def randn(*shape, seed=0, dtype=torch.float32):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    return torch.randn(*shape, generator=g, device="cuda").to(dtype)
+
+
+def dirty(*shape, dtype=torch.float32):
+    """Memory that a call has to write: not a number, or all bits set."""
+    n = int(np.prod(shape)) * torch.empty(0, dtype=dtype).element_size()
+    return torch.full((max(n, 1),), 255, dtype=torch.uint8, device="cuda")[:n].view(dtype).view(*shape)
+
+
+def oracle_quant(x):
+    """(codes [rows][cols up to 32], scale bytes [rows][blocks]) of float rows."""
+    x = x.astype(np.float64)
+    r, c = x.shape
+    nb = -(-c // 32)
+    v = np.zeros((r, nb * 32))
+    v[:, :c] = x
+    v = v.reshape(r, nb, 32)
+    with np.errstate(invalid="ignore"):
+        top = np.abs(v).max(2)
+    bad = ~np.isfinite(v).all(2)
+    top = np.where(bad | (top == 0), 1.0, top)
+    e = np.frexp(top)[1] - 3 + (np.frexp(top)[0] >= 0.875)
+    e = np.maximum(np.where(np.abs(np.where(np.isfinite(v), v, 1)).max(2) == 0, -127, e), -127)
+    t = np.where(bad[:, :, None], 0.0, np.where(np.isfinite(v), v, 0)) * np.exp2(-e.astype(np.float64))[:, :, None]
+    a = np.abs(t)
+    hi = np.clip(np.searchsorted(NUMBERS, a), 1, 7)
+    da, db = NUMBERS[hi] - a, a - NUMBERS[hi - 1]
+    code = np.where((da < db) | ((da == db) & (hi % 2 == 0)), hi, hi - 1)
+    code = np.where(np.signbit(t), code + 8, code)
+    return code.reshape(r, -1), np.where(bad, 255, e + 127)
+
+
+def codes_of(m):
+    q = m.q.cpu().numpy()
+    return np.stack([q & 15, q >> 4], 2).reshape(q.shape[0], -1)
+
+
+def values_of(m):
+    """A Mat4's values in float64 (a NaN scale: NaN)."""
+    c = codes_of(m)[:, :m.cols].astype(int)
+    v = NUMBERS[c & 7] * np.where(c & 8, -1, 1)
+    s = m.scale.view(torch.uint8).cpu().numpy().astype(int).transpose(1, 0, 2).reshape(m.rows, -1)
+    x = np.where(s == 255, np.nan, np.exp2(s - 127.0))
+    return v * x[:, np.arange(m.cols) // 32]
+
+
+def check_mat4(m, x, what):
+    r, c = x.shape
+    assert (m.rows, m.cols) == (r, c)
+    code, s = oracle_quant(x)
+    got = codes_of(m)
+    assert got.shape == code.shape, what
+    # the sign of a zero counts for nothing
+    same = (got == code) | ((got & 7 == 0) & (code & 7 == 0))
+    assert same.all(), (what, np.argwhere(~same)[:4])
+    assert (got[:, c:] == 0).all(), what
+    sc = m.scale.view(torch.uint8).cpu().numpy().transpose(1, 0, 2).reshape(r, -1)
+    assert np.array_equal(sc[:, :s.shape[1]], s), (what, np.argwhere(sc[:, :s.shape[1]] != s)[:4])
+    assert (sc[:, s.shape[1]:] == 0).all(), what
+
+
+SIZES = [(1, 1), (1, 4096), (3, 31), (2, 32), (5, 33), (130, 16), (17, 150), (127, 257), (128, 128), (129, 384),
+         (300, 1000), (33, 8), (700, 1), (65, 95)]
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("copies", ["rows", "columns", "both"])
+def test_quant4(dtype, copies):
+    for n, (r, c) in enumerate(SIZES):
+        x = (randn(r, c, seed=n) * torch.exp(3 * randn(r, 1, seed=n + 50))).to(T[dtype])
+        out = mgn.mgn_quant4(x, copies != "columns", copies != "rows", colsum=copies == "both")
+        xn = x.float().cpu().numpy()
+        if copies != "columns":
+            check_mat4(out.rows, xn, (r, c))
+        if copies != "rows":
+            check_mat4(out.columns, np.ascontiguousarray(xn.T), (r, c))
+        if copies == "both":
+            ref, mag = xn.astype(np.float64).sum(0), np.abs(xn.astype(np.float64)).sum(0)
+            assert (np.abs(out.colsum.cpu().numpy() - ref) <= (r + 16) * U * mag).all()
+
+
+def hard_rows():
+    """Middles of neighbouring numbers and their float neighbours at several scales,
+    the borders of a scale, subnormals, the largest numbers, zeros, infinities, NaN."""
+    mid = (NUMBERS[1:] + NUMBERS[:-1]) / 2
+    v = np.concatenate([mid, np.nextafter(mid.astype(np.float32), np.float32(9)), np.nextafter(mid.astype(np.float32), np.float32(0))])
+    rows = []
+    for top in (6.0, 4.0, 3.5, np.nextafter(np.float32(7), np.float32(0)), 7.0, np.nextafter(np.float32(3.5), np.float32(0))):
+        for e in (-140, -127, -126, -60, 0, 3, 100, 124):
+            r = np.zeros(32, np.float64)
+            r[:len(v)] = v
+            r[0], r[31] = top, -top
+            with np.errstate(over="ignore"):
+                r = (r * np.exp2(float(e))).astype(np.float32)
+            rows.append(np.where(np.isfinite(r), r, np.float32(3e38)))
+    big = np.float32(3.4028234e38)
+    rows += [np.full(32, big), np.full(32, np.float32(1e-45)), np.zeros(32), -np.zeros(32),
+             np.linspace(2e-39, 4e-39, 32), np.linspace(0, 1.2e-38, 32)]
+    for bad in (np.inf, -np.inf, np.nan):
+        r = np.ones(32)
+        r[13] = bad
+        rows.append(r)
+    return np.stack(rows).astype(np.float32)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_quant4_hard_values(dtype):
+    x = hard_rows()
+    x = np.concatenate([x, np.roll(x, 1, 0)], 1)  # two blocks a row
+    xt = torch.from_numpy(x).cuda().to(T[dtype])
+    for src in (xt, xt.t().contiguous()):
+        xn = src.float().cpu().numpy()
+        out = mgn.mgn_quant4(src, True, True)
+        check_mat4(out.rows, xn, "rows")
+        check_mat4(out.columns, np.ascontiguousarray(xn.T), "columns")
+        check_mat4(mgn.mgn_quant4(src).rows, xn, "rows only")
+
+
+def test_quant4_strides_and_rows_behind():
+    for dt in ("fp32", "bf16"):
+        big = dirty(200, 301, dtype=T[dt])
+        big[3:140, 5:160] = randn(137, 155, seed=3).to(T[dt])
+        x = big[3:140, 5:160]
+        out = mgn.mgn_quant4(x, True, True, colsum=True)
+        xn = x.float().cpu().numpy()
+        check_mat4(out.rows, xn, "rows")
+        check_mat4(out.columns, np.ascontiguousarray(xn.T), "columns")
+        # results inside larger buffers: what is behind them stays
+        q, s = torch.full((139, 96), 7, dtype=torch.uint8, device="cuda"), torch.full((2 * 137 + 1, 4), 9, dtype=torch.uint8, device="cuda")
+        rc = mgn.lib().mgn_quant4(x.data_ptr(), mgn.FP32 if dt == "fp32" else mgn.BF16, 137, 155, 301, q.data_ptr(), 96,
+                                  s.data_ptr(), None, 0, None, None, 0, None, 0, torch.cuda.current_stream().cuda_stream)
+        assert rc == mgn.OK
+        torch.cuda.synchronize()
+        assert (q[137:] == 7).all() and (q[:, 80:] == 7).all() and (s[-1] == 9).all()
+        assert torch.equal(q[:137, :80], out.rows.q)
+    sums = torch.arange(155, dtype=torch.float32, device="cuda")
+    keep = sums.clone()
+    x = randn(40, 155, seed=4)
+    mgn.mgn_quant4(x, colsum=sums, accumulate=True)
+    assert torch.allclose(sums, keep + x.double().sum(0).float(), atol=1e-4)
+
+
+def test_quant4_empty():
+    for r, c in ((0, 40), (40, 0), (0, 0)):
+        out = mgn.mgn_quant4(torch.empty(r, c, device="cuda"), True, True, colsum=True)
+        assert (out.rows.rows, out.rows.cols, out.columns.rows, out.columns.cols) == (r, c, c, r)
+        assert out.colsum.shape == (c,) and (out.colsum == 0).all()
+        assert mgn.mgn_dequant4(out.rows).shape == (r, c)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_dequant4(dtype):
+    for n, (r, c) in enumerate(SIZES):
+        m = mgn.mgn_quant4(randn(r, c, seed=n) * 100).rows
+        y = mgn.mgn_dequant4(m, T[dtype])
+        assert y.dtype == T[dtype] and np.array_equal(y.double().cpu().numpy(), values_of(m))
+    # every number at every scale, into a place with a larger leading dimension
+    q = torch.arange(256, dtype=torch.uint8, device="cuda").view(16, 16).repeat(255, 1)
+    s = torch.zeros(1, 255 * 16, 4, dtype=torch.uint8, device="cuda")
+    s[0, :, 0] = torch.arange(255, device="cuda").repeat_interleave(16).to(torch.uint8)
+    s[0, -16:, 0] = 255
+    m = mgn.Mat4(q, s, 31)
+    big = dirty(255 * 16 + 2, 50, dtype=T[dtype])
+    mgn.mgn_dequant4(m, out=big[1:-1, 3:34])
+    ref = values_of(m)
+    with np.errstate(over="ignore"):
+        ref = ref.astype(np.float32).astype(np.float64)  # over the largest float32: infinity
+    assert np.array_equal(big[1:-1, 3:34].double().cpu().numpy(), ref, equal_nan=True)
+    assert torch.isnan(big[1:-1, :3].float()).all() and torch.isnan(big[1:-1, 34:].float()).all()
+    assert torch.isnan(big[0].float()).all() and torch.isnan(big[-1].float()).all()
+
+
+# ------------------------------------------------------------------- matmul4
+def mats(m, n, k, seed=0, spread=1.0):
+    a = randn(m, k, seed=seed) * torch.exp(spread * randn(m, 1, seed=seed + 1))
+    b = randn(n, k, seed=seed + 2) * torch.exp(spread * randn(n, 1, seed=seed + 3))
+    return mgn.mgn_quant4(a).rows, mgn.mgn_quant4(b).rows
+
+
+def check_product(got, a, b, dtype, bias=None, act=None, aux=None, add=None, what=None):
+    va, vb = (torch.from_numpy(values_of(v)).cuda() for v in (a, b))
+    ref, mag = va @ vb.t(), va.abs() @ vb.abs().t()
+    tol = (a.cols / 32 + 24) * 2 * U * mag
+    if bias is not None:
+        ref, tol = ref + bias.double(), tol + 2 * U * (mag + bias.double().abs())
+    if act == "relu":
+        ref = ref.clamp(min=0)
+    elif act == "relu_grad":
+        on = (aux.float() > 0).double()
+        ref, tol = ref * on, tol * on
+    if add is not None:
+        ref, tol = ref + add.double(), tol + 2 * U * (ref.abs() + add.double().abs())
+    if dtype == torch.bfloat16:
+        tol = tol + 2.0 ** -8 * (ref.abs() + tol) + 2.0 ** -134
+    off = (got.double() - ref).abs()
+    assert (off <= tol).all(), (what, float((off / (tol + 1e-300)).max()), (off > tol).nonzero()[:4].tolist())
+
+
+SHAPES = [(1, 1, 1), (1, 16, 32), (1, 4096, 4096), (2, 17, 33), (15, 130, 300), (16, 64, 128), (17, 200, 1000), (31, 33, 129),
+          (32, 100, 257), (33, 65, 95), (64, 128, 128), (100, 129, 384), (128, 128, 640), (129, 300, 1152), (257, 255, 1000),
+          (300, 31, 5000), (40, 24, 30000), (20, 40, 70000), (500, 7, 31), (63, 1000, 513)]
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_matmul4(dtype):
+    for i, (m, n, k) in enumerate(SHAPES):
+        a, b = mats(m, n, k, seed=10 * i)
+        check_product(mgn.mgn_matmul4(a, b, dtype=T[dtype]), a, b, T[dtype], what=(m, n, k))
+
+
+@pytest.mark.parametrize("m,n,k", [(4096, 3841, 1100), (3840, 4096, 1024), (4100, 4090, 2049), (16400, 1000, 1500)])
+def test_matmul4_large_tiles(m, n, k):
+    a, b = mats(m, n, k, seed=m)
+    for dt in ("fp32", "bf16"):
+        check_product(mgn.mgn_matmul4(a, b, dtype=T[dt]), a, b, T[dt], what=dt)
+
+
+@pytest.mark.parametrize("steps", list(range(1, 18)))
+def test_matmul4_every_number_of_steps(steps):
+    """The ring of buffers from its filling to its emptying, with and without a
+    part of a last step."""
+    for k in (128 * steps, 128 * steps - 37):
+        a, b = mats(160, 140, k, seed=steps)
+        check_product(mgn.mgn_matmul4(a, b), a, b, torch.float32, what=k)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("act", ["none", "relu", "relu_grad"])
+def test_matmul4_epilogue(dtype, act):
+    for m, n, k in ((1, 40, 100), (30, 131, 200), (140, 133, 300), (200, 35, 40000)):
+        a, b = mats(m, n, k, seed=m)
+        bias = randn(n, seed=5) * 10
+        for at in ("fp32", "bf16"):
+            aux = randn(m, n + 3, seed=6).to(T[at])[:, 2:n + 2] if act == "relu_grad" else None
+            check_product(mgn.mgn_matmul4(a, b, bias=bias, act=act, aux=aux, dtype=T[dtype]), a, b, T[dtype], bias, act, aux)
+        big = dirty(m + 1, n + 5, dtype=T[dtype])
+        out = big[:m, 3:n + 3]
+        out.copy_(randn(m, n, seed=7) * 10)
+        add = out.clone()
+        mgn.mgn_matmul4(a, b, act=act, aux=aux, out=out, accumulate=True)
+        check_product(out, a, b, T[dtype], None, act, aux, add)
+        assert torch.isnan(big[:, :3].float()).all() and torch.isnan(big[:, n + 3:].float()).all() and torch.isnan(big[m].float()).all()
+
+
+def test_matmul4_strides():
+    """Operands inside larger buffers whose other bytes hold anything."""
+    for m, n, k in ((9, 40, 200), (150, 140, 200), (150, 140, 33)):
+        a, b = mats(m, n, k, seed=k)
+        w = a.q.shape[1]
+        qa = torch.full((m + 2, w + 48), 0x77, dtype=torch.uint8, device="cuda")
+        qa[1:-1, 16:16 + w] = a.q
+        qb = torch.full((n + 1, w + 16), 0x77, dtype=torch.uint8, device="cuda")
+        qb[:n, :w] = b.q
+        got = mgn.mgn_matmul4(mgn.Mat4(qa[1:-1, 16:16 + w], a.scale, k), mgn.Mat4(qb[:n, :w], b.scale, k))
+        assert torch.equal(got, mgn.mgn_matmul4(a, b))
+        check_product(got, a, b, torch.float32)
+
+
+@pytest.mark.parametrize("m,n,k", [(3, 50, 500), (150, 140, 500), (40, 30, 9000)])
+def test_matmul4_not_finite(m, n, k):
+    """A block that holds an infinity or a NaN reaches its own rows and no others."""
+    a, b = randn(m, k, seed=1), randn(n, k, seed=2)
+    a[1, 40], b[7, k - 1], b[9, 300] = float("inf"), float("nan"), float("-inf")
+    got = mgn.mgn_matmul4(mgn.mgn_quant4(a).rows, mgn.mgn_quant4(b).rows)
+    bad = torch.zeros(m, n, dtype=torch.bool, device="cuda")
+    bad[1], bad[:, 7], bad[:, 9] = True, True, True
+    assert torch.equal(torch.isnan(got), bad)
+
+
+@pytest.mark.parametrize("m", [5, 150])
+def test_matmul4_far_scales(m):
+    """Scales from one end of their range to the other whose products are in range."""
+    n, k = 140, 160
+    a, b = mats(m, n, k, spread=0.0)
+    for ea, eb in ((0, 120), (254, 5), (1, 253), (3, 127), (127, 0), (60, 200)):
+        sa, sb = a.scale.view(torch.uint8).clone(), b.scale.view(torch.uint8).clone()
+        sa[:, :, 0], sb[:, :, 0], sa[1, :, 1:], sb[1, :, 1:] = ea, eb, 0, 0
+        sa[0, :, 1:], sb[0, :, 1:] = ea, eb
+        sa[1, :, 0], sb[1, :, 0] = ea, eb
+        x, y = mgn.Mat4(a.q, sa, k), mgn.Mat4(b.q, sb, k)
+        got = mgn.mgn_matmul4(x, y).double().cpu().numpy()
+        va, vb = values_of(x), values_of(y)
+        ref, mag = va @ vb.T, np.abs(va) @ np.abs(vb).T
+        fits = mag < 3e38
+        assert fits.any()
+        # below the smallest normal number half a step of the subnormals for each addition
+        assert (np.abs(got - ref)[fits] <= ((k / 32 + 24) * (2 * U * mag + 2.0 ** -148))[fits]).all(), (ea, eb)
+
+
+def test_matmul4_empty():
+    a, b = mats(5, 6, 40)
+    none = mgn.mgn_quant4(torch.empty(0, 40, device="cuda")).rows
+    assert mgn.mgn_matmul4(none, b).shape == (0, 6) and mgn.mgn_matmul4(a, none).shape == (5, 0)
+    for m, n in ((5, 6), (40, 200)):
+        x, y = (mgn.mgn_quant4(torch.empty(r, 0, device="cuda")).rows for r in (m, n))
+        assert (mgn.mgn_matmul4(x, y) == 0).all()
+        bias = randn(n)
+        assert torch.equal(mgn.mgn_matmul4(x, y, bias=bias), bias.expand(m, n))
+
+
+def test_far_offsets():
+    """Rows whose bytes lie past 2^31, numbers and results."""
+    m, n, k = 300, 140, 96
+    a, b = mats(m, n, k, seed=4)
+    wide = torch.empty(m, 1 << 24, dtype=torch.uint8, device="cuda")
+    wide[:, :48] = a.q
+    x = mgn.Mat4(wide[:, :48], a.scale, k)
+    out = torch.empty(m, 1 << 23, device="cuda")[:, 5:5 + n]
+    mgn.mgn_matmul4(x, b, out=out)
+    assert torch.equal(out, mgn.mgn_matmul4(a, b))
+    few = mgn.Mat4(wide[270:, :48], a.scale[:, 270:].contiguous(), k)
+    assert torch.equal(mgn.mgn_matmul4(few, b), mgn.mgn_matmul4(mgn.Mat4(a.q[270:], few.scale, k), b))
+    vals = torch.empty(m, 1 << 22, device="cuda")[:, 7:7 + k]
+    mgn.mgn_dequant4(x, out=vals)
+    assert torch.equal(vals, mgn.mgn_dequant4(a))
+    back = mgn.mgn_quant4(vals, True, True)
+    assert torch.equal(back.rows.q, mgn.mgn_quant4(vals.contiguous()).rows.q)
+
+
+def test_binding_refusals():
+    a, b = mats(4, 5, 64)
+    x = randn(4, 64)
+    bad = [lambda: mgn.mgn_quant4(x.cpu()), lambda: mgn.mgn_quant4(x.half()), lambda: mgn.mgn_quant4(x[0]),
+           lambda: mgn.mgn_quant4(x.t()), lambda: mgn.mgn_quant4(x, accumulate=True),
+           lambda: mgn.mgn_quant4(x, colsum=torch.empty(3, device="cuda")), lambda: mgn.mgn_dequant4(a.q),
+           lambda: mgn.mgn_dequant4(a, torch.float16), lambda: mgn.mgn_dequant4(a, out=torch.empty(4, 63, device="cuda")),
+           lambda: mgn.Mat4(a.q, a.scale, 65), lambda: mgn.Mat4(a.q.float(), a.scale, 64),
+           lambda: mgn.Mat4(a.q, a.scale[:, :3], 64), lambda: mgn.Mat4(a.q, a.scale, -1), lambda: mgn.Mat4(a.q.cpu(), a.scale, 64),
+           lambda: mgn.mgn_matmul4(a, b, act="silu"), lambda: mgn.mgn_matmul4(a, b, aux=x),
+           lambda: mgn.mgn_matmul4(a, b, accumulate=True), lambda: mgn.mgn_matmul4(a, b, bias=torch.empty(4, device="cuda")),
+           lambda: mgn.mgn_matmul4(a, b, dtype=torch.float16), lambda: mgn.mgn_matmul4(a, mats(3, 3, 63)[0]),
+           lambda: mgn.mgn_matmul4(a, x), lambda: mgn.mgn_matmul4(a, b, act="relu_grad")]
+    for f in bad:
+        with pytest.raises((mgn.MgnError, TypeError)):
+            f()
+
+
+def test_reproducible_streams_and_graphs():
+    x, w = randn(700, 300, seed=1), randn(40, 300, seed=2)
+
+    def step():
+        xq, wq = mgn.mgn_quant4(x, transposed=True, colsum=True), mgn.mgn_quant4(w, transposed=True)
+        y = mgn.mgn_matmul4(xq.rows, wq.rows)
+        dy = mgn.mgn_quant4(y, transposed=True)
+        return [y, mgn.mgn_matmul4(dy.rows, wq.columns), mgn.mgn_matmul4(dy.columns, xq.columns), xq.colsum,
+                mgn.mgn_dequant4(xq.rows)]
+    ref = step()
+    for _ in range(3):
+        assert all(torch.equal(p, q) for p, q in zip(step(), ref))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    m = mgn.mgn_quant4(x, stream=side).rows
+    got = mgn.mgn_matmul4(m, mgn.mgn_quant4(w, stream=side).rows, stream=side)
+    side.synchronize()
+    assert torch.equal(got, ref[0])
+    with torch.cuda.stream(side):
+        step()
+    side.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = step()
+    for k in range(4):
+        x.copy_(randn(700, 300, seed=10 + k))
+        want = step()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(p, q) for p, q in zip(out, want)), k

@@ -1,0 +1,206 @@
+"""The norm over many gradients and its clipping on the GPU against numpy in 64 bits.
+
+The sum is of 64 bits, so the norm is off by its one rounding to float32 (u = 2^-24;
+allowed 1.01 u), and a clipped value by one rounding of its type and, in bfloat16, the
+float32 before it (2^-8 + u)."""
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+from paper_2304_00338_amd import mgn  # noqa: E402
+
+U = 2.0 ** -24
+T = {"fp32": torch.float32, "bf16": torch.bfloat16}
+
+
+def tensors(sizes, types, seed=0, scale=1.0):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    return [(torch.randn(n, generator=g, device="cuda") * scale * (1 + i % 3)).to(T[types[i % len(types)]])
+            for i, n in enumerate(sizes)]
+
+
+def exact(ts):
+    return float(np.sqrt(sum((t.double().cpu().numpy() ** 2).sum() for t in ts)))
+
+
+def check(got, before, norm, most, what=None):
+    k = min(1.0, most / norm) if np.isfinite(norm) else 1.0
+    for i, (o, b) in enumerate(zip(got, before)):
+        ref = b.double() * k
+        step = U if o.dtype == torch.float32 else 2.0 ** -8 + U
+        low = 2.0 ** -149 if o.dtype == torch.float32 else 2.0 ** -133
+        off = (o.double() - ref).abs() - ref.abs() * step * 1.01
+        assert o.numel() == 0 or float(off.max()) <= low, (what, i)
+
+
+SIZES = {"one": [1], "few": [5, 128, 49152, 1, 16384, 16385, 0, 3], "many": [(37 * i) % 501 for i in range(700)],
+         "large": [3_000_001, 17, 5_000_000]}
+
+
+@pytest.mark.parametrize("sizes", list(SIZES))
+@pytest.mark.parametrize("types", [["fp32"], ["bf16"], ["bf16", "fp32", "fp32"]])
+@pytest.mark.parametrize("most", [0.3, 3.0])
+def test_clip(sizes, types, most):
+    g = tensors(SIZES[sizes], types, seed=len(sizes))
+    norm = exact(g)
+    before = [t.clone() for t in g]
+    lst = mgn.TensorList(g)
+    assert abs(float(mgn.mgn_grad_norm(lst)) - norm) <= 1.01 * U * norm
+    # into one flat buffer of float32, whose pieces are of any alignment
+    flat = torch.full((sum(SIZES[sizes]) + 2,), float("nan"), device="cuda")
+    places = list(flat[1:-1].split([t.numel() for t in g]))
+    got = mgn.mgn_grad_clip(mgn.TensorList(g, places), most * norm)
+    assert abs(float(got) - norm) <= 1.01 * U * norm
+    check(places, before, norm, most * norm, "flat")
+    assert torch.isnan(flat[0]) and torch.isnan(flat[-1])
+    assert all(torch.equal(a, b) for a, b in zip(g, before))
+    # in place
+    mgn.mgn_grad_clip(lst, most * norm)
+    check(g, before, norm, most * norm, "in place")
+    if most > 1:
+        assert all(torch.equal(a, b) for a, b in zip(g, before))
+
+
+@pytest.mark.parametrize("out", ["fp32", "bf16"])
+def test_types_and_alignments(out):
+    buf = torch.zeros(40000, dtype=torch.bfloat16, device="cuda")
+    g = [buf[1:20000], buf[20001:20010]]
+    for i, t in enumerate(g):
+        t.copy_(tensors([t.numel()], ["bf16"], seed=i)[0])
+    places = [torch.empty(t.numel() + 3, dtype=T[out], device="cuda")[3:] for t in g]
+    norm = exact(g)
+    mgn.mgn_grad_clip(mgn.TensorList(g, places), 0.1 * norm)
+    check(places, g, norm, 0.1 * norm)
+    f = tensors([1000], ["fp32"])
+    o = [torch.empty(1000, dtype=T[out], device="cuda")]
+    mgn.mgn_grad_clip(mgn.TensorList(f, o), 1.0)
+    check(o, f, exact(f), 1.0)
+
+
+@pytest.mark.parametrize("scale", [1e-44, 1e-30, 1e30, 1e36])
+def test_any_magnitude(scale):
+    """Squares beyond float32's range, and a factor below its normal numbers."""
+    g = tensors([100, 70000], ["fp32"], scale=scale)
+    norm = exact(g)
+    for most in (1e-3, 1e-20):
+        out = [torch.empty_like(t) for t in g]
+        got = float(mgn.mgn_grad_clip(mgn.TensorList(g, out), most))
+        # at 1e36 the norm, 1e36 times the root of 100 + 4 * 70,000, is 5.3e38: more than
+        # the largest float32, 3.4e38, and so an infinity
+        assert got == float("inf") if norm > 3.4028236e38 else abs(got - norm) <= 1.01 * U * norm + 2.0 ** -149
+        check(out, g, norm, most)
+
+
+def test_norm_over_float32():
+    """The norm is no float32; the factor comes of its 64 bits."""
+    g = [torch.full((5000,), 3e38, device="cuda")]
+    out = [torch.empty_like(g[0])]
+    assert float(mgn.mgn_grad_clip(mgn.TensorList(g, out), 1.0)) == float("inf")
+    check(out, g, exact(g), 1.0)
+
+
+@pytest.mark.parametrize("bad", [float("inf"), float("-inf"), float("nan")])
+def test_not_finite(bad):
+    """A norm that is no number clips nothing."""
+    g = tensors([300, 20000], ["fp32", "bf16"])
+    g[1][777] = bad
+    out = [torch.zeros_like(t) for t in g]
+    norm = mgn.mgn_grad_clip(mgn.TensorList(g, out), 1.0)
+    assert not torch.isfinite(norm)
+    for a, b in zip(out, g):
+        assert np.array_equal(a.float().cpu().numpy(), b.float().cpu().numpy(), equal_nan=True)
+    mgn.mgn_grad_clip(mgn.TensorList(g), 1.0)
+    assert np.array_equal(g[1].float().cpu().numpy(), out[1].float().cpu().numpy(), equal_nan=True)
+
+
+def test_zero_and_infinite_largest_norm():
+    g = tensors([400], ["fp32"])
+    out = [torch.empty_like(g[0])]
+    mgn.mgn_grad_clip(mgn.TensorList(g, out), 0.0)
+    assert (out[0] == 0).all()
+    mgn.mgn_grad_clip(mgn.TensorList(g, out), float("inf"))
+    assert torch.equal(out[0], g[0])
+    zero = [torch.zeros(5, device="cuda")]
+    assert float(mgn.mgn_grad_clip(mgn.TensorList(zero), 1.0)) == 0 and (zero[0] == 0).all()
+
+
+def test_given_norm():
+    """A norm formed elsewhere, as over several processes: not written."""
+    g = tensors([1000, 30000], ["fp32", "bf16"])
+    lst = mgn.TensorList(g)
+    before = [t.clone() for t in g]
+    norm = mgn.mgn_grad_norm(lst) * 4
+    keep = norm.clone()
+    assert mgn.mgn_grad_clip(lst, 2.0, norm=norm) is norm and torch.equal(norm, keep)
+    check(g, before, float(keep), 2.0)
+    for bad in (float("inf"), float("nan")):
+        now = [t.clone() for t in g]
+        mgn.mgn_grad_clip(lst, 1e-3, norm=torch.full((1,), bad, device="cuda"))
+        assert all(torch.equal(a, b) for a, b in zip(g, now))
+
+
+def test_empty_tensors_only():
+    g = [torch.empty(0, device="cuda")]
+    assert float(mgn.mgn_grad_norm(mgn.TensorList(g))) == 0
+    assert float(mgn.mgn_grad_clip(mgn.TensorList(g), 1.0)) == 0
+
+
+def test_refusals():
+    a, b = torch.zeros(10, device="cuda"), torch.zeros(20, device="cuda")
+    lst = mgn.TensorList([a])
+    for f in (lambda: mgn.TensorList([]), lambda: mgn.TensorList([a], [b]), lambda: mgn.TensorList([a, a]),
+              lambda: mgn.TensorList([a, a[2:4]]), lambda: mgn.TensorList([a], [a.half()]), lambda: mgn.TensorList([a.cpu()]),
+              lambda: mgn.TensorList([b[::2]]), lambda: mgn.TensorList([a], []), lambda: mgn.TensorList([a, b[:10]], [b[:10], b[10:]]),
+              lambda: mgn.TensorList([b[:10]], [b[1:11]]), lambda: mgn.mgn_grad_norm([a]),
+              lambda: mgn.mgn_grad_clip(lst, -1.0), lambda: mgn.mgn_grad_clip(lst, float("nan")),
+              lambda: mgn.mgn_grad_clip(lst, 1.0, norm=b)):
+        with pytest.raises(mgn.MgnError):
+            f()
+    assert mgn.TensorList([a, a], [b[:10], b[10:]]).n == 2  # the same gradient into two places
+
+
+def test_reproducible_streams_and_graphs():
+    g = tensors(SIZES["many"] + [400000], ["fp32", "bf16"], seed=3)
+    flat = torch.empty(sum(t.numel() for t in g), device="cuda")
+    lst = mgn.TensorList(g, list(flat.split([t.numel() for t in g])))
+    norm = mgn.mgn_grad_clip(lst, 1.0)
+    ref = flat.clone()
+    for _ in range(3):
+        flat.zero_()
+        assert torch.equal(mgn.mgn_grad_clip(lst, 1.0), norm) and torch.equal(flat, ref)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    flat.zero_()
+    side.wait_stream(torch.cuda.current_stream())
+    got = mgn.mgn_grad_clip(lst, 1.0, stream=side)
+    side.synchronize()
+    assert torch.equal(got, norm) and torch.equal(flat, ref)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = mgn.mgn_grad_clip(lst, 1.0)
+    for k in range(4):
+        for t, new in zip(g, tensors([t.numel() for t in g], ["fp32", "bf16"], seed=20 + k, scale=0.5)):
+            t.copy_(new)
+        want = mgn.mgn_grad_clip(lst, 1.0).clone(), flat.clone()
+        torch.cuda.synchronize()
+        flat.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want[0]) and torch.equal(flat, want[1]), k
+
+
+def test_before_adam():
+    """Gradients kept one by one, clipped into the flat buffer of an Adam update."""
+    g = tensors([128 * 384, 128, 128 * 128, 128], ["bf16", "fp32"], seed=5, scale=3.0)
+    n = sum(t.numel() for t in g)
+    flat = torch.empty(n, device="cuda")
+    lst = mgn.TensorList(g, list(flat.split([t.numel() for t in g])))
+    p, m, v = torch.ones(n, device="cuda"), torch.zeros(n, device="cuda"), torch.zeros(n, device="cuda")
+    mgn.mgn_grad_clip(lst, 1.0)
+    mgn.mgn_adam_step(mgn.Adam(), 1, p, flat, m, v)
+    ref = torch.cat([t.double() for t in g]) / exact(g)
+    # m = (1 - beta1) g, from one clipping and one product's roundings
+    assert ((m.double() - (1 - 0.9) * ref).abs() <= 4 * U * ref.abs() * 0.1 + 1e-30).all()
+    assert (p != 1).any()

@@ -1,0 +1,403 @@
+"""The group norm with its activation and its reverse on the GPU against numpy in 64
+bits.
+
+Tolerances count roundings of u = 2^-24.  Sums of x and x^2 are of 64 bits, so the
+statistics are off by one rounding each: xhat by ex = u (|mean| rstd + 4 |xhat|), z by
+ez = |gamma| ex + 3 u (|gamma xhat| + |z|).  A sigmoid is off by (|z| + 8) u of itself
+(the exponent's rounding, an exponential, a sum, a reciprocal), so y by 1.1 ez + (|z| + 10) u |y|
+(below 2^-100 of it nothing is counted: exp(-z) past float32 makes a zero) and dy
+act'(z) by ed = |dy| (0.6 ez + 16 u (1 + |z|)^2).  A mean over a sample's group of n values
+adds a chain of at most n + 64 roundings of the magnitudes' mean; dx has those of
+its two means, of xhat, and six more; a column's sum at most rows + 512.
+"""
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+from paper_2304_00338_amd import mgn  # noqa: E402
+
+U = 2.0 ** -24
+T = {"fp32": torch.float32, "bf16": torch.bfloat16}
+EPS = 1e-5
+
+
+def randn(*shape, seed=0, dtype=torch.float32):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    return torch.randn(*shape, generator=g, device="cuda").to(dtype)
+
+
+def dirty(*shape, dtype=torch.float32):
+    return torch.full(shape, float("nan"), dtype=dtype, device="cuda")
+
+
+def spans_of(rows, samples, ptr):
+    return list(zip(ptr[:-1], ptr[1:])) if ptr is not None else \
+        [(i * (rows // samples), (i + 1) * (rows // samples)) for i in range(samples)]
+
+
+def oracle(x, dy, gamma, beta, groups, act, spans):
+    """Results and tolerances in 64 bits, rows outside of the samples NaN."""
+    rows, cols = x.shape
+    d = cols // groups
+    gamma = np.ones(cols) if gamma is None else gamma
+    beta = np.zeros(cols) if beta is None else beta
+    out = {k: np.full((rows, cols), np.nan) for k in ("y", "ty", "dx", "tdx")}
+    out["stats"] = np.zeros((len(spans), groups, 2))
+    out["stats"][:, :, 1] = 1 / np.sqrt(EPS)
+    for k in ("dgamma", "dbeta", "tdgamma", "tdbeta", "mdgamma", "mdbeta"):
+        out[k] = np.zeros(cols)
+
+    def each(v):  # of groups to columns
+        return np.repeat(v, d)[None, :]
+    for s, (a, b) in enumerate(spans):
+        if a >= b:
+            continue
+        v = x[a:b]
+        g = v.reshape(b - a, groups, d)
+        n = (b - a) * d
+        mean = g.mean((0, 2))
+        rstd = 1 / np.sqrt(((g - mean[None, :, None]) ** 2).mean((0, 2)) + EPS)
+        out["stats"][s] = np.stack([mean, rstd], 1)
+        xhat = (v - each(mean)) * each(rstd)
+        ex = U * (np.abs(each(mean)) * each(rstd) + 4 * np.abs(xhat))
+        z = gamma * xhat + beta
+        ez = np.abs(gamma) * ex + 3 * U * (np.abs(gamma * xhat) + np.abs(z))
+        with np.errstate(over="ignore"):
+            sig = 1 / (1 + np.exp(-z))
+        az = np.abs(z)
+        if act == "silu":
+            y, slope = z * sig, sig * (1 + z * (1 - sig))
+            out["y"][a:b], out["ty"][a:b] = y, 1.1 * ez + (az + 10) * U * np.abs(y) + 2.0 ** -100
+        elif act == "relu":
+            y, slope = np.maximum(z, 0), (z > 0).astype(float)
+            out["y"][a:b], out["ty"][a:b] = y, ez
+        else:
+            slope = np.ones_like(z)
+            out["y"][a:b], out["ty"][a:b] = z, ez
+        if dy is None:
+            continue
+        t = dy[a:b]
+        dd = t * slope
+        if act == "silu":
+            ed = np.abs(t) * (0.6 * ez + 16 * U * (1 + az) ** 2)
+        elif act == "relu":
+            ed = np.where(az <= 2 * ez, np.abs(t), 0.0)  # the other side of the kink
+        else:
+            ed = np.zeros_like(t)
+        eg = ed * np.abs(xhat) + np.abs(dd) * ex
+        out["dgamma"] += (dd * xhat).sum(0)
+        out["dbeta"] += dd.sum(0)
+        out["mdgamma"] += np.abs(dd * xhat).sum(0)
+        out["mdbeta"] += np.abs(dd).sum(0)
+        out["tdgamma"] += eg.sum(0)
+        out["tdbeta"] += ed.sum(0)
+        u, eu = gamma * dd, np.abs(gamma) * ed + 2 * U * np.abs(gamma * dd)
+
+        def mean_of(w):
+            return each(w.reshape(b - a, groups, d).mean((0, 2)))
+        m1, m2 = mean_of(u), mean_of(u * xhat)
+        em1 = mean_of(eu) + (n + 64) * U * mean_of(np.abs(u))
+        em2 = mean_of(eu * np.abs(xhat) + np.abs(u) * ex) + (n + 64) * U * mean_of(np.abs(u * xhat))
+        out["dx"][a:b] = each(rstd) * (u - m1 - xhat * m2)
+        out["tdx"][a:b] = each(rstd) * (eu + em1 + np.abs(xhat) * em2 + ex * np.abs(m2) +
+                                        6 * U * (np.abs(u) + np.abs(m1) + np.abs(xhat * m2)))
+    for k in ("dgamma", "dbeta"):
+        out["t" + k] += (rows + 512) * U * out["m" + k]
+    return out
+
+
+def near(got, ref, tol, what, bf16=False):
+    got = got.double().cpu().numpy()
+    if bf16:
+        tol = tol + 2.0 ** -8 * (np.abs(ref) + tol)
+    in_ = ~np.isnan(ref)
+    off = np.abs(got - ref)[in_]
+    assert np.isfinite(got[in_]).all() and (off <= tol[in_]).all(), (what, float((off / (tol[in_] + 1e-300)).max()))
+
+
+def case(rows, cols, groups, dtype="fp32", act="silu", samples=1, ptr=None, affine=True, seed=0, shift=1.0, x=None, grads=True):
+    x = (randn(rows, cols, seed=seed) * torch.exp(0.5 * randn(1, cols, seed=seed + 1)) + shift * randn(1, cols, seed=seed + 2)).to(T[dtype]) if x is None else x
+    dy = randn(rows, cols, seed=seed + 3).to(T[dtype])
+    gamma, beta = (1 + 0.3 * randn(cols, seed=seed + 4), 0.3 * randn(cols, seed=seed + 5)) if affine else (None, None)
+    with_ = dict(gamma=gamma, beta=beta, act=act, eps=EPS)
+    with_.update(samples=samples) if ptr is None else with_.update(sample_ptr=torch.tensor(ptr, dtype=torch.int32, device="cuda"))
+    spans = spans_of(rows, samples, ptr)
+    host = [None if v is None else v.double().cpu().numpy() for v in (x, dy, gamma, beta)]
+    ref = oracle(*host, groups, act, spans)
+    what, low = (rows, cols, groups, dtype, act, samples, ptr and len(ptr)), dtype == "bf16"
+    y, stats = mgn.mgn_group_norm_forward(x, groups, save=True, y=dirty(rows, cols, dtype=T[dtype]), **with_)
+    near(y, ref["y"], ref["ty"], ("y", what), low)
+    out = np.isnan(ref["y"])
+    assert np.isnan(y.double().cpu().numpy()[out]).all(), ("rows outside", what)
+    st = stats.double().cpu().numpy()
+    assert (np.abs(st[:, :, 0] - ref["stats"][:, :, 0]) <= 1.01 * U * np.abs(ref["stats"][:, :, 0]) + 1e-12).all(), ("mean", what)
+    assert (np.abs(st[:, :, 1] / ref["stats"][:, :, 1] - 1) <= 2 * U + 1e-9).all(), ("rstd", what)
+    if not grads:
+        return
+    r = mgn.mgn_group_norm_backward(x, stats, dy, groups, dx=dirty(rows, cols, dtype=T[dtype]), **with_)
+    near(r.dx, ref["dx"], ref["tdx"], ("dx", what), low)
+    assert np.isnan(r.dx.double().cpu().numpy()[out]).all(), ("rows outside", what)
+    if affine:
+        near(r.dgamma, ref["dgamma"], ref["tdgamma"], ("dgamma", what))
+        near(r.dbeta, ref["dbeta"], ref["tdbeta"], ("dbeta", what))
+    else:
+        assert r.dgamma is None and r.dbeta is None
+
+
+SHAPES = [(1, 1, 1), (1, 8, 1), (2, 5, 1), (7, 9, 3), (64, 128, 32), (33, 150, 10), (100, 128, 128), (50, 96, 1), (17, 2050, 1),
+          (9, 4099, 1), (40, 2048, 2048), (5, 16384, 32), (3, 16384, 1), (600, 24, 3), (31, 2120, 8), (64, 3, 3)]
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("rows,cols,groups", SHAPES)
+def test_shapes(rows, cols, groups, dtype):
+    """Small calls: a block for a sample."""
+    case(rows, cols, groups, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("rows,cols,groups", [(30001, 128, 32), (9000, 150, 15), (3001, 640, 32), (2000, 2051, 7), (700, 16384, 4),
+                                              (1200, 4100, 1), (40000, 24, 24), (300000, 5, 1), (1500, 2048, 2048)])
+def test_tiles(rows, cols, groups, dtype):
+    case(rows, cols, groups, dtype, samples=1)
+
+
+@pytest.mark.parametrize("act", ["none", "relu", "silu"])
+@pytest.mark.parametrize("affine", [True, False])
+@pytest.mark.parametrize("rows", [90, 30000])
+def test_acts(act, affine, rows):
+    for dtype in ("fp32", "bf16"):
+        case(rows, 48, 6, dtype, act, samples=3, affine=affine, seed=7)
+
+
+def ragged(rows, samples, seed, lo=0, hi=None):
+    r = np.random.default_rng(seed)
+    cut = np.sort(r.integers(lo, (rows if hi is None else hi) + 1, samples - 1))
+    return [lo] + cut.tolist() + [rows if hi is None else hi]
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("rows,cols,groups,samples", [(500, 128, 32, 9), (40000, 128, 32, 32), (40000, 64, 8, 300),
+                                                      (20000, 96, 3, 20000), (3000, 640, 32, 50), (9000, 20, 1, 2)])
+def test_ragged(rows, cols, groups, samples, dtype):
+    """Samples of any length, empty ones among them, many in a tile and tiles in one."""
+    case(rows, cols, groups, dtype, ptr=ragged(rows, samples, rows), shift=0.3)
+
+
+@pytest.mark.parametrize("rows", [400, 30000])
+def test_rows_outside(rows):
+    """Rows outside of the samples hold anything and stay as they were."""
+    for lo, hi in ((37, rows - 45), (0, rows - 1), (5, rows), (100, 100)):
+        ptr = ragged(rows, 7, 3, lo, hi)
+        x = randn(rows, 64, seed=1)
+        x[:lo], x[hi:] = float("nan"), float("inf")
+        case(rows, 64, 8, ptr=ptr, x=x)
+
+
+def test_empty_samples_and_none():
+    case(300, 32, 4, ptr=[0, 0, 0, 300, 300, 300])
+    case(30000, 32, 4, ptr=[0, 0, 20000, 20000, 30000, 30000])
+    x = torch.empty(0, 32, device="cuda")
+    g = randn(32)
+    y, st = mgn.mgn_group_norm_forward(x, 4, gamma=g, beta=g, samples=3, eps=EPS, save=True)
+    assert y.shape == (0, 32) and (st[..., 0] == 0).all() and torch.allclose(st[..., 1], torch.tensor(EPS ** -0.5, device="cuda"))
+    r = mgn.mgn_group_norm_backward(x, st, x, 4, gamma=g, beta=g, samples=3, eps=EPS)
+    assert (r.dgamma == 0).all() and (r.dbeta == 0).all()
+    # no samples at all: rows outside
+    x, ptr = randn(10, 32), torch.zeros(1, dtype=torch.int32, device="cuda")
+    y, st = mgn.mgn_group_norm_forward(x, 4, sample_ptr=ptr, save=True, y=dirty(10, 32))
+    assert torch.isnan(y).all() and st.shape == (0, 4, 2)
+    r = mgn.mgn_group_norm_backward(x, st, x, 4, gamma=g, sample_ptr=ptr, dx=dirty(10, 32))
+    assert torch.isnan(r.dx).all() and (r.dgamma == 0).all()
+
+
+@pytest.mark.parametrize("rows", [60, 30000])
+def test_far_mean(rows):
+    """A mean a thousand times the deviation: the statistics keep it."""
+    case(rows, 32, 4, shift=1000.0, seed=2)
+
+
+@pytest.mark.parametrize("rows", [60, 30000])
+def test_not_finite(rows):
+    """An infinity or a NaN reaches its sample's group and no other."""
+    x = randn(rows, 32, seed=1)
+    x[rows // 3, 9], x[rows - 1, 30] = float("inf"), float("nan")
+    y, st = mgn.mgn_group_norm_forward(x, 4, samples=2, act="silu", save=True)
+    bad = torch.zeros(2, 4, dtype=torch.bool, device="cuda")
+    bad[0, 1], bad[1, 3] = True, True
+    assert torch.equal(torch.isnan(st[..., 1]) | torch.isnan(st[..., 0]) | torch.isinf(st[..., 0]), bad)
+    want = bad.repeat_interleave(rows // 2, 0).repeat_interleave(8, 1)
+    assert torch.isfinite(y[~want]).all() and torch.isnan(y[want]).all()
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("rows", [70, 20000])
+def test_strides_and_in_place(rows, dtype):
+    cols = 75
+    big = dirty(rows + 2, cols + 9, dtype=T[dtype])
+    x = big[1:-1, 3:3 + cols]
+    x.copy_(randn(rows, cols, seed=1))
+    plain = x.contiguous()
+    g, b = randn(cols, seed=2), randn(cols, seed=3)
+    with_ = dict(gamma=g, beta=b, act="silu", samples=2)
+    y, st = mgn.mgn_group_norm_forward(plain, 5, save=True, **with_)
+    dy = randn(rows, cols, seed=4).to(T[dtype])
+    r = mgn.mgn_group_norm_backward(plain, st, dy, 5, **with_)
+    dbig = dirty(rows, cols + 1, dtype=T[dtype])
+    dbig[:, :cols] = dy
+    r2 = mgn.mgn_group_norm_backward(x, st, dbig[:, :cols], 5, dx=dbig[:, :cols], **with_)  # dx in dy's place
+    assert all(torch.equal(p, q) for p, q in zip(r, r2)) and torch.isnan(dbig[:, cols].float()).all()
+    assert torch.equal(x, plain)
+    keep = x.clone()
+    r3 = mgn.mgn_group_norm_backward(x, st, dy, 5, dx=x, **with_)  # in x's
+    assert torch.equal(r3.dx, r.dx)
+    x.copy_(keep)
+    y2, _ = mgn.mgn_group_norm_forward(x, 5, y=x, **with_)
+    assert torch.equal(y2, y)
+    assert torch.isnan(big[0].float()).all() and torch.isnan(big[-1].float()).all()
+    assert torch.isnan(big[:, :3].float()).all() and torch.isnan(big[:, 3 + cols:].float()).all()
+
+
+@pytest.mark.parametrize("rows", [70, 20000])
+def test_gradients_added_and_absent(rows):
+    x, dy, g, b = randn(rows, 48), randn(rows, 48, seed=1), randn(48, seed=2), randn(48, seed=3)
+    with_ = dict(gamma=g, beta=b, act="silu")
+    _, st = mgn.mgn_group_norm_forward(x, 6, save=True, **with_)
+    r = mgn.mgn_group_norm_backward(x, st, dy, 6, **with_)
+    again = mgn.mgn_group_norm_backward(x, st, dy, 6, grads=r._replace(dgamma=r.dgamma.clone(), dbeta=r.dbeta.clone()), **with_)
+    assert torch.allclose(again.dgamma, 2 * r.dgamma) and torch.allclose(again.dbeta, 2 * r.dbeta)
+    only = mgn.mgn_group_norm_backward(x, st, dy, 6, gamma=g, beta=b, act="silu", grads=mgn.GroupNormGrads(None, None, torch.zeros(48, device="cuda")))
+    assert only.dgamma is None and torch.equal(only.dbeta, r.dbeta) and torch.equal(only.dx, r.dx)
+
+
+def test_against_differences():
+    """The gradients against central differences of the forward in 64 bits (the oracle's)."""
+    rows, cols, groups, spans = 12, 12, 3, [(0, 5), (5, 12)]
+    g = np.random.default_rng(0)
+    x, dy, gamma, beta = g.normal(size=(rows, cols)), g.normal(size=(rows, cols)), g.normal(size=cols), g.normal(size=cols)
+
+    def loss(x, gamma, beta):
+        return (oracle(x, None, gamma, beta, groups, "silu", spans)["y"] * dy).sum()
+    d = [torch.tensor(v, dtype=torch.float32, device="cuda") for v in (x, dy, gamma, beta)]
+    ptr = torch.tensor([0, 5, 12], dtype=torch.int32, device="cuda")
+    _, st = mgn.mgn_group_norm_forward(d[0], groups, d[2], d[3], "silu", sample_ptr=ptr, save=True, eps=EPS)
+    r = mgn.mgn_group_norm_backward(d[0], st, d[1], groups, d[2], d[3], "silu", sample_ptr=ptr, eps=EPS)
+    h = 1e-5
+    for got, k in ((r.dx, 0), (r.dgamma, 1), (r.dbeta, 2)):
+        v = [x, gamma, beta]
+        ref = np.zeros_like(v[k])
+        for i in np.ndindex(ref.shape):
+            e = np.zeros_like(ref)
+            e[i] = h
+            ref[i] = (loss(*[w + (e if j == k else 0) for j, w in enumerate(v)]) -
+                      loss(*[w - (e if j == k else 0) for j, w in enumerate(v)])) / (2 * h)
+        # the differences' own error h^2 and 2^-52 / h, and float32 inputs
+        assert np.abs(got.cpu().numpy() - ref).max() <= 1e-5 * max(1, np.abs(ref).max())
+
+
+def test_far_offsets():
+    """Rows whose elements lie past 2^31."""
+    rows, cols = 5000, 32
+    wide = torch.empty(rows, 1 << 19, device="cuda")[:, 11:11 + cols]
+    x = randn(rows, cols)
+    wide.copy_(x)
+    y, st = mgn.mgn_group_norm_forward(x, 4, act="silu", samples=5, save=True)
+    y2, st2 = mgn.mgn_group_norm_forward(wide, 4, act="silu", samples=5, save=True)
+    assert torch.equal(y, y2) and torch.equal(st, st2)
+    assert torch.equal(mgn.mgn_group_norm_backward(wide, st, y, 4, act="silu", samples=5, dx=wide).dx,
+                       mgn.mgn_group_norm_backward(x, st, y, 4, act="silu", samples=5).dx)
+
+
+def test_refusals():
+    x, g = randn(12, 32), randn(32)
+    ptr = torch.tensor([0, 12], dtype=torch.int32, device="cuda")
+    _, st = mgn.mgn_group_norm_forward(x, 4, save=True)
+    F, B = mgn.mgn_group_norm_forward, mgn.mgn_group_norm_backward
+    for f in (lambda: F(x, 5), lambda: F(x, 0), lambda: F(x, 4, act="gelu"), lambda: F(x, 4, samples=5), lambda: F(x.half(), 4),
+              lambda: F(x.cpu(), 4), lambda: F(x, 4, gamma=g[:31]), lambda: F(x, 4, sample_ptr=ptr.long()), lambda: F(x, 4, sample_ptr=ptr.cpu()),
+              lambda: F(x, 4, samples=2, sample_ptr=ptr), lambda: F(x, 4, sample_ptr=ptr[:0]), lambda: F(x, 4, y=x.bfloat16()),
+              lambda: F(x, 4, eps=0.0), lambda: F(x[:, ::2], 4), lambda: B(x, st[:, :3], x, 4), lambda: B(x, st, None, 4),
+              lambda: B(x, st, x[:5], 4), lambda: B(x, st, x, 4, grads=mgn.GroupNormGrads(None, g, None)), lambda: F(x, 4, samples=0)):
+        with pytest.raises(mgn.MgnError):
+            f()
+
+
+def test_reproducible_streams_and_graphs():
+    """With a call on one stream and in a graph, each with a workspace of its own."""
+    x, dy, g, b = randn(20000, 96), randn(20000, 96, seed=1), randn(96, seed=2), randn(96, seed=3)
+    ptr = torch.tensor(ragged(20000, 6, 1), dtype=torch.int32, device="cuda")
+    with_ = dict(gamma=g, beta=b, act="silu", sample_ptr=ptr)
+
+    def step(stream=None):
+        y, st = mgn.mgn_group_norm_forward(x, 8, save=True, stream=stream, **with_)
+        return [y, st, *mgn.mgn_group_norm_backward(x, st, dy, 8, stream=stream, **with_)]
+    ref = step()
+    for _ in range(3):
+        assert all(torch.equal(p, q) for p, q in zip(step(), ref))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got = step(side)
+    side.synchronize()
+    assert all(torch.equal(p, q) for p, q in zip(got, ref))
+    with torch.cuda.stream(side):
+        step()
+    side.synchronize()
+    first, second = torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(first):
+        one = step()
+    with torch.cuda.graph(second):
+        two = step()
+    for k in range(4):
+        x.copy_(randn(20000, 96, seed=30 + k))
+        want = step()
+        torch.cuda.synchronize()
+        first.replay()
+        second.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(p, q) for p, q in zip(one, want)), k
+        assert all(torch.equal(p, q) for p, q in zip(two, want)), k
+
+
+@pytest.mark.parametrize("rows,width,hidden", [(1, 128, 256), (300, 128, 512), (20000, 128, 160)])
+def test_layer_of_all(rows, width, hidden):
+    """A step as a model runs it: group norm with SiLU, a 4-bit layer, its reverse, the
+    gradients' norm and clipping, an update; against the same in 64 bits on the numbers
+    that the quantiser gave."""
+    x, w, dy = randn(rows, width, seed=1), randn(hidden, width, seed=2) / width ** 0.5, randn(rows, hidden, seed=3)
+    g, b, bias = 1 + 0.1 * randn(width, seed=4), 0.1 * randn(width, seed=5), randn(hidden, seed=6)
+    with_ = dict(gamma=g, beta=b, act="silu", samples=1, eps=EPS)
+    h, st = mgn.mgn_group_norm_forward(x, 8, save=True, **with_)
+    hq, wq = mgn.mgn_quant4(h, transposed=True), mgn.mgn_quant4(w, transposed=True)
+    y = mgn.mgn_matmul4(hq.rows, wq.rows, bias=bias)
+    dq = mgn.mgn_quant4(dy, transposed=True, colsum=True)
+    dh = mgn.mgn_matmul4(dq.rows, wq.columns)
+    dw = mgn.mgn_matmul4(dq.columns, hq.columns)
+    r = mgn.mgn_group_norm_backward(x, st, dh, 8, **with_)
+    grads = [dw.view(-1), dq.colsum, r.dgamma, r.dbeta]
+    n = sum(t.numel() for t in grads)
+    flat = torch.empty(n, device="cuda")
+    norm = mgn.mgn_grad_clip(mgn.TensorList(grads, list(flat.split([t.numel() for t in grads]))), 1.0)
+    p, m, v = torch.zeros(n, device="cuda"), torch.zeros(n, device="cuda"), torch.zeros(n, device="cuda")
+    mgn.mgn_adam_step(mgn.Adam(), 1, p, flat, m, v)
+
+    val = {k: mgn.mgn_dequant4(q).double() for k, q in (("h", hq.rows), ("ht", hq.columns), ("w", wq.rows), ("wt", wq.columns),
+                                                        ("d", dq.rows), ("dt", dq.columns))}
+
+    def close(got, a, c, terms, plus=None):
+        ref, mag = a @ c, a.abs() @ c.abs()
+        ref, mag = (ref, mag) if plus is None else (ref + plus.double(), mag + plus.double().abs())
+        assert ((got.double() - ref).abs() <= (terms / 32 + 26) * 2 * U * mag).all()
+    close(y, val["h"], val["w"].t(), width, bias)
+    close(dh, val["d"], val["wt"].t(), hidden)
+    close(dw, val["dt"], val["ht"].t(), rows)
+    ref = oracle(x.double().cpu().numpy(), dh.double().cpu().numpy(), g.double().cpu().numpy(), b.double().cpu().numpy(), 8, "silu",
+                 [(0, rows)])
+    near(h, ref["y"], ref["ty"], "h")
+    near(r.dx, ref["dx"], ref["tdx"], "dx")
+    total = float(sum((t.double() ** 2).sum() for t in grads)) ** 0.5
+    assert abs(float(norm) - total) <= 1.01 * U * total
+    want = torch.cat([t.double() for t in grads]) * min(1.0, 1.0 / total)
+    assert ((flat.double() - want).abs() <= 1.01 * U * want.abs() + 2.0 ** -149).all()
+    assert torch.isfinite(p).all()
