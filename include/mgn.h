@@ -551,7 +551,7 @@ int mgn_norm_gate_backward(const mgn_norm_gate* op, mgn_rows x, mgn_rows b,
 typedef struct mgn_mat4 {
   const uint8_t* q;
   const uint8_t* scale;
-  int64_t rows, cols, ld; /* ld in bytes */
+  int64_t rows, cols, ld; /* ld in bytes, under 2^28 */
 } mgn_mat4;
 
 /* Quantises x [rows][cols] (MGN_FP32 or MGN_BF16).  The scale X of 32 columns is the

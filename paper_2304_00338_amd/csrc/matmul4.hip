@@ -13,6 +13,8 @@
 // the first operand (i), a's the second (j), so a lane's results belong to one row of a
 // and to runs of 4 consecutive columns of c: result r is row 8 (r / 4) + 4 (l >> 5) +
 // r % 4 of the 32.
+#include <cmath>
+
 #include "dev_common.hpp"
 #include "product_io.hpp"
 #include "row_ops.hpp"
@@ -32,30 +34,45 @@ struct Job4 {
 
 __device__ __forceinline__ i32x8 operand(uint4 v) { return i32x8{(int)v.x, (int)v.y, (int)v.z, (int)v.w, 0, 0, 0, 0}; }
 
+// 16 bytes past the caches: results that stay in L2 push out the operands (32,768 x 4096 x
+// 1024 to fp32 170 us, through L2 208; 852,640 x 128 x 256 to fp32 121, 144).
+__device__ __forceinline__ void store16(void* p, uint4 v) {
+  typedef uint32_t u32x4 __attribute__((ext_vector_type(4), aligned(2)));
+  __builtin_nontemporal_store(u32x4{v.x, v.y, v.z, v.w}, (u32x4*)p);
+}
+
 // ---- tiles: BM x BN of c a block of WM x WN waves, each TM x TN times 32 x 32.
 //
-// Steps of 128 columns (64 bytes of a row) go through four LDS buffers by loads that
-// write LDS themselves, three steps ahead, the rows' scales (4 bytes a row and step)
+// Steps of 128 columns (64 bytes of a row) go through NB LDS buffers by loads that
+// write LDS themselves, NB - 1 steps ahead, the rows' scales (4 bytes a row and step)
 // with them.  A row's 16-byte chunk c sits at place c ^ (row / 4 % 4), so that 16
 // rows of a fragment read cover all 64 banks; the lanes' source addresses are permuted
 // to match.  A step has two halves of 64 columns, and a half's fragments are read under
 // the products of the half before it.  The barrier of a step lies between its halves: there
 // a wave has read all of the step, whose buffer may be filled again, and waited for its own
 // loads of the next one.
-template <int WM, int WN, int TM, int TN, int OCC>
-__global__ void __launch_bounds__(WM * WN * 64, OCC) k_matmul4_tile(Job4 J) {
-  constexpr int NB = 4;
+//
+// Measured: 32,768 x 4096 x 4096 to bf16 297 to 306 us (3.7 PFLOP/s; the library's
+// product of such matrices takes 531, and reaches 3.6 at 16,384 each way).  Power
+// bounds it: 1024 of a step's 1520 cycles are products, but at 1.5 GHz on random
+// numbers (2.2 on zeros: 0.71 us a step instead of 1.0; products alone, on what the
+// registers hold, 0.72 and 0.54).  A tile's filling takes 2.4 us, its results 3.6.  With
+// three buffers 128 x 128 has three blocks a CU: 852,640 x 128 x 256 to fp32 106 us (of
+// two blocks 121), 852,640 x 256 x 128 148 (6.3 TB/s).  Four waves of 128 x 128 took 355
+// us instead of 323, loads between the products 321.
+template <int WM, int WN, int TM, int TN, int NB>
+__global__ void __launch_bounds__(WM * WN * 64, TM * TN > 8 ? 1 : 2) k_matmul4_tile(Job4 J) {
   constexpr int BM = WM * TM * 32, BN = WN * TN * 32, NWV = WM * WN, ROWS = BM + BN;
-  constexpr int LA = BM / 16 / NWV, LB = BN / 16 / NWV, LS = ROWS / 64 / NWV;  // loads of a wave and step
+  constexpr int LA = BM / 16 / NWV, LB = BN / 16 / NWV, LS = (ROWS / 64 + NWV - 1) / NWV;  // loads of a wave and step
   constexpr int PER = LA + LB + LS;
-  static_assert(BM % (16 * NWV) == 0 && BN % (16 * NWV) == 0 && ROWS % (64 * NWV) == 0, "as many loads for every wave");
-  static_assert(BM % 64 == 0, "a load of scales is of one operand");
+  static_assert(BM % (16 * NWV) == 0 && BN % (16 * NWV) == 0, "as many loads for every wave");
+  static_assert(BM % 64 == 0 && BN % 64 == 0, "a load of scales is of one operand");
   static_assert(PER * (NB - 2) < 63, "the counter of loads holds them");
-  constexpr int CH = TN * 8;  // chunks of 4 columns of a wave's results
-  static_assert(ROWS * 64 >= NWV * 32 * CH * 16 / 2, "results fit two buffers");
   // arrays of their own, so that a read waits for the loads of its buffer and no others
   constexpr int BYTES = ROWS * 68;  // 64 of numbers for each row, then 4 of scales
-  __shared__ __align__(16) uint8_t b0[BYTES], b1[BYTES], b2[BYTES], b3[BYTES];
+  static_assert(NB == 3 || NB == 4, "buffers");
+  __shared__ __align__(16) uint8_t b0[BYTES], b1[BYTES], b2[BYTES], b3[NB > 3 ? BYTES : 16];
+  uint8_t* const bufs[4] = {b0, b1, b2, b3};
   const Matmul4& p = J.p;
   const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), j = l & 31, h = l >> 5;
   const int wm = w / WN, wn = w % WN;
@@ -72,27 +89,31 @@ __global__ void __launch_bounds__(WM * WN * 64, OCC) k_matmul4_tile(Job4 J) {
   const int64_t kb0 = split * J.per, kb1 = min(kb0 + J.per, J.kb), steps = kb1 - kb0;
   const int64_t end = (p.a.cols + 31) / 32 * 16;  // bytes of a row
 
-  // Loads: wave w takes 16 rows from 16 (i NWV + w) on, a lane 16 bytes of one, at an
-  // address that moves on by 64 bytes a step.  A row that is not there is the last one
-  // again (its results are not stored).  Chunks behind the columns are the last one
-  // again: their numbers, which are finite, count for nothing, since the scales there
-  // are 2^-127 in both operands.
+  // Loads: wave w takes 16 rows from 16 (i NWV + w) on, a lane 16 bytes of one: a scalar
+  // base, which moves on by 64 bytes a step, and a 32-bit offset.  A row that is not there
+  // is the last one again (its results are not stored).  Chunks behind the columns are the
+  // last one again: their numbers, which are finite, count for nothing, since the scales
+  // there are 2^-127 in both operands.
   const int lrow = l >> 2, lchunk = ((l & 3) ^ ((l >> 4) & 3)) * 16;
   const uint8_t *src[LA + LB], *ssrc[LS];
-#pragma unroll
-  for (int i = 0; i < LA + LB; ++i) {
-    const int row = (i < LA ? i * NWV + w : (i - LA) * NWV + w) * 16 + lrow;
-    src[i] = (i < LA ? p.a.q + min(m0 + row, p.a.rows - 1) * p.a.ld : p.b.q + min(n0 + row, p.b.rows - 1) * p.b.ld) +
-             kb0 * 64 + lchunk;
-  }
+  uint32_t off[LA + LB], soff[LS];
   int64_t sstep[LS];
 #pragma unroll
+  for (int i = 0; i < LA + LB; ++i) {
+    const bool isa = i < LA;
+    const int64_t last = (isa ? p.a.rows : p.b.rows) - 1, ld = isa ? p.a.ld : p.b.ld;
+    const int64_t row = min(isa ? m0 + (i * NWV + w) * 16 : n0 + ((i - LA) * NWV + w) * 16, last);
+    src[i] = (isa ? p.a.q : p.b.q) + row * ld + kb0 * 64;
+    off[i] = (uint32_t)min((int64_t)lrow, last - row) * (uint32_t)ld + lchunk;
+  }
+#pragma unroll
   for (int i = 0; i < LS; ++i) {
-    const int row = (i * NWV + w) * 64;
-    const bool isa = row < BM;
-    const int64_t rows = isa ? p.a.rows : p.b.rows, r = min((isa ? m0 + row : n0 + row - BM) + l, rows - 1);
+    const int at = (i * NWV + w) % (ROWS / 64) * 64;  // some twice, where the waves are more
+    const bool isa = at < BM;
+    const int64_t rows = isa ? p.a.rows : p.b.rows, row = min(isa ? m0 + at : n0 + at - BM, rows - 1);
     sstep[i] = rows * 4;
-    ssrc[i] = (isa ? p.a.scale : p.b.scale) + (kb0 * rows + r) * 4;
+    ssrc[i] = (isa ? p.a.scale : p.b.scale) + (kb0 * rows + row) * 4;
+    soff[i] = (uint32_t)min((int64_t)l, rows - 1 - row) * 4;
   }
   auto to_lds = [&](const uint8_t* from, uint8_t* dst) {
     __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from,
@@ -104,34 +125,36 @@ __global__ void __launch_bounds__(WM * WN * 64, OCC) k_matmul4_tile(Job4 J) {
   };
   int64_t left = end - kb0 * 64;  // bytes of a row from the next step on
   auto fetch = [&](uint8_t* buf) {  // the next step
-    const int back = max(lchunk + 16 - (int)min(left, (int64_t)64), 0);
+    const uint32_t back = max(lchunk + 16 - (int)min(left, (int64_t)64), 0);
 #pragma unroll
     for (int i = 0; i < LA + LB; ++i) {
-      to_lds(src[i] - back, buf + (i < LA ? i * NWV + w : BM / 16 + (i - LA) * NWV + w) * 1024);
+      asm volatile("" : "+s"(src[i]));  // else the addresses of several steps are kept, and spill
+      to_lds(src[i] + (off[i] - back), buf + (i < LA ? i * NWV + w : BM / 16 + (i - LA) * NWV + w) * 1024);
       src[i] += 64;
     }
 #pragma unroll
     for (int i = 0; i < LS; ++i) {
-      to_lds4(ssrc[i], buf + ROWS * 64 + (i * NWV + w) * 256);
+      asm volatile("" : "+s"(ssrc[i]));
+      to_lds4(ssrc[i] + soff[i], buf + ROWS * 64 + (i * NWV + w) % (ROWS / 64) * 256);
       ssrc[i] += sstep[i];
     }
     left -= 64;
   };
   f32x16 acc[TM][TN] = {};
-  int off[2];
+  int at[2];
 #pragma unroll
-  for (int s = 0; s < 2; ++s) off[s] = j * 64 + (((2 * s + h) ^ ((j >> 2) & 3)) * 16);
+  for (int s = 0; s < 2; ++s) at[s] = j * 64 + (((2 * s + h) ^ ((j >> 2) & 3)) * 16);
   struct Half {
     uint4 a[TM], b[TN];
   } f0, f1;
   struct Scales {
     uint32_t a[TM], b[TN];
-  } s0, s1;  // of even and odd steps
+  } sc[2];  // of even and odd steps
   auto read = [&](Half& f, const uint8_t* buf, int s) {
 #pragma unroll
-    for (int n = 0; n < TN; ++n) f.b[n] = *(const uint4*)(buf + (BM + (wn * TN + n) * 32) * 64 + off[s]);
+    for (int n = 0; n < TN; ++n) f.b[n] = *(const uint4*)(buf + (BM + (wn * TN + n) * 32) * 64 + at[s]);
 #pragma unroll
-    for (int m = 0; m < TM; ++m) f.a[m] = *(const uint4*)(buf + (wm * TM + m) * 2048 + off[s]);
+    for (int m = 0; m < TM; ++m) f.a[m] = *(const uint4*)(buf + (wm * TM + m) * 2048 + at[s]);
   };
   auto read_scales = [&](Scales& x, const uint8_t* buf) {
     const uint32_t* scl = (const uint32_t*)(buf + ROWS * 64);
@@ -189,51 +212,134 @@ __global__ void __launch_bounds__(WM * WN * 64, OCC) k_matmul4_tile(Job4 J) {
     products(f1, x, std::integral_constant<int, 2>());
   };
   if (steps > 0) {
-    fetch(b0);
-    if (steps > 1) fetch(b1);
-    if (steps > 2) fetch(b2);
-    if (steps > 2)
+#pragma unroll
+    for (int u = 0; u < NB - 1; ++u)
+      if (u < steps) fetch(bufs[u]);
+    if (steps >= NB - 1)
       arrived(std::integral_constant<int, NB - 2>());
     else
       arrived(std::integral_constant<int, 0>());
     meet();
     read(f0, b0, 0);
-    read_scales(s0, b0);
+    read_scales(sc[0], b0);
     int64_t i = 0;
-    for (; i + 2 * NB - 1 <= steps; i += NB) {
-      step(std::true_type(), i, b0, b3, b1, s0, s1);
-      step(std::true_type(), i + 1, b1, b0, b2, s1, s0);
-      step(std::true_type(), i + 2, b2, b1, b3, s0, s1);
-      step(std::true_type(), i + 3, b3, b2, b0, s1, s0);
+    constexpr int UN = NB % 2 ? 2 * NB : NB;  // steps after which buffers and scales are the same again
+    for (; i + UN + NB - 1 <= steps; i += UN) {
+#pragma unroll
+      for (int u = 0; u < UN; ++u)
+        step(std::true_type(), i + u, bufs[u % NB], bufs[(u + NB - 1) % NB], bufs[(u + 1) % NB], sc[u & 1], sc[(u + 1) & 1]);
     }
-    for (; i < steps; i += NB) {
-      step(std::false_type(), i, b0, b3, b1, s0, s1);
-      if (i + 1 < steps) step(std::false_type(), i + 1, b1, b0, b2, s1, s0);
-      if (i + 2 < steps) step(std::false_type(), i + 2, b2, b1, b3, s0, s1);
-      if (i + 3 < steps) step(std::false_type(), i + 3, b3, b2, b0, s1, s0);
+    for (; i < steps; i += UN) {
+#pragma unroll
+      for (int u = 0; u < UN; ++u)
+        if (i + u < steps)
+          step(std::false_type(), i + u, bufs[u % NB], bufs[(u + NB - 1) % NB], bufs[(u + 1) % NB], sc[u & 1], sc[(u + 1) & 1]);
     }
   }
   __syncthreads();  // every wave has read its last operands
-  // rows of CH chunks of 4 columns, chunk c at place c ^ row
-  f32x4* mine = (f32x4*)(w < NWV / 2 ? b0 : b1) + w % (NWV / 2) * 32 * CH;
-#pragma unroll
-  for (int m = 0; m < TM; ++m) {
+  // The results go through the wave's own piece of LDS to be stored as whole rows, a
+  // bf16 c as bf16 and all at once.
+  constexpr int PIECE = TM * TN * 2048;
+  static_assert(NB * (BYTES / PIECE) >= NWV, "a piece for each wave");
+  const int of = w / (BYTES / PIECE);
+  uint8_t* const piece = (of == 0 ? b0 : of == 1 ? b1 : of == 2 ? b2 : b3) + w % (BYTES / PIECE) * PIECE;
+  const int64_t mw = m0 + wm * TM * 32, nw = n0 + wn * TN * 32;
+  const bool raw = J.splits > 1, plain = raw || (p.ep.act != MGN_ACT_RELU_GRAD && !p.ep.accumulate);
+  if (plain && !raw) {
 #pragma unroll
     for (int n = 0; n < TN; ++n)
 #pragma unroll
-      for (int g = 0; g < 4; ++g)
-        mine[j * CH + ((n * 8 + 2 * g + h) ^ (j & (CH - 1)))] =
-            f32x4{acc[m][n][4 * g], acc[m][n][4 * g + 1], acc[m][n][4 * g + 2], acc[m][n][4 * g + 3]};
+      for (int g = 0; g < 4; ++g) {
+        const int64_t col = nw + n * 32 + 8 * g + 4 * h;
+        f32x4 bias = {0.f, 0.f, 0.f, 0.f};
+        if (p.ep.bias != nullptr) bias = load4(p.ep.bias + col, (int)min(max(p.b.rows - col, (int64_t)0), (int64_t)4));
+#pragma unroll
+        for (int m = 0; m < TM; ++m)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float v = p.ep.bias != nullptr ? acc[m][n][4 * g + e] + bias[e] : acc[m][n][4 * g + e];
+            acc[m][n][4 * g + e] = p.ep.act == MGN_ACT_RELU && v < 0.f ? 0.f : v;  // a NaN stays
+          }
+      }
+  }
+  if (plain && !raw && p.c_type == MGN_BF16) {
+    // rows of TN * 4 chunks of 8 columns, chunk c at place c ^ row
+    constexpr int CH = TN * 4;
+    static_assert(TM * 32 * CH * 16 <= PIECE, "the wave's results fit");
+#pragma unroll
+    for (int m = 0; m < TM; ++m)
+#pragma unroll
+      for (int n = 0; n < TN; ++n)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const bf16 v[4] = {(bf16)acc[m][n][4 * g], (bf16)acc[m][n][4 * g + 1], (bf16)acc[m][n][4 * g + 2],
+                             (bf16)acc[m][n][4 * g + 3]};
+          __builtin_memcpy(piece + (m * 32 + j) * CH * 16 + ((n * 4 + g) ^ (j & (CH - 1))) * 16 + 8 * h, v, 8);
+        }
     wave_lds_sync();
-    constexpr int LPR = CH / 2;  // lanes of a row
-    const int c = l % LPR * 2;
-    const int64_t n = n0 + wn * TN * 32 + c * 4;
+    const int c = l % CH;
+    const int64_t n = nw + c * 8;
+    bf16* to = (bf16*)p.c + mw * p.ldc + n;
+#pragma unroll
+    for (int i = 0; i < TM * 32; i += 64 / CH) {
+      const int r = i + l / CH;
+      const uint4 v = *(const uint4*)(piece + r * CH * 16 + (c ^ (r & (CH - 1))) * 16);
+      if (mw + r < p.a.rows) {
+        if (n + 8 <= p.b.rows) {
+          store16(to + r * p.ldc, v);
+        } else {
+          const uint32_t u[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (n + e < p.b.rows) to[r * p.ldc + e] = __builtin_bit_cast(bf16, (uint16_t)(u[e >> 1] >> (16 * (e & 1))));
+        }
+      }
+    }
+    return;
+  }
+  // rows of TN * 8 chunks of 4 columns, chunk c at place c ^ row, MR times 32 of them at a time
+  constexpr int CH = TN * 8, MR = PIECE / (32 * CH * 16) < TM ? PIECE / (32 * CH * 16) : TM;
+  static_assert(MR >= 1 && TM % MR == 0, "whole rounds");
+  f32x4* const mine = (f32x4*)piece;
+  float* const out = raw ? p.part + (int64_t)split * p.a.rows * p.b.rows : (float*)p.c;
+  const int64_t ldo = raw ? p.b.rows : p.ldc;
+#pragma unroll
+  for (int m = 0; m < TM; m += MR) {
+#pragma unroll
+    for (int q = 0; q < MR; ++q)
+#pragma unroll
+      for (int n = 0; n < TN; ++n)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const f32x16& v = acc[m + q][n];
+          mine[(q * 32 + j) * CH + ((n * 8 + 2 * g + h) ^ (j & (CH - 1)))] =
+              f32x4{v[4 * g], v[4 * g + 1], v[4 * g + 2], v[4 * g + 3]};
+        }
+    wave_lds_sync();
+    const int c = l % CH;
+    const int64_t n = nw + c * 4;
+    const int k = (int)min(p.b.rows - n, (int64_t)4);
+    if (plain) {
+#pragma unroll
+      for (int i = 0; i < MR * 32; i += 64 / CH) {
+        const int r = i + l / CH;
+        const int64_t row = mw + m * 32 + r;
+        const f32x4 v = mine[r * CH + (c ^ (r & (CH - 1)))];
+        if (row < p.a.rows && k > 0) {
+          if (k == 4)
+            store16(out + row * ldo + n, __builtin_bit_cast(uint4, v));
+          else
+            store4(out + row * ldo + n, v, k);
+        }
+      }
+    } else {
 #pragma unroll 2
-    for (int i = 0; i < 32; i += 64 / LPR) {
-      const int r = i + l / LPR;
-      const int64_t row = m0 + (wm * TM + m) * 32 + r;
-      const f32x4 v = mine[r * CH + (c ^ (r & (CH - 1)))], u = mine[r * CH + ((c + 1) ^ (r & (CH - 1)))];
-      if (row < p.a.rows && n < p.b.rows) put8(J, split, row, n, v, u);
+      for (int i = 0; i < MR * 32; i += 64 / CH) {
+        const int r = i + l / CH;
+        const int64_t row = mw + m * 32 + r;
+        const f32x4 v = mine[r * CH + (c ^ (r & (CH - 1)))];
+        if (row < p.a.rows && k > 0) finish(p, row, n, v);
+      }
     }
     wave_lds_sync();
   }
@@ -323,7 +429,7 @@ using namespace dev;
 
 namespace {
 
-constexpr int64_t kCUs = 256;
+constexpr int64_t kCUs = 256, kFewRows = 64;
 
 enum { kFew, kSmallTile, kBigTile };
 struct Plan {
@@ -332,25 +438,41 @@ struct Plan {
   int splits;
 };
 
-constexpr int64_t kFewRows = 32;
+// Which kernel, and into how many parts the sums are split: the least of what these
+// take by a model of their times (us), fitted to calls in a graph:
+//  * few rows: 3 and what all blocks read (their 16 rows of b, and a each) at 6.2 TB/s
+//    (1 x 4096 x 4096 4.2, 32 x 4096 x 4096 6.4, 64 x 4096 x 4096 9.0, tiles 12.5; 64 x
+//    8192 x 8192 27, tiles 16.7);
+//  * tiles of 128 x 128: 1.4 a tile of a CU and 0.31 a step and tile where all CUs have
+//    two or more, else 0.34 to 0.54 a step (2048 x 2048 x 2048 11.9, of 256 x 256 17.9);
+//    sums split into s parts add a launch and 8 s bytes a result (512 x 512 x 20,000 whole
+//    67, in 4, 8 and 32 parts 21.8, 17.5, 26.6);
+//  * tiles of 256 x 256: 7 and 0.98 a step for every 256 of them (4096 x 4096 x 4096 42,
+//    of 128 x 128 51; 32,768 x 4096 x 1024 144, 125).
 Plan plan(int64_t m, int64_t n, int64_t k) {
-  Plan r;
-  const int64_t kb = ceil_div(k, 128);
-  int64_t want;
-  if (m <= kFewRows) {
-    r.kind = kFew;
-    r.mt = 1;
-    r.nt = ceil_div(n, 16);
-    want = std::min(kCUs / std::max<int64_t>(r.nt, 1), kb / 32);
-  } else {
-    const int64_t m2 = ceil_div(m, 256), n2 = ceil_div(n, 256), m1 = ceil_div(m, 128), n1 = ceil_div(n, 128);
-    const bool big = m2 * n2 >= kCUs * 3 / 4 && kb >= 8 && 4 * m2 * n2 * 7 <= m1 * n1 * 8;
-    r.kind = big ? kBigTile : kSmallTile;
-    r.mt = big ? m2 : m1;
-    r.nt = big ? n2 : n1;
-    want = big ? 1 : std::min(2 * kCUs / (r.mt * r.nt), kb / 4);
+  const int64_t kb = ceil_div(k, 128), m1 = ceil_div(m, 128), n1 = ceil_div(n, 128), m2 = ceil_div(m, 256),
+                n2 = ceil_div(n, 256);
+  Plan r = {kSmallTile, m1, n1, 0, 1};
+  double best = 1e30;
+  for (int64_t s = 1; s <= 512 && (s == 1 || 2 * s <= kb); s *= 2) {
+    const double blocks = (double)m1 * n1 * s, rounds = std::ceil(blocks / kCUs);
+    const double step = blocks <= kCUs ? 0.34 * std::max(1.0, blocks / 160) : 0.31 * rounds;
+    const double t = 2.5 + 1.4 * rounds + step * ceil_div(kb, s) + (s > 1 ? 3.5 + 8e-6 / 4 * s * m * n : 0.0);
+    if (t < best) {
+      best = t;
+      r.splits = (int)s;
+    }
   }
-  r.splits = (int)std::max<int64_t>(want, 1);
+  const double big = (7 + 0.98 * kb) * std::ceil((double)m2 * n2 / kCUs);
+  if (big < best) {
+    best = big;
+    r = {kBigTile, m2, n2, 0, 1};
+  }
+  if (m <= kFewRows) {
+    const int64_t rows = m <= 16 ? 16 : m <= 32 ? 32 : 64, nt = ceil_div(n, 16);
+    if (3 + (double)nt * (rows + 16) * k / 2 / 6.2e6 < best)
+      r = {kFew, 1, nt, 0, (int)std::max<int64_t>(std::min(kCUs / std::max<int64_t>(nt, 1), kb / 32), 1)};
+  }
   r.per = std::max<int64_t>(ceil_div(kb, r.splits), 1);
   r.splits = (int)std::max<int64_t>(ceil_div(kb, r.per), 1);
   return r;
@@ -373,12 +495,14 @@ hipError_t launch_matmul4(const Matmul4& p, hipStream_t s) {
     g.z = (unsigned)r.splits;
     if (p.a.rows <= 16)
       hipLaunchKernelGGL((k_matmul4_few<1>), g, dim3(512), 0, s, J);
-    else
+    else if (p.a.rows <= 32)
       hipLaunchKernelGGL((k_matmul4_few<2>), g, dim3(512), 0, s, J);
+    else
+      hipLaunchKernelGGL((k_matmul4_few<4>), g, dim3(512), 0, s, J);
   } else if (r.kind == kBigTile) {
-    hipLaunchKernelGGL((k_matmul4_tile<2, 4, 4, 2, 2>), grid, dim3(512), 0, s, J);
+    hipLaunchKernelGGL((k_matmul4_tile<2, 4, 4, 2, 4>), grid, dim3(512), 0, s, J);
   } else {
-    hipLaunchKernelGGL((k_matmul4_tile<2, 2, 2, 2, 2>), grid, dim3(256), 0, s, J);
+    hipLaunchKernelGGL((k_matmul4_tile<2, 2, 2, 2, 3>), grid, dim3(256), 0, s, J);
   }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || r.splits == 1) return e;

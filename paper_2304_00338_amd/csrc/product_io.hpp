@@ -88,23 +88,6 @@ __device__ __forceinline__ void put4(const J_& J, int split, int64_t m, int64_t 
     store4(J.p.part + ((int64_t)split * J.p.a.rows + m) * J.p.b.rows + n, v, (int)min(J.p.b.rows - n, (int64_t)4));
 }
 
-// Eight consecutive columns: v and, behind it, u.  A bf16 row goes out 16 bytes at a time.
-template <typename J_>
-__device__ __forceinline__ void put8(const J_& J, int split, int64_t m, int64_t n, f32x4 v, f32x4 u) {
-  const auto& p = J.p;
-  if (J.splits == 1 && p.c_type == MGN_BF16 && p.ep.act == MGN_ACT_NONE && !p.ep.accumulate && n + 8 <= p.b.rows) {
-    if (p.ep.bias != nullptr) {
-      v += load4(p.ep.bias + n, 4);
-      u += load4(p.ep.bias + n + 4, 4);
-    }
-    const bf16 w[8] = {(bf16)v[0], (bf16)v[1], (bf16)v[2], (bf16)v[3], (bf16)u[0], (bf16)u[1], (bf16)u[2], (bf16)u[3]};
-    __builtin_memcpy((bf16*)p.c + m * p.ldc + n, w, sizeof(w));
-    return;
-  }
-  put4(J, split, m, n, v);
-  if (n + 4 < p.b.rows) put4(J, split, m, n + 4, u);
-}
-
 // Sums of the splits, 4 columns a thread: G threads for each, thread g the splits
 // g, g + G, ..., then the G sums in order.
 template <int G, typename J_>
