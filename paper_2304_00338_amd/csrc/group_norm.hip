@@ -3,8 +3,8 @@
 //
 // Rows are cut into tiles of as many rows, whatever samples they belong to, so that
 // ragged samples load the device evenly.  A block takes a tile's rows in columns of whole
-// groups (up to 2048 columns, wider groups in strips), a thread 8 neighbouring columns of
-// every RL-th row.  A launch forms the sums of every piece that a tile and a sample
+// groups (up to 2048 columns in bf16, 1024 in fp32, wider groups in strips), a thread 16
+// neighbouring bytes of every RL-th row.  A launch forms the sums of every piece that a tile and a sample
 // share; tile t's and sample s's lies in slot t + s, which no other pair has, since
 // of two such pairs one has the larger tile or sample and neither the smaller.  A second
 // joins a sample's slots in order, a third reads the rows again and writes the results.
@@ -12,21 +12,25 @@
 // loses (mean / std)^2 2^-53.  Small calls take one block for a sample and group columns
 // instead, in one launch.
 #include "dev_common.hpp"
-#include "row_io.hpp"
 #include "row_ops.hpp"
 
 namespace mgn {
 namespace dev {
 
-constexpr int kStrip = 2048;  // columns that 256 threads hold, 8 each
+// A thread has 16 bytes of a row: so many columns, and so many 256 threads.
+template <typename T>
+struct Run {
+  static constexpr int V = 16 / sizeof(T), strip = 256 * V;
+  typedef T vec __attribute__((ext_vector_type(16 / sizeof(T)), aligned(2)));
+};
 
 struct GnPlan {
   bool whole;    // a block has all rows of a sample
-  int threads;
   int width;     // columns of a block: whole groups
   int cblocks;
-  int64_t tile;  // rows
+  int64_t tile;  // rows of a tile of the sums
   int64_t tiles;
+  int64_t atile, atiles;  // of the results
 };
 
 struct GnJob {
@@ -44,27 +48,56 @@ struct Pair {
   V x, y;
 };
 
-// A thread's place in a strip of columns [c0, c1): runs of 8 columns, the last one moved
+// A thread's place in a strip of columns [c0, c1): runs of V columns, the last one moved
 // to end at c1, so that every load is a whole one; of it the thread has the columns
-// [lo, hi).  Strips of under 8 columns are one run of hi columns.
+// [lo, hi).  Strips of under V columns are one run of hi columns.
+template <typename T>
 struct Cols {
+  static constexpr int V = Run<T>::V;
+  typedef typename Run<T>::vec vec;
   int c0, c1, cl, rl, RL;
   int col, lo, hi;
   bool on;
   __device__ __forceinline__ Cols(int c0, int c1) : c0(c0), c1(c1) {
-    const int CL = (c1 - c0 + 7) >> 3;
+    const int CL = (c1 - c0 + V - 1) / V;
     RL = (int)blockDim.x / CL;
     rl = (int)threadIdx.x / CL;
     cl = (int)threadIdx.x - rl * CL;
     on = rl < RL;
-    col = max(min(c0 + cl * 8, c1 - 8), c0);
-    lo = c0 + cl * 8 - col;
-    hi = min(c1 - c0, 8);
+    col = max(min(c0 + cl * V, c1 - V), c0);
+    lo = c0 + cl * V - col;
+    hi = min(c1 - c0, V);
   }
   __device__ __forceinline__ bool has(int e) const { return e >= lo && e < hi; }
-  template <typename T>
-  __device__ __forceinline__ Raw8<T> load(const mgn_rows& t, int64_t r) const {
-    return load8((const T*)t.data + r * t.ld + col, hi);
+  __device__ __forceinline__ vec load(const mgn_rows& t, int64_t r) const {
+    const T* p = (const T*)t.data + r * t.ld + col;
+    vec v = {};
+    if (hi == V) {
+      v = *(const vec*)p;
+    } else {
+#pragma unroll
+      for (int e = 0; e < V - 1; ++e)
+        if (e < hi) v[e] = p[e];
+    }
+    return v;
+  }
+  // LARGE: the whole is larger than the L2s and goes past them.
+  template <bool LARGE>
+  __device__ __forceinline__ void store(const mgn_rows& t, int64_t r, const float (&f)[V]) const {
+    T* p = (T*)t.data + r * t.ld + col;
+    vec v;
+#pragma unroll
+    for (int e = 0; e < V; ++e) v[e] = (T)f[e];
+    if (hi - lo == V) {
+      if (LARGE)
+        __builtin_nontemporal_store(v, (vec*)p);
+      else
+        *(vec*)p = v;
+    } else {
+#pragma unroll
+      for (int e = 0; e < V; ++e)
+        if (has(e)) p[e] = v[e];
+    }
   }
 };
 
@@ -125,14 +158,15 @@ __device__ __forceinline__ void for_samples(const mgn_group_norm& op, int64_t r0
 }
 
 // Sums over a strip's rows and the columns of each of its groups (d columns) from every
-// thread's eight: put(g, sums) by one thread for each group.  buf: a pair for each of
+// thread's: put(g, sums) by one thread for each group.  buf: a pair for each of
 // the block's threads' columns.  Ends with the block together.
-template <typename V, typename F>
-__device__ __forceinline__ void group_sums(const Cols& at, int d, const V (&s1)[8], const V (&s2)[8], Pair<V>* buf, F put) {
+template <typename T, typename V, typename F>
+__device__ __forceinline__ void group_sums(const Cols<T>& at, int d, const V (&s1)[Run<T>::V], const V (&s2)[Run<T>::V],
+                                           Pair<V>* buf, F put) {
   const int w = at.c1 - at.c0, gs = max(w / d, 1), dw = min(d, w);
   if (at.on) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
+    for (int e = 0; e < Run<T>::V; ++e)
       if (at.has(e)) buf[at.rl * w + at.col - at.c0 + e] = Pair<V>{s1[e], s2[e]};
   }
   __syncthreads();
@@ -159,20 +193,22 @@ __device__ __forceinline__ void group_sums(const Cols& at, int d, const V (&s1)[
 
 // Sums of x and x^2 of rows [r, e).
 template <typename T>
-__device__ __forceinline__ void moments(const mgn_rows& x, const Cols& at, int64_t r, int64_t e, double (&s1)[8], double (&s2)[8]) {
+__device__ __forceinline__ void moments(const mgn_rows& x, const Cols<T>& at, int64_t r, int64_t e, double (&s1)[Run<T>::V],
+                                        double (&s2)[Run<T>::V]) {
+  constexpr int U = 8, V = Run<T>::V;
 #pragma unroll
-  for (int k = 0; k < 8; ++k) s1[k] = s2[k] = 0.0;
+  for (int k = 0; k < V; ++k) s1[k] = s2[k] = 0.0;
   if (!at.on) return;
-  for (int64_t i = r + at.rl; i < e; i += 4 * at.RL) {
-    Raw8<T> v[4];
+  for (int64_t i = r + at.rl; i < e; i += U * at.RL) {
+    typename Run<T>::vec v[U];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) v[u] = at.template load<T>(x, min(i + u * at.RL, e - 1));
+    for (int u = 0; u < U; ++u) v[u] = at.load(x, min(i + u * at.RL, e - 1));
 #pragma unroll
-    for (int u = 0; u < 4; ++u)
+    for (int u = 0; u < U; ++u)
       if (i + u * at.RL < e) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const double f = (double)v[u].get(k);
+        for (int k = 0; k < V; ++k) {
+          const double f = (double)(float)v[u][k];
           s1[k] += f;
           s2[k] = __builtin_fma(f, f, s2[k]);
         }
@@ -187,66 +223,71 @@ __device__ __forceinline__ float2 moments_to_stats(Pair<double> t, double n, flo
 }
 
 // What a thread keeps of its columns.
-struct Vec8 {
-  float v[8];
-  __device__ __forceinline__ Vec8(const float* p, const Cols& at, float other) {
+template <typename T>
+struct Vec {
+  float v[Run<T>::V];
+  __device__ __forceinline__ Vec(const float* p, const Cols<T>& at, float other) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = p != nullptr && at.has(e) ? p[at.col + e] : other;
+    for (int e = 0; e < Run<T>::V; ++e) v[e] = p != nullptr && at.has(e) ? p[at.col + e] : other;
   }
 };
 
 // y of rows [r, e) by the statistics of their sample's groups.
-template <typename T, int ACT, typename S>
-__device__ __forceinline__ void apply(const GnJob& J, const Cols& at, int d, int64_t r, int64_t e, S stats_of) {
+template <typename T, int ACT, bool LARGE, typename S>
+__device__ __forceinline__ void apply(const GnJob& J, const Cols<T>& at, int d, int64_t r, int64_t e, S stats_of) {
+  constexpr int U = 4, V = Run<T>::V;
   if (!at.on) return;
-  const Vec8 gamma(J.a.op.gamma, at, 1.f), beta(J.a.op.beta, at, 0.f);
-  float mean[8], f[8];
+  const Vec<T> gamma(J.a.op.gamma, at, 1.f), beta(J.a.op.beta, at, 0.f);
+  float mean[V], f[V];
 #pragma unroll
-  for (int k = 0; k < 8; ++k) {
+  for (int k = 0; k < V; ++k) {
     const float2 s = at.has(k) ? stats_of((at.col + k) / d) : float2{0.f, 0.f};
     mean[k] = s.x;
     f[k] = s.y * gamma.v[k];
   }
-  for (int64_t i = r + at.rl; i < e; i += 4 * at.RL) {
-    Raw8<T> v[4];
+  for (int64_t i = r + at.rl; i < e; i += U * at.RL) {
+    typename Run<T>::vec v[U];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) v[u] = at.template load<T>(J.a.x, min(i + u * at.RL, e - 1));
+    for (int u = 0; u < U; ++u) v[u] = at.load(J.a.x, min(i + u * at.RL, e - 1));
 #pragma unroll
-    for (int u = 0; u < 4; ++u)
+    for (int u = 0; u < U; ++u)
       if (i + u * at.RL < e) {
-        float y[8];
+        float y[V];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) y[k] = activated<ACT>(__builtin_fmaf(v[u].get(k) - mean[k], f[k], beta.v[k]));
-        store8((T*)J.a.y.data + (i + u * at.RL) * J.a.y.ld + at.col, at.lo, at.hi, y);
+        for (int k = 0; k < V; ++k)
+          y[k] = activated<ACT>(__builtin_fmaf((float)v[u][k] - mean[k], f[k], beta.v[k]));
+        at.template store<LARGE>(J.a.y, i + u * at.RL, y);
       }
   }
 }
 
-// f(u, k, xhat, d) for rows [r, e): d = dy act'(z).
+// each(k, xhat, d, gamma, rstd) for every column of rows [r, e), d = dy act'(z), then row(i).
 template <typename T, int ACT, typename S, typename F, typename G>
-__device__ __forceinline__ void reversed(const GnJob& J, const Cols& at, int d, int64_t r, int64_t e, S stats_of, F each, G row) {
-  const Vec8 gamma(J.a.op.gamma, at, 1.f), beta(J.a.op.beta, at, 0.f);
-  float mean[8], rstd[8];
+__device__ __forceinline__ void reversed(const GnJob& J, const Cols<T>& at, int d, int64_t r, int64_t e, S stats_of, F each,
+                                         G row) {
+  constexpr int U = 4, V = Run<T>::V;
+  const Vec<T> gamma(J.a.op.gamma, at, 1.f), beta(J.a.op.beta, at, 0.f);
+  float mean[V], rstd[V];
 #pragma unroll
-  for (int k = 0; k < 8; ++k) {
+  for (int k = 0; k < V; ++k) {
     const float2 s = at.has(k) ? stats_of((at.col + k) / d) : float2{0.f, 0.f};
     mean[k] = s.x;
     rstd[k] = s.y;
   }
-  for (int64_t i = r + at.rl; i < e; i += 2 * at.RL) {
-    Raw8<T> v[2], w[2];
+  for (int64_t i = r + at.rl; i < e; i += U * at.RL) {
+    typename Run<T>::vec v[U], w[U];
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      v[u] = at.template load<T>(J.a.x, min(i + u * at.RL, e - 1));
-      w[u] = at.template load<T>(J.a.dy, min(i + u * at.RL, e - 1));
+    for (int u = 0; u < U; ++u) {
+      v[u] = at.load(J.a.x, min(i + u * at.RL, e - 1));
+      w[u] = at.load(J.a.dy, min(i + u * at.RL, e - 1));
     }
 #pragma unroll
-    for (int u = 0; u < 2; ++u)
+    for (int u = 0; u < U; ++u)
       if (i + u * at.RL < e) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const float xhat = (v[u].get(k) - mean[k]) * rstd[k];
-          each(k, xhat, activated_grad<ACT>(__builtin_fmaf(xhat, gamma.v[k], beta.v[k]), w[u].get(k)), gamma.v[k], rstd[k]);
+        for (int k = 0; k < V; ++k) {
+          const float xhat = ((float)v[u][k] - mean[k]) * rstd[k];
+          each(k, xhat, activated_grad<ACT>(__builtin_fmaf(xhat, gamma.v[k], beta.v[k]), (float)w[u][k]), gamma.v[k], rstd[k]);
         }
         row(i + u * at.RL);
       }
@@ -254,10 +295,10 @@ __device__ __forceinline__ void reversed(const GnJob& J, const Cols& at, int d, 
 }
 // Sums of d xhat and d over rows [r, e).
 template <typename T, int ACT, typename S>
-__device__ __forceinline__ void gradient_sums(const GnJob& J, const Cols& at, int d, int64_t r, int64_t e, S stats_of,
-                                              float (&b)[8], float (&a)[8]) {
+__device__ __forceinline__ void gradient_sums(const GnJob& J, const Cols<T>& at, int d, int64_t r, int64_t e, S stats_of,
+                                              float (&b)[Run<T>::V], float (&a)[Run<T>::V]) {
 #pragma unroll
-  for (int k = 0; k < 8; ++k) a[k] = b[k] = 0.f;
+  for (int k = 0; k < Run<T>::V; ++k) a[k] = b[k] = 0.f;
   if (!at.on) return;
   reversed<T, ACT>(
       J, at, d, r, e, stats_of,
@@ -267,12 +308,12 @@ __device__ __forceinline__ void gradient_sums(const GnJob& J, const Cols& at, in
       },
       [](int64_t) {});
 }
-template <typename T, int ACT, typename S, typename M>
-__device__ __forceinline__ void input_gradient(const GnJob& J, const Cols& at, int d, int64_t r, int64_t e, S stats_of, M means_of) {
+template <typename T, int ACT, bool LARGE, typename S, typename M>
+__device__ __forceinline__ void input_gradient(const GnJob& J, const Cols<T>& at, int d, int64_t r, int64_t e, S stats_of, M means_of) {
   if (!at.on) return;
-  float m1[8], m2[8], dx[8];
+  float m1[Run<T>::V], m2[Run<T>::V], dx[Run<T>::V];
 #pragma unroll
-  for (int k = 0; k < 8; ++k) {
+  for (int k = 0; k < Run<T>::V; ++k) {
     const float2 s = at.has(k) ? means_of((at.col + k) / d) : float2{0.f, 0.f};
     m1[k] = s.x;
     m2[k] = s.y;
@@ -282,15 +323,15 @@ __device__ __forceinline__ void input_gradient(const GnJob& J, const Cols& at, i
       [&](int k, float xhat, float g, float gamma, float rstd) {
         dx[k] = rstd * (__builtin_fmaf(gamma, g, -m1[k]) - xhat * m2[k]);
       },
-      [&](int64_t i) { store8((T*)J.a.dx.data + i * J.a.dx.ld + at.col, at.lo, at.hi, dx); });
+      [&](int64_t i) { at.template store<LARGE>(J.a.dx, i, dx); });
 }
 // A strip's columns' sums over the threads that share them: put(column, sums).
-template <typename F>
-__device__ __forceinline__ void column_pairs(const Cols& at, const float (&s1)[8], const float (&s2)[8], Pair<float>* buf, F put) {
+template <typename T, typename F>
+__device__ __forceinline__ void column_pairs(const Cols<T>& at, const float (&s1)[Run<T>::V], const float (&s2)[Run<T>::V], Pair<float>* buf, F put) {
   const int w = at.c1 - at.c0;
   if (at.on) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
+    for (int e = 0; e < Run<T>::V; ++e)
       if (at.has(e)) buf[at.rl * w + at.col - at.c0 + e] = Pair<float>{s1[e], s2[e]};
   }
   __syncthreads();
@@ -304,11 +345,12 @@ __device__ __forceinline__ void column_pairs(const Cols& at, const float (&s1)[8
   }
   __syncthreads();
 }
-__device__ __forceinline__ void times_gamma(const GnJob& J, const Cols& at, float (&u)[8], float (&v)[8], const float (&a)[8],
-                                            const float (&b)[8]) {
-  const Vec8 gamma(J.a.op.gamma, at, 1.f);
+template <typename T>
+__device__ __forceinline__ void times_gamma(const GnJob& J, const Cols<T>& at, float (&u)[Run<T>::V], float (&v)[Run<T>::V], const float (&a)[Run<T>::V],
+                                            const float (&b)[Run<T>::V]) {
+  const Vec<T> gamma(J.a.op.gamma, at, 1.f);
 #pragma unroll
-  for (int k = 0; k < 8; ++k) {
+  for (int k = 0; k < Run<T>::V; ++k) {
     u[k] = a[k] * gamma.v[k];
     v[k] = b[k] * gamma.v[k];
   }
@@ -320,10 +362,10 @@ extern __shared__ __align__(16) uint8_t gn_lds[];
 struct TilePlace {
   int64_t tile, r0, r1;
   int c0, c1, d;
-  __device__ __forceinline__ TilePlace(const GnJob& J) {
+  __device__ __forceinline__ TilePlace(const GnJob& J, int64_t rows) {
     tile = blockIdx.x;
-    r0 = tile * J.p.tile;
-    r1 = min(r0 + J.p.tile, J.a.op.rows);
+    r0 = tile * rows;
+    r1 = min(r0 + rows, J.a.op.rows);
     d = J.a.op.cols / J.a.op.groups;
     c0 = blockIdx.y * J.p.width;
     c1 = min(c0 + J.p.width, J.a.op.cols);
@@ -332,13 +374,13 @@ struct TilePlace {
 
 template <typename T>
 __global__ void __launch_bounds__(256) k_group_moments(GnJob J) {
-  const TilePlace t(J);
+  const TilePlace t(J, J.p.tile);
   const mgn_group_norm& op = J.a.op;
   Pair<double>* buf = (Pair<double>*)gn_lds;
-  for (int c = t.c0; c < t.c1; c += kStrip) {
-    const Cols at(c, min(c + kStrip, t.c1));
+  for (int c = t.c0; c < t.c1; c += Run<T>::strip) {
+    const Cols<T> at(c, min(c + Run<T>::strip, t.c1));
     for_samples(op, t.r0, t.r1, [&](int64_t s, int64_t r, int64_t e) {
-      double s1[8], s2[8];
+      double s1[Run<T>::V], s2[Run<T>::V];
       moments<T>(J.a.x, at, r, e, s1, s2);
       group_sums(at, t.d, s1, s2, buf, [&](int g, Pair<double> v) {
         double2* to = J.slots + (t.tile + s) * op.groups + c / t.d + g;
@@ -350,8 +392,9 @@ __global__ void __launch_bounds__(256) k_group_moments(GnJob J) {
 
 // Statistics (MEANS false) or the means of u and u xhat (true): 32 groups of a sample a block.
 template <bool MEANS>
-__global__ void __launch_bounds__(1024) k_group_join(GnJob J) {
-  __shared__ Pair<double> buf[32][33];
+__global__ void __launch_bounds__(512) k_group_join(GnJob J) {
+  constexpr int P = 16;
+  __shared__ Pair<double> buf[P][33];
   const mgn_group_norm& op = J.a.op;
   const int g = blockIdx.y * 32 + (threadIdx.x & 31), part = threadIdx.x >> 5;
   const int64_t s = blockIdx.x;
@@ -362,7 +405,7 @@ __global__ void __launch_bounds__(1024) k_group_join(GnJob J) {
   Pair<double> t = {0.0, 0.0};
   if (g < op.groups) {
 #pragma unroll 4
-    for (int64_t i = t0 + part; i <= t1; i += 32) {
+    for (int64_t i = t0 + part; i <= t1; i += P) {
       const int64_t at = (i + s) * op.groups + g;
       if constexpr (MEANS) {
         const float2 v = J.bslots[at];
@@ -378,7 +421,7 @@ __global__ void __launch_bounds__(1024) k_group_join(GnJob J) {
   buf[part][threadIdx.x & 31] = t;
   __syncthreads();
   if (part > 0 || g >= op.groups) return;
-  for (int i = 1; i < 32; ++i) {
+  for (int i = 1; i < P; ++i) {
     t.x += buf[i][threadIdx.x].x;
     t.y += buf[i][threadIdx.x].y;
   }
@@ -389,28 +432,28 @@ __global__ void __launch_bounds__(1024) k_group_join(GnJob J) {
     J.stats[s * op.groups + g] = moments_to_stats(t, n, op.eps);
 }
 
-template <typename T, int ACT>
+template <typename T, int ACT, bool LARGE>
 __global__ void __launch_bounds__(256) k_group_apply(GnJob J) {
-  const TilePlace t(J);
+  const TilePlace t(J, J.p.atile);
   const mgn_group_norm& op = J.a.op;
-  for (int c = t.c0; c < t.c1; c += kStrip) {
-    const Cols at(c, min(c + kStrip, t.c1));
+  for (int c = t.c0; c < t.c1; c += Run<T>::strip) {
+    const Cols<T> at(c, min(c + Run<T>::strip, t.c1));
     for_samples(op, t.r0, t.r1, [&](int64_t s, int64_t r, int64_t e) {
-      apply<T, ACT>(J, at, t.d, r, e, [&](int g) { return J.stats[s * op.groups + g]; });
+      apply<T, ACT, LARGE>(J, at, t.d, r, e, [&](int g) { return J.stats[s * op.groups + g]; });
     });
   }
 }
 
 template <typename T, int ACT>
 __global__ void __launch_bounds__(256) k_group_bwd_sums(GnJob J) {
-  const TilePlace t(J);
+  const TilePlace t(J, J.p.tile);
   const mgn_group_norm& op = J.a.op;
   Pair<float>* buf = (Pair<float>*)gn_lds;
-  for (int c = t.c0; c < t.c1; c += kStrip) {
-    const Cols at(c, min(c + kStrip, t.c1));
-    float ta[8] = {}, tb[8] = {};
+  for (int c = t.c0; c < t.c1; c += Run<T>::strip) {
+    const Cols<T> at(c, min(c + Run<T>::strip, t.c1));
+    float ta[Run<T>::V] = {}, tb[Run<T>::V] = {};
     for_samples(op, t.r0, t.r1, [&](int64_t s, int64_t r, int64_t e) {
-      float a[8], b[8], u[8], v[8];
+      float a[Run<T>::V], b[Run<T>::V], u[Run<T>::V], v[Run<T>::V];
       gradient_sums<T, ACT>(J, at, t.d, r, e, [&](int g) { return J.stats[s * op.groups + g]; }, b, a);
       times_gamma(J, at, u, v, a, b);
       group_sums(at, t.d, u, v, buf, [&](int g, Pair<float> w) {
@@ -418,7 +461,7 @@ __global__ void __launch_bounds__(256) k_group_bwd_sums(GnJob J) {
         *to = c > t.c0 ? float2{to->x + w.x, to->y + w.y} : float2{w.x, w.y};
       });
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
+      for (int k = 0; k < Run<T>::V; ++k) {
         ta[k] += a[k];
         tb[k] += b[k];
       }
@@ -432,14 +475,14 @@ __global__ void __launch_bounds__(256) k_group_bwd_sums(GnJob J) {
   }
 }
 
-template <typename T, int ACT>
+template <typename T, int ACT, bool LARGE>
 __global__ void __launch_bounds__(256) k_group_bwd_apply(GnJob J) {
-  const TilePlace t(J);
+  const TilePlace t(J, J.p.atile);
   const mgn_group_norm& op = J.a.op;
-  for (int c = t.c0; c < t.c1; c += kStrip) {
-    const Cols at(c, min(c + kStrip, t.c1));
+  for (int c = t.c0; c < t.c1; c += Run<T>::strip) {
+    const Cols<T> at(c, min(c + Run<T>::strip, t.c1));
     for_samples(op, t.r0, t.r1, [&](int64_t s, int64_t r, int64_t e) {
-      input_gradient<T, ACT>(J, at, t.d, r, e, [&](int g) { return J.stats[s * op.groups + g]; },
+      input_gradient<T, ACT, LARGE>(J, at, t.d, r, e, [&](int g) { return J.stats[s * op.groups + g]; },
                              [&](int g) { return J.means[s * op.groups + g]; });
     });
   }
@@ -462,14 +505,14 @@ struct WholePlace {
 };
 
 template <typename T, int ACT>
-__global__ void __launch_bounds__(512) k_group_whole(GnJob J) {
+__global__ void __launch_bounds__(256) k_group_whole(GnJob J) {
   const WholePlace t(J);
   const mgn_group_norm& op = J.a.op;
   Pair<double>* buf = (Pair<double>*)gn_lds;
-  Pair<double>* sums = buf + blockDim.x * 8;  // of the block's groups
-  for (int c = t.c0; c < t.c1; c += kStrip) {
-    const Cols at(c, min(c + kStrip, t.c1));
-    double s1[8], s2[8];
+  Pair<double>* sums = buf + blockDim.x * Run<T>::V;  // of the block's groups
+  for (int c = t.c0; c < t.c1; c += Run<T>::strip) {
+    const Cols<T> at(c, min(c + Run<T>::strip, t.c1));
+    double s1[Run<T>::V], s2[Run<T>::V];
     moments<T>(J.a.x, at, t.r0, t.r1, s1, s2);
     group_sums(at, t.d, s1, s2, buf, [&](int g, Pair<double> v) {
       sums[g] = c > t.c0 ? Pair<double>{sums[g].x + v.x, sums[g].y + v.y} : v;
@@ -482,22 +525,22 @@ __global__ void __launch_bounds__(512) k_group_whole(GnJob J) {
     if (J.stats != nullptr) J.stats[t.s * op.groups + g0 + g] = st[g];
   }
   __syncthreads();
-  for (int c = t.c0; c < t.c1; c += kStrip) {
-    const Cols at(c, min(c + kStrip, t.c1));
-    apply<T, ACT>(J, at, t.d, t.r0, t.r1, [&](int g) { return st[g - g0]; });
+  for (int c = t.c0; c < t.c1; c += Run<T>::strip) {
+    const Cols<T> at(c, min(c + Run<T>::strip, t.c1));
+    apply<T, ACT, false>(J, at, t.d, t.r0, t.r1, [&](int g) { return st[g - g0]; });
   }
 }
 
 template <typename T, int ACT>
-__global__ void __launch_bounds__(512) k_group_bwd_whole(GnJob J) {
+__global__ void __launch_bounds__(256) k_group_bwd_whole(GnJob J) {
   const WholePlace t(J);
   const mgn_group_norm& op = J.a.op;
   Pair<float>* buf = (Pair<float>*)gn_lds;
-  Pair<float>* sums = buf + blockDim.x * 8;
+  Pair<float>* sums = buf + blockDim.x * Run<T>::V;
   auto stats_of = [&](int g) { return J.stats[t.s * op.groups + g]; };
-  for (int c = t.c0; c < t.c1; c += kStrip) {
-    const Cols at(c, min(c + kStrip, t.c1));
-    float a[8], b[8], u[8], v[8];
+  for (int c = t.c0; c < t.c1; c += Run<T>::strip) {
+    const Cols<T> at(c, min(c + Run<T>::strip, t.c1));
+    float a[Run<T>::V], b[Run<T>::V], u[Run<T>::V], v[Run<T>::V];
     gradient_sums<T, ACT>(J, at, t.d, t.r0, t.r1, stats_of, b, a);
     times_gamma(J, at, u, v, a, b);
     group_sums(at, t.d, u, v, buf, [&](int g, Pair<float> w) {
@@ -512,9 +555,9 @@ __global__ void __launch_bounds__(512) k_group_bwd_whole(GnJob J) {
   }
   const int g0 = t.c0 / t.d;
   const float inv = t.n > 0.0 ? (float)(1.0 / t.n) : 0.f;
-  for (int c = t.c0; c < t.c1; c += kStrip) {
-    const Cols at(c, min(c + kStrip, t.c1));
-    input_gradient<T, ACT>(J, at, t.d, t.r0, t.r1, stats_of,
+  for (int c = t.c0; c < t.c1; c += Run<T>::strip) {
+    const Cols<T> at(c, min(c + Run<T>::strip, t.c1));
+    input_gradient<T, ACT, false>(J, at, t.d, t.r0, t.r1, stats_of,
                            [&](int g) { return float2{sums[g - g0].x * inv, sums[g - g0].y * inv}; });
   }
 }
@@ -525,21 +568,30 @@ using namespace dev;
 
 namespace {
 
+// Blocks that tiles are cut for: as many sums as run at a time (three a CU; 307,981 x 128
+// fp32, forward and reverse 96 and 142 us, with 2048 blocks 96 and 154), and as many
+// results, four a CU, or tiles of 16 rows a thread where these are more than four rounds
+// (852,640 x 128 fp32 231 and 397 us, one round 245 and 415).
+constexpr int kSumBlocks = 768, kResultBlocks = 1024;
+
+
 GnPlan plan(const mgn_group_norm& op) {
   GnPlan p;
   const int d = op.cols / op.groups;
   const int64_t size = op.type == MGN_BF16 ? 2 : 4;
-  p.width = d >= kStrip ? d : kStrip / d * d;
-  if (p.width > op.cols) p.width = op.cols;
-  p.cblocks = (int)ceil_div(op.cols, p.width);
+  const int run = (int)(16 / size), strip = 256 * run;
+  // as many groups as fit a strip, and as many for every block
+  p.cblocks = (int)ceil_div(op.groups, std::max(strip / d, 1));
+  p.width = (int)ceil_div(op.groups, p.cblocks) * d;
   const int64_t bytes = op.rows * p.width * size;
   p.whole = bytes <= (1 << 20) ||
             (op.sample_ptr == nullptr && bytes / op.n_samples <= (1 << 17) && op.n_samples * p.cblocks >= 256);
-  p.threads = 256;
-  // about 2048 blocks, of 4 rows a thread or more
-  const int64_t lanes = ceil_div(std::min(p.width, kStrip), 8), rl = std::max<int64_t>(256 / lanes, 1);
-  p.tile = std::max(rl * 4, ceil_div(op.rows * p.cblocks, 2048));
+  const int64_t lanes = ceil_div(std::min(p.width, strip), run), rl = std::max<int64_t>(256 / lanes, 1);
+  auto rows_of = [&](int64_t blocks) { return std::max(ceil_div(op.rows * p.cblocks, blocks), rl * 4); };
+  p.tile = rows_of(kSumBlocks);
   p.tiles = p.whole ? 0 : ceil_div(op.rows, p.tile);
+  p.atile = rows_of(kResultBlocks) > rl * 64 ? rl * 16 : rows_of(kResultBlocks);
+  p.atiles = p.whole ? 0 : ceil_div(op.rows, p.atile);
   return p;
 }
 
@@ -582,22 +634,27 @@ GnJob job(const GroupNorm& a, const GnPlan& p, bool backward) {
   return J;
 }
 
-#define MGN_GN(K, grid, threads, lds)                                                                          \
+// K<type, act ...>
+#define MGN_GN(K, grid, lds, ...)                                                                              \
   do {                                                                                                         \
     const bool f32 = a.op.type == MGN_FP32;                                                                    \
     if (a.op.act == MGN_ACT_NONE) {                                                                            \
-      if (f32) hipLaunchKernelGGL((K<float, MGN_ACT_NONE>), grid, dim3(threads), lds, s, J);                   \
-      else hipLaunchKernelGGL((K<bf16, MGN_ACT_NONE>), grid, dim3(threads), lds, s, J);                        \
+      if (f32) hipLaunchKernelGGL((K<float, MGN_ACT_NONE __VA_ARGS__>), grid, dim3(256), lds, s, J);           \
+      else hipLaunchKernelGGL((K<bf16, MGN_ACT_NONE __VA_ARGS__>), grid, dim3(256), lds, s, J);                \
     } else if (a.op.act == MGN_ACT_RELU) {                                                                     \
-      if (f32) hipLaunchKernelGGL((K<float, MGN_ACT_RELU>), grid, dim3(threads), lds, s, J);                   \
-      else hipLaunchKernelGGL((K<bf16, MGN_ACT_RELU>), grid, dim3(threads), lds, s, J);                        \
+      if (f32) hipLaunchKernelGGL((K<float, MGN_ACT_RELU __VA_ARGS__>), grid, dim3(256), lds, s, J);           \
+      else hipLaunchKernelGGL((K<bf16, MGN_ACT_RELU __VA_ARGS__>), grid, dim3(256), lds, s, J);                \
     } else {                                                                                                   \
-      if (f32) hipLaunchKernelGGL((K<float, MGN_ACT_SILU>), grid, dim3(threads), lds, s, J);                   \
-      else hipLaunchKernelGGL((K<bf16, MGN_ACT_SILU>), grid, dim3(threads), lds, s, J);                        \
+      if (f32) hipLaunchKernelGGL((K<float, MGN_ACT_SILU __VA_ARGS__>), grid, dim3(256), lds, s, J);           \
+      else hipLaunchKernelGGL((K<bf16, MGN_ACT_SILU __VA_ARGS__>), grid, dim3(256), lds, s, J);                \
     }                                                                                                          \
     const hipError_t err = hipGetLastError();                                                                  \
     if (err != hipSuccess) return err;                                                                         \
   } while (0)
+
+bool large(const mgn_group_norm& op) { return op.rows * op.cols * (op.type == MGN_BF16 ? 2 : 4) > (32LL << 20); }
+// Bytes of LDS for `pair` bytes for each of the block's columns.
+size_t lds_of(const mgn_group_norm& op, size_t pair) { return 256 * (op.type == MGN_BF16 ? 8 : 4) * pair; }
 
 }  // namespace
 
@@ -612,21 +669,25 @@ hipError_t launch_group_norm_forward(const GroupNorm& a, hipStream_t s) {
   const GnJob J = job(a, p, false);
   if (p.whole) {
     const dim3 g((unsigned)a.op.n_samples, p.cblocks);
-    MGN_GN(k_group_whole, g, p.threads, p.threads * 128 + (size_t)(p.width / (a.op.cols / a.op.groups)) * 16);
+    MGN_GN(k_group_whole, g, lds_of(a.op, 16) + (size_t)(p.width / (a.op.cols / a.op.groups)) * 16, );
     return hipSuccess;
   }
   const dim3 g((unsigned)p.tiles, p.cblocks);
   if (a.op.type == MGN_FP32)
-    hipLaunchKernelGGL((k_group_moments<float>), g, dim3(256), 256 * 128, s, J);
+    hipLaunchKernelGGL((k_group_moments<float>), g, dim3(256), lds_of(a.op, 16), s, J);
   else
-    hipLaunchKernelGGL((k_group_moments<bf16>), g, dim3(256), 256 * 128, s, J);
+    hipLaunchKernelGGL((k_group_moments<bf16>), g, dim3(256), lds_of(a.op, 16), s, J);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((k_group_join<false>), dim3((unsigned)a.op.n_samples, (unsigned)ceil_div(a.op.groups, 32)), dim3(1024), 0,
+  hipLaunchKernelGGL((k_group_join<false>), dim3((unsigned)a.op.n_samples, (unsigned)ceil_div(a.op.groups, 32)), dim3(512), 0,
                      s, J);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
-  MGN_GN(k_group_apply, g, 256, 0);
+  const dim3 ga((unsigned)p.atiles, p.cblocks);
+  if (large(a.op))
+    MGN_GN(k_group_apply, ga, 0, , true);
+  else
+    MGN_GN(k_group_apply, ga, 0, , false);
   return hipSuccess;
 }
 
@@ -638,15 +699,19 @@ hipError_t launch_group_norm_backward(const GroupNorm& a, hipStream_t s) {
   const GnJob J = job(a, p, true);
   if (p.whole) {
     const dim3 g((unsigned)a.op.n_samples, p.cblocks);
-    MGN_GN(k_group_bwd_whole, g, p.threads, p.threads * 64 + (size_t)(p.width / (a.op.cols / a.op.groups)) * 8);
+    MGN_GN(k_group_bwd_whole, g, lds_of(a.op, 8) + (size_t)(p.width / (a.op.cols / a.op.groups)) * 8, );
   } else {
     const dim3 g((unsigned)p.tiles, p.cblocks);
-    MGN_GN(k_group_bwd_sums, g, 256, 256 * 64);
-    hipLaunchKernelGGL((k_group_join<true>), dim3((unsigned)a.op.n_samples, (unsigned)ceil_div(a.op.groups, 32)), dim3(1024), 0,
+    MGN_GN(k_group_bwd_sums, g, lds_of(a.op, 8), );
+    hipLaunchKernelGGL((k_group_join<true>), dim3((unsigned)a.op.n_samples, (unsigned)ceil_div(a.op.groups, 32)), dim3(512), 0,
                        s, J);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    MGN_GN(k_group_bwd_apply, g, 256, 0);
+    const dim3 ga((unsigned)p.atiles, p.cblocks);
+    if (large(a.op))
+      MGN_GN(k_group_bwd_apply, ga, 0, , true);
+    else
+      MGN_GN(k_group_bwd_apply, ga, 0, , false);
   }
   if (!J.part) return hipSuccess;
   return launch_column_reduce(J.part, p.whole ? a.op.n_samples : p.tiles, a.op.cols, out, 2, a.accumulate, s);

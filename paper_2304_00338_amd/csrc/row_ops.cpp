@@ -341,7 +341,7 @@ int mgn_dequant4(const mgn_mat4* a, int32_t y_type, void* y, int64_t ldy, void* 
   if (a->rows == 0 || a->cols == 0) return MGN_OK;
   if (!y || ldy < a->cols || !fits(a->rows, ldy) || !aligned(y, elem(y_type)))
     return fail(MGN_ERR_ARG, "%s: null or misaligned y, or its leading dimension %lld", who, (long long)ldy);
-  if (ceil_div(a->rows, 16) * ceil_div(a->cols, 128) >= kMost)
+  if (ceil_div(a->rows, 8) * ceil_div(a->cols, 128) >= kMost)
     return fail(MGN_ERR_SHAPE, "%s: a of %lld x %lld is too large for one call", who, (long long)a->rows,
                 (long long)a->cols);
   const Dequant4 d = {*a, y_type, y, ldy};
