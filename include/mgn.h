@@ -609,7 +609,8 @@ typedef struct mgn_group_norm {
 
 /* y from x; stats (nullable: inference) [n_samples][groups][2] float32 keeps mean and
  * 1 / sqrt(var + eps) for the reverse (of a sample without rows: 0 and 1 / sqrt(eps)).
- * Sums are of 64 bits.  y may be x (with the same ld).
+ * Sums are of 64 bits.  y may be x (with the same ld).  At most 2^21 samples, and 2^22
+ * times 32 groups of all samples.
  * Errors: ARG, SHAPE, WORKSPACE, DEVICE. */
 int mgn_group_norm_workspace(const mgn_group_norm* op, int32_t backward, size_t* ws_bytes);
 int mgn_group_norm_forward(const mgn_group_norm* op, mgn_rows x, mgn_rows y, float* stats,

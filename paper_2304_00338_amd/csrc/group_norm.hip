@@ -390,19 +390,48 @@ __global__ void __launch_bounds__(256) k_group_moments(GnJob J) {
   }
 }
 
-// Statistics (MEANS false) or the means of u and u xhat (true): 32 groups of a sample a block.
+// Statistics (MEANS false) or the means of u and u xhat (true): 32 groups of a sample a
+// block.  In the reverse the blocks behind those sum 32 columns of the tiles' parts.
 template <bool MEANS>
 __global__ void __launch_bounds__(512) k_group_join(GnJob J) {
   constexpr int P = 16;
   __shared__ Pair<double> buf[P][33];
   const mgn_group_norm& op = J.a.op;
-  const int g = blockIdx.y * 32 + (threadIdx.x & 31), part = threadIdx.x >> 5;
-  const int64_t s = blockIdx.x;
+  const int lane = threadIdx.x & 31, part = threadIdx.x >> 5;
+  const int64_t gblocks = ceil_div(op.groups, 32);
+  Pair<double> t = {0.0, 0.0};
+  auto joined = [&]() {  // over the parts, in part 0
+    buf[part][lane] = t;
+    __syncthreads();
+    if (part > 0) return false;
+    for (int i = 1; i < P; ++i) {
+      t.x += buf[i][lane].x;
+      t.y += buf[i][lane].y;
+    }
+    return true;
+  };
+  if (MEANS && blockIdx.x >= op.n_samples * gblocks) {
+    const int64_t c = (blockIdx.x - op.n_samples * gblocks) * 32 + lane;
+    if (c < op.cols) {
+#pragma unroll 4
+      for (int64_t i = part; i < J.p.tiles; i += P) {
+        const float* v = J.part + i * 2 * op.cols + c;
+        t.x += v[0];
+        t.y += v[op.cols];
+      }
+    }
+    if (!joined() || c >= op.cols) return;
+    float *const dg = J.a.dgamma, *const db = J.a.dbeta;
+    if (dg != nullptr) dg[c] = J.a.accumulate ? dg[c] + (float)t.x : (float)t.x;
+    if (db != nullptr) db[c] = J.a.accumulate ? db[c] + (float)t.y : (float)t.y;
+    return;
+  }
+  const int64_t s = blockIdx.x / gblocks;
+  const int g = (int)(blockIdx.x - s * gblocks) * 32 + lane;
   int64_t b, e;
   rows_of(op, s, b, e);
   const bool any = e > b;
   const int64_t t0 = any ? b / J.p.tile : 0, t1 = any ? (e - 1) / J.p.tile : -1;
-  Pair<double> t = {0.0, 0.0};
   if (g < op.groups) {
 #pragma unroll 4
     for (int64_t i = t0 + part; i <= t1; i += P) {
@@ -418,13 +447,7 @@ __global__ void __launch_bounds__(512) k_group_join(GnJob J) {
       }
     }
   }
-  buf[part][threadIdx.x & 31] = t;
-  __syncthreads();
-  if (part > 0 || g >= op.groups) return;
-  for (int i = 1; i < P; ++i) {
-    t.x += buf[i][threadIdx.x].x;
-    t.y += buf[i][threadIdx.x].y;
-  }
+  if (!joined() || g >= op.groups) return;
   const double n = any ? (double)(e - b) * (double)(op.cols / op.groups) : 0.0;
   if constexpr (MEANS)
     J.means[s * op.groups + g] = any ? float2{(float)(t.x / n), (float)(t.y / n)} : float2{0.f, 0.f};
@@ -679,8 +702,7 @@ hipError_t launch_group_norm_forward(const GroupNorm& a, hipStream_t s) {
     hipLaunchKernelGGL((k_group_moments<bf16>), g, dim3(256), lds_of(a.op, 16), s, J);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((k_group_join<false>), dim3((unsigned)a.op.n_samples, (unsigned)ceil_div(a.op.groups, 32)), dim3(512), 0,
-                     s, J);
+  hipLaunchKernelGGL((k_group_join<false>), dim3((unsigned)(a.op.n_samples * ceil_div(a.op.groups, 32))), dim3(512), 0, s, J);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
   const dim3 ga((unsigned)p.atiles, p.cblocks);
@@ -703,8 +725,9 @@ hipError_t launch_group_norm_backward(const GroupNorm& a, hipStream_t s) {
   } else {
     const dim3 g((unsigned)p.tiles, p.cblocks);
     MGN_GN(k_group_bwd_sums, g, lds_of(a.op, 8), );
-    hipLaunchKernelGGL((k_group_join<true>), dim3((unsigned)a.op.n_samples, (unsigned)ceil_div(a.op.groups, 32)), dim3(512), 0,
-                       s, J);
+    hipLaunchKernelGGL((k_group_join<true>),
+                       dim3((unsigned)(a.op.n_samples * ceil_div(a.op.groups, 32) + (J.part ? ceil_div(a.op.cols, 32) : 0))),
+                       dim3(512), 0, s, J);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     const dim3 ga((unsigned)p.atiles, p.cblocks);
@@ -713,8 +736,8 @@ hipError_t launch_group_norm_backward(const GroupNorm& a, hipStream_t s) {
     else
       MGN_GN(k_group_bwd_apply, ga, 0, , false);
   }
-  if (!J.part) return hipSuccess;
-  return launch_column_reduce(J.part, p.whole ? a.op.n_samples : p.tiles, a.op.cols, out, 2, a.accumulate, s);
+  if (!J.part || !p.whole) return hipSuccess;
+  return launch_column_reduce(J.part, a.op.n_samples, a.op.cols, out, 2, a.accumulate, s);
 }
 
 }  // namespace mgn

@@ -347,22 +347,26 @@ __global__ void __launch_bounds__(WM * WN * 64, TM * TN > 8 ? 1 : 2) k_matmul4_t
 
 // ---- few rows of a (up to TM times 16), bound by the weights' bytes.
 //
-// A block takes 16 rows of b, its 8 waves the steps of 256 columns in turn; operands
-// come straight from memory, 16 bytes a lane (four lanes cover a row's 128 columns,
-// two loads its 128-byte line), a step ahead, and the waves' sums meet in LDS.
-template <int TM>
+// A block takes TN times 16 rows of b, its 8 waves the steps of 256 columns in turn;
+// operands come straight from memory, 16 bytes a lane (four lanes cover a row's 128
+// columns, two loads its 128-byte line), a step ahead, and the waves' sums meet in LDS.
+template <int TM, int TN>
 __global__ void __launch_bounds__(512) k_matmul4_few(Job4 J) {
   constexpr int NWV = 8;
-  __shared__ f32x4 sums[NWV][TM][64];
+  __shared__ f32x4 sums[NWV][TM * TN][64];
   const Matmul4& p = J.p;
   const int l = threadIdx.x & 63, w = threadIdx.x >> 6, j = l & 15, q = l >> 4;
-  const int64_t n0 = (blockIdx.y * kGridRow + blockIdx.x) * 16;
+  const int64_t n0 = (blockIdx.y * kGridRow + blockIdx.x) * (16 * TN);
   const int split = blockIdx.z;
   const int64_t kb0 = split * J.per, kb1 = min(kb0 + J.per, J.kb);
   const int64_t end = (p.a.cols + 31) / 32 * 16 - q * 16;
-  const int64_t nj = min(n0 + j, p.b.rows - 1);
-  const uint8_t *rb = p.b.q + nj * p.b.ld + q * 16, *sb = p.b.scale + nj * 4 + q;
-  const uint8_t *ra[TM], *sa[TM];
+  const uint8_t *rb[TN], *sb[TN], *ra[TM], *sa[TM];
+#pragma unroll
+  for (int i = 0; i < TN; ++i) {
+    const int64_t n = min(n0 + i * 16 + j, p.b.rows - 1);
+    rb[i] = p.b.q + n * p.b.ld + q * 16;
+    sb[i] = p.b.scale + n * 4 + q;
+  }
 #pragma unroll
   for (int i = 0; i < TM; ++i) {
     const int64_t m = min((int64_t)i * 16 + j, p.a.rows - 1);
@@ -370,33 +374,40 @@ __global__ void __launch_bounds__(512) k_matmul4_few(Job4 J) {
     sa[i] = p.a.scale + m * 4 + q;
   }
   struct Step {
-    uint4 a[2][TM], b[2];
-    uint32_t sa[2][TM], sb[2];
+    uint4 a[2][TM], b[2][TN];
+    uint32_t sa[2][TM], sb[2][TN];
   };
   auto fetch = [&](Step& x, int64_t kb) {
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
+      // of a step that is another split's, or behind the last, b's scales are 2^-127 and the
+      // numbers zero
       const int64_t at = min(kb + u, J.kb - 1), k = (kb + u) * 64;
       const bool in = kb + u < kb1 && k < end;
-      x.b[u] = *(const uint4*)(in ? rb + k : (const uint8_t*)&zero16);
-      x.sb[u] = sb[at * p.b.rows * 4];
+#pragma unroll
+      for (int i = 0; i < TN; ++i) {
+        x.b[u][i] = *(const uint4*)(in ? rb[i] + k : (const uint8_t*)&zero16);
+        x.sb[u][i] = sb[i][at * p.b.rows * 4];
+        if (kb + u >= kb1) x.sb[u][i] = 0;
+      }
 #pragma unroll
       for (int i = 0; i < TM; ++i) {
         x.a[u][i] = *(const uint4*)(in ? ra[i] + k : (const uint8_t*)&zero16);
         x.sa[u][i] = sa[i][at * p.a.rows * 4];
+        if (kb + u >= kb1) x.sa[u][i] = 0;
       }
-      // of a step that is another split's the scales count for nothing
-      if (kb + u >= kb1) x.sb[u] = 0;
     }
   };
-  f32x4 acc[TM] = {};
+  f32x4 acc[TM][TN] = {};
   auto products = [&](const Step& x) {
 #pragma unroll
     for (int u = 0; u < 2; ++u)
 #pragma unroll
       for (int i = 0; i < TM; ++i)
-        acc[i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(operand(x.b[u]), operand(x.a[u][i]), acc[i], kE2M1, kE2M1, 0,
-                                                                  (int)x.sb[u], 0, (int)x.sa[u][i]);
+#pragma unroll
+        for (int n = 0; n < TN; ++n)
+          acc[i][n] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(operand(x.b[u][n]), operand(x.a[u][i]), acc[i][n], kE2M1,
+                                                                       kE2M1, 0, (int)x.sb[u][n], 0, (int)x.sa[u][i]);
   };
   if (kb0 + 2 * w < kb1) {
     Step x, y;
@@ -412,13 +423,15 @@ __global__ void __launch_bounds__(512) k_matmul4_few(Job4 J) {
     }
   }
 #pragma unroll
-  for (int i = 0; i < TM; ++i) sums[w][i][l] = acc[i];
+  for (int i = 0; i < TM; ++i)
+#pragma unroll
+    for (int n = 0; n < TN; ++n) sums[w][i * TN + n][l] = acc[i][n];
   __syncthreads();
-  if (w < TM) {
+  if (w < TM * TN) {
     f32x4 v = sums[0][w][l];
 #pragma unroll
     for (int k = 1; k < NWV; ++k) v += sums[k][w][l];
-    const int64_t m = w * 16 + j, n = n0 + 4 * q;
+    const int64_t m = w / TN * 16 + j, n = n0 + w % TN * 16 + 4 * q;
     if (m < p.a.rows && n < p.b.rows) put4(J, split, m, n, v);
   }
 }
@@ -436,13 +449,15 @@ struct Plan {
   int kind;
   int64_t mt, nt, per;
   int splits;
+  int tn;  // times 16 rows of b (few rows)
 };
 
 // Which kernel, and into how many parts the sums are split: the least of what these
 // take by a model of their times (us), fitted to calls in a graph:
-//  * few rows: 3 and what all blocks read (their 16 rows of b, and a each) at 6.2 TB/s
-//    (1 x 4096 x 4096 4.2, 32 x 4096 x 4096 6.4, 64 x 4096 x 4096 9.0, tiles 12.5; 64 x
-//    8192 x 8192 27, tiles 16.7);
+//  * few rows: 3 and what all blocks read (their rows of b, and a each) at 6.2 TB/s
+//    (1 x 4096 x 4096 4.2, 32 x 4096 x 4096 6.4, 64 x 4096 x 4096 8.8, tiles 12.5; 21 x
+//    9001 x 6000 with 16, 32, 48 and 64 rows of b a block 12.9, 13.3, 9.5, 10.9; 64 x 8192
+//    x 8192 with 32 17.4, tiles 16.7);
 //  * tiles of 128 x 128: 1.4 a tile of a CU and 0.31 a step and tile where all CUs have
 //    two or more, else 0.34 to 0.54 a step (2048 x 2048 x 2048 11.9, of 256 x 256 17.9);
 //    sums split into s parts add a launch and 8 s bytes a result (512 x 512 x 20,000 whole
@@ -452,7 +467,7 @@ struct Plan {
 Plan plan(int64_t m, int64_t n, int64_t k) {
   const int64_t kb = ceil_div(k, 128), m1 = ceil_div(m, 128), n1 = ceil_div(n, 128), m2 = ceil_div(m, 256),
                 n2 = ceil_div(n, 256);
-  Plan r = {kSmallTile, m1, n1, 0, 1};
+  Plan r = {kSmallTile, m1, n1, 0, 1, 0};
   double best = 1e30;
   for (int64_t s = 1; s <= 512 && (s == 1 || 2 * s <= kb); s *= 2) {
     const double blocks = (double)m1 * n1 * s, rounds = std::ceil(blocks / kCUs);
@@ -466,16 +481,32 @@ Plan plan(int64_t m, int64_t n, int64_t k) {
   const double big = (7 + 0.98 * kb) * std::ceil((double)m2 * n2 / kCUs);
   if (big < best) {
     best = big;
-    r = {kBigTile, m2, n2, 0, 1};
+    r = {kBigTile, m2, n2, 0, 1, 0};
   }
   if (m <= kFewRows) {
-    const int64_t rows = m <= 16 ? 16 : m <= 32 ? 32 : 64, nt = ceil_div(n, 16);
-    if (3 + (double)nt * (rows + 16) * k / 2 / 6.2e6 < best)
-      r = {kFew, 1, nt, 0, (int)std::max<int64_t>(std::min(kCUs / std::max<int64_t>(nt, 1), kb / 32), 1)};
+    // as many rows of b a block as leave it a CU of its own, up to what registers and LDS hold
+    const int64_t rows = m <= 16 ? 16 : m <= 32 ? 32 : 64, most = rows == 64 || (rows == 16 && n > 4 * 16 * kCUs) ? 2 : 4;
+    const int64_t tn = std::min(ceil_div(ceil_div(n, 16), kCUs), most), nt = ceil_div(n, 16 * tn);
+    if (3 + (double)nt * (rows + 16 * tn) * k / 2 / 6.2e6 < best)
+      r = {kFew, 1, nt, 0, (int)std::max<int64_t>(std::min(kCUs / nt, kb / 32), 1), (int)tn};
   }
   r.per = std::max<int64_t>(ceil_div(kb, r.splits), 1);
   r.splits = (int)std::max<int64_t>(ceil_div(kb, r.per), 1);
   return r;
+}
+
+template <int TM>
+void launch_few(const Job4& J, int tn, dim3 g, hipStream_t s) {
+  if (tn == 1)
+    hipLaunchKernelGGL((k_matmul4_few<TM, 1>), g, dim3(512), 0, s, J);
+  else if (tn == 2)
+    hipLaunchKernelGGL((k_matmul4_few<TM, 2>), g, dim3(512), 0, s, J);
+  else if constexpr (TM <= 2) {
+    if (tn == 3)
+      hipLaunchKernelGGL((k_matmul4_few<TM, 3>), g, dim3(512), 0, s, J);
+    else
+      hipLaunchKernelGGL((k_matmul4_few<TM, 4>), g, dim3(512), 0, s, J);
+  }
 }
 
 }  // namespace
@@ -494,11 +525,11 @@ hipError_t launch_matmul4(const Matmul4& p, hipStream_t s) {
     dim3 g = grid_of(r.nt);
     g.z = (unsigned)r.splits;
     if (p.a.rows <= 16)
-      hipLaunchKernelGGL((k_matmul4_few<1>), g, dim3(512), 0, s, J);
+      launch_few<1>(J, r.tn, g, s);
     else if (p.a.rows <= 32)
-      hipLaunchKernelGGL((k_matmul4_few<2>), g, dim3(512), 0, s, J);
+      launch_few<2>(J, r.tn, g, s);
     else
-      hipLaunchKernelGGL((k_matmul4_few<4>), g, dim3(512), 0, s, J);
+      launch_few<4>(J, r.tn, g, s);
   } else if (r.kind == kBigTile) {
     hipLaunchKernelGGL((k_matmul4_tile<2, 4, 4, 2, 4>), grid, dim3(512), 0, s, J);
   } else {

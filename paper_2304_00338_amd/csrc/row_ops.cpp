@@ -95,6 +95,8 @@ int check_group_norm(const mgn_group_norm* op, const char* who) {
   if (op->rows < 0 || op->n_samples < 0) return fail(MGN_ERR_ARG, "%s: negative size", who);
   if (op->rows >= kMost) return fail(MGN_ERR_SHAPE, "%s: 2^31 rows", who);
   if (op->n_samples > (1 << 21)) return fail(MGN_ERR_SHAPE, "%s: over 2^21 samples", who);
+  if (op->groups > 0 && op->n_samples * ceil_div(op->groups, 32) > (1 << 22))  // blocks of 512 threads
+    return fail(MGN_ERR_SHAPE, "%s: %lld samples of %d groups", who, (long long)op->n_samples, op->groups);
   if (op->cols < 1 || op->cols > MGN_NORM_MAX_COLS)
     return fail(MGN_ERR_SHAPE, "%s: %d columns (1 to %d)", who, op->cols, MGN_NORM_MAX_COLS);
   if (op->groups < 1 || op->cols % op->groups != 0)

@@ -240,6 +240,15 @@ def test_matmul4_large_tiles(m, n, k):
         check_product(mgn.mgn_matmul4(a, b, dtype=T[dt]), a, b, T[dt], what=dt)
 
 
+@pytest.mark.parametrize("m", [1, 16, 17, 32, 33, 64])
+def test_matmul4_few_rows_of_wide_weights(m):
+    """Blocks of 16 to 64 rows of b, the last of them with a part of theirs."""
+    for n, k in ((4097, 300), (8192, 130), (9001, 2100), (12301, 96), (16385, 500), (20000, 33)):
+        a, b = mats(m, n, k, seed=m + k)
+        bias = randn(n, seed=3)
+        check_product(mgn.mgn_matmul4(a, b, bias=bias, act="relu", dtype=torch.bfloat16), a, b, torch.bfloat16, bias, "relu", what=(n, k))
+
+
 @pytest.mark.parametrize("steps", list(range(1, 18)))
 def test_matmul4_every_number_of_steps(steps):
     """The ring of buffers from its filling to its emptying, with and without a
