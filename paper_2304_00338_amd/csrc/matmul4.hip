@@ -34,11 +34,18 @@ struct Job4 {
 
 __device__ __forceinline__ i32x8 operand(uint4 v) { return i32x8{(int)v.x, (int)v.y, (int)v.z, (int)v.w, 0, 0, 0, 0}; }
 
-// 16 bytes past the caches: results that stay in L2 push out the operands (32,768 x 4096 x
-// 1024 to fp32 170 us, through L2 208; 852,640 x 128 x 256 to fp32 121, 144).
+// 16 bytes of a result.  PAST: past the caches, where rows are aligned: results that stay
+// in L2 push out the operands (32,768 x 4096 x 1024 to fp32 170 us, through L2 208; 852,640 x
+// 128 x 256 to fp32 121, 144).  Unaligned ones meet in L2 (32,768 x 4099 x 1024 to bf16
+// 144, past it 166).
+template <bool PAST>
 __device__ __forceinline__ void store16(void* p, uint4 v) {
   typedef uint32_t u32x4 __attribute__((ext_vector_type(4), aligned(2)));
-  __builtin_nontemporal_store(u32x4{v.x, v.y, v.z, v.w}, (u32x4*)p);
+  const u32x4 w = {v.x, v.y, v.z, v.w};
+  if (PAST)
+    __builtin_nontemporal_store(w, (u32x4*)p);
+  else
+    *(u32x4*)p = w;
 }
 
 // ---- tiles: BM x BN of c a block of WM x WN waves, each TM x TN times 32 x 32.
@@ -60,7 +67,7 @@ __device__ __forceinline__ void store16(void* p, uint4 v) {
 // three buffers 128 x 128 has three blocks a CU: 852,640 x 128 x 256 to fp32 106 us (of
 // two blocks 121), 852,640 x 256 x 128 148 (6.3 TB/s).  Four waves of 128 x 128 took 355
 // us instead of 323, loads between the products 321.
-template <int WM, int WN, int TM, int TN, int NB>
+template <int WM, int WN, int TM, int TN, int NB, bool PAST>
 __global__ void __launch_bounds__(WM * WN * 64, TM * TN > 8 ? 1 : 2) k_matmul4_tile(Job4 J) {
   constexpr int BM = WM * TM * 32, BN = WN * TN * 32, NWV = WM * WN, ROWS = BM + BN;
   constexpr int LA = BM / 16 / NWV, LB = BN / 16 / NWV, LS = (ROWS / 64 + NWV - 1) / NWV;  // loads of a wave and step
@@ -286,7 +293,7 @@ __global__ void __launch_bounds__(WM * WN * 64, TM * TN > 8 ? 1 : 2) k_matmul4_t
       const uint4 v = *(const uint4*)(piece + r * CH * 16 + (c ^ (r & (CH - 1))) * 16);
       if (mw + r < p.a.rows) {
         if (n + 8 <= p.b.rows) {
-          store16(to + r * p.ldc, v);
+          store16<PAST>(to + r * p.ldc, v);
         } else {
           const uint32_t u[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
@@ -327,7 +334,7 @@ __global__ void __launch_bounds__(WM * WN * 64, TM * TN > 8 ? 1 : 2) k_matmul4_t
         const f32x4 v = mine[r * CH + (c ^ (r & (CH - 1)))];
         if (row < p.a.rows && k > 0) {
           if (k == 4)
-            store16(out + row * ldo + n, __builtin_bit_cast(uint4, v));
+            store16<PAST>(out + row * ldo + n, __builtin_bit_cast(uint4, v));
           else
             store4(out + row * ldo + n, v, k);
         }
@@ -521,6 +528,8 @@ hipError_t launch_matmul4(const Matmul4& p, hipStream_t s) {
   const Plan r = plan(p.a.rows, p.b.rows, p.a.cols);
   const Job4 J = {p, r.mt, r.nt, ceil_div(p.a.cols, 128), r.per, r.splits};
   const dim3 grid((unsigned)(8 * ceil_div(r.mt * r.nt * r.splits, 8)));
+  const uintptr_t rows = r.splits > 1 ? (uintptr_t)p.b.rows * 4 : (uintptr_t)p.c | (uintptr_t)(p.ldc * (p.c_type == MGN_BF16 ? 2 : 4));
+  const bool past = rows % 16 == 0;
   if (r.kind == kFew) {
     dim3 g = grid_of(r.nt);
     g.z = (unsigned)r.splits;
@@ -531,9 +540,14 @@ hipError_t launch_matmul4(const Matmul4& p, hipStream_t s) {
     else
       launch_few<4>(J, r.tn, g, s);
   } else if (r.kind == kBigTile) {
-    hipLaunchKernelGGL((k_matmul4_tile<2, 4, 4, 2, 4>), grid, dim3(512), 0, s, J);
+    if (past)
+      hipLaunchKernelGGL((k_matmul4_tile<2, 4, 4, 2, 4, true>), grid, dim3(512), 0, s, J);
+    else
+      hipLaunchKernelGGL((k_matmul4_tile<2, 4, 4, 2, 4, false>), grid, dim3(512), 0, s, J);
+  } else if (past) {
+    hipLaunchKernelGGL((k_matmul4_tile<2, 2, 2, 2, 3, true>), grid, dim3(256), 0, s, J);
   } else {
-    hipLaunchKernelGGL((k_matmul4_tile<2, 2, 2, 2, 3>), grid, dim3(256), 0, s, J);
+    hipLaunchKernelGGL((k_matmul4_tile<2, 2, 2, 2, 3, false>), grid, dim3(256), 0, s, J);
   }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || r.splits == 1) return e;

@@ -264,7 +264,8 @@ using namespace dev;
 // Reads of more than half the last-level cache (256 MB), and writes of more than all L2s
 // hold, do not pass through L2: 852,640 x 256 fp32 to both copies 264 to 234 us, 32,768 x
 // 4096 bf16 93 to 77, but 5120 x 5120 bf16, which the last level holds, 20 to 23; back to
-// fp32 852,640 x 256 (with 16 bytes a lane) 324 to 139.
+// fp32 852,640 x 256 (with 16 bytes a lane) 324 to 139, but rows that are not aligned meet
+// in L2 (5120 x 4999 bf16 14 us, past it 19).
 constexpr int64_t kLargeIn = 128LL << 20, kLargeOut = 32LL << 20;
 
 template <typename XT, bool SUMS>
@@ -300,7 +301,7 @@ hipError_t launch_quant4(const Quant4& a, hipStream_t s) {
 template <typename YT>
 void launch_back(const Dequant4& a, hipStream_t s) {
   const dim3 g = grid_of(ceil_div(ceil_div(a.a.rows, (int64_t)(32 / sizeof(YT))) * ceil_div(a.a.cols, 128), kUnits));
-  if (a.a.rows * a.a.cols * (int64_t)sizeof(YT) > kLargeOut)
+  if (a.a.rows * a.a.cols * (int64_t)sizeof(YT) > kLargeOut && (((uintptr_t)a.y | (uintptr_t)(a.ldy * sizeof(YT))) & 15) == 0)
     hipLaunchKernelGGL((k_dequant4<YT, true>), g, dim3(256), 0, s, a);
   else
     hipLaunchKernelGGL((k_dequant4<YT, false>), g, dim3(256), 0, s, a);
