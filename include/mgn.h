@@ -630,7 +630,7 @@ int mgn_group_norm_backward(const mgn_group_norm* op, mgn_rows x, const float* s
  * the clipped ones, which may be the gradient itself (same type). */
 typedef struct mgn_tensor {
   const void* in;
-  void* out; /* NULL: the list is for norms only */
+  void* out; /* NULL: counts for the norm only */
   int64_t n;
   int32_t in_type, out_type;
 } mgn_tensor;

@@ -144,7 +144,7 @@ __global__ void __launch_bounds__(256) k_grad_clip(GradClip a, int parts) {
   if (!a.clip) return;
   const double k = factor(norm, a.max_norm);
   for (int64_t i = first; i >= 0;) {
-    if (k != 1.0 || p.in != p.out) {  // else nothing changes
+    if (p.out != nullptr && (k != 1.0 || p.in != p.out)) {  // else nothing changes
       for (int at = t; at < p.n; at += 1024 * kBatch) {
         if (at != t) {
 #pragma unroll
@@ -195,7 +195,7 @@ __global__ void __launch_bounds__(1024) k_grad_clip_small(GradClip a) {
   for (int k = 0; k < H; ++k) {
     const int u = k * 1024 + t, q = u >= end, at = (u - (q ? end : 0)) * 4;
     const mgn_piece& o = p[q];
-    if (at < o.n && (f != 1.0 || o.in != o.out)) put_four(o, at, v[k], f);
+    if (at < o.n && o.out != nullptr && (f != 1.0 || o.in != o.out)) put_four(o, at, v[k], f);
   }
 }
 

@@ -40,7 +40,7 @@ struct GnJob {
   float2* means;   // [n_samples][groups]: of u and u xhat (reverse)
   double2* slots;  // forward: [tiles + n_samples][groups] sums of x and x^2
   float2* bslots;  // reverse: of u and u xhat
-  float* part;     // reverse: [tiles or n_samples][2][cols] sums of d xhat and d
+  float* part;     // reverse: [tiles or whole_blocks][2][cols] sums of d xhat and d
 };
 
 template <typename V>
@@ -118,7 +118,7 @@ __device__ __forceinline__ float activated_grad(float z, float dy) {
   return dy;
 }
 
-// The sample that row r is of: the largest s with ptr[s] <= r.  (-1: none has it.)
+// The sample that row r is of: the largest s with ptr[s] <= r.
 __device__ __forceinline__ int64_t sample_of(const mgn_group_norm& op, int64_t r) {
   if (op.sample_ptr == nullptr) return r / (op.rows / op.n_samples);
   int64_t lo = 0, hi = op.n_samples - 1;
@@ -516,8 +516,8 @@ struct WholePlace {
   int64_t s, r0, r1;
   int c0, c1, d, gs;
   double n;
-  __device__ __forceinline__ WholePlace(const GnJob& J) {
-    s = blockIdx.x;
+  __device__ __forceinline__ WholePlace(const GnJob& J, int64_t sample) {
+    s = sample;
     rows_of(J.a.op, s, r0, r1);
     d = J.a.op.cols / J.a.op.groups;
     c0 = blockIdx.y * J.p.width;
@@ -529,7 +529,7 @@ struct WholePlace {
 
 template <typename T, int ACT>
 __global__ void __launch_bounds__(256) k_group_whole(GnJob J) {
-  const WholePlace t(J);
+  const WholePlace t(J, blockIdx.x);
   const mgn_group_norm& op = J.a.op;
   Pair<double>* buf = (Pair<double>*)gn_lds;
   Pair<double>* sums = buf + blockDim.x * Run<T>::V;  // of the block's groups
@@ -554,9 +554,10 @@ __global__ void __launch_bounds__(256) k_group_whole(GnJob J) {
   }
 }
 
+// A block takes every gridDim.x-th sample, whose columns' sums it adds up in its part.
 template <typename T, int ACT>
-__global__ void __launch_bounds__(256) k_group_bwd_whole(GnJob J) {
-  const WholePlace t(J);
+__device__ __forceinline__ void bwd_whole(const GnJob& J, int64_t sample) {
+  const WholePlace t(J, sample);
   const mgn_group_norm& op = J.a.op;
   Pair<float>* buf = (Pair<float>*)gn_lds;
   Pair<float>* sums = buf + blockDim.x * Run<T>::V;
@@ -571,9 +572,10 @@ __global__ void __launch_bounds__(256) k_group_bwd_whole(GnJob J) {
     });
     if (J.part != nullptr)
       column_pairs(at, b, a, buf, [&](int col, Pair<float> w) {
-        float* to = J.part + t.s * 2 * op.cols + col;
-        to[0] = w.x;
-        to[op.cols] = w.y;
+        float* to = J.part + (int64_t)blockIdx.x * 2 * op.cols + col;
+        const bool first = t.s == blockIdx.x;
+        to[0] = first ? w.x : to[0] + w.x;
+        to[op.cols] = first ? w.y : to[op.cols] + w.y;
       });
   }
   const int g0 = t.c0 / t.d;
@@ -582,6 +584,13 @@ __global__ void __launch_bounds__(256) k_group_bwd_whole(GnJob J) {
     const Cols<T> at(c, min(c + Run<T>::strip, t.c1));
     input_gradient<T, ACT, false>(J, at, t.d, t.r0, t.r1, stats_of,
                            [&](int g) { return float2{sums[g - g0].x * inv, sums[g - g0].y * inv}; });
+  }
+}
+template <typename T, int ACT>
+__global__ void __launch_bounds__(256) k_group_bwd_whole(GnJob J) {
+  for (int64_t s = blockIdx.x; s < J.a.op.n_samples; s += gridDim.x) {
+    bwd_whole<T, ACT>(J, s);
+    __syncthreads();  // the sums have been read
   }
 }
 
@@ -618,6 +627,9 @@ GnPlan plan(const mgn_group_norm& op) {
   return p;
 }
 
+// Blocks of the reverse with a sample a block.
+int64_t whole_blocks(const mgn_group_norm& op) { return std::min<int64_t>(op.n_samples, 2048); }
+
 struct Layout {
   size_t stats, means, slots, part, total;
 };
@@ -635,7 +647,7 @@ Layout layout(const mgn_group_norm& op, const GnPlan& p, bool backward) {
     l.means = take(backward ? per * 8 : 0);
     l.slots = take((size_t)(p.tiles + op.n_samples) * op.groups * (backward ? 8 : 16));
   }
-  if (backward) l.part = take((size_t)(p.whole ? op.n_samples : p.tiles) * 2 * op.cols * 4);
+  if (backward) l.part = take((size_t)(p.whole ? whole_blocks(op) : p.tiles) * 2 * op.cols * 4);
   l.total = at;
   return l;
 }
@@ -725,7 +737,7 @@ hipError_t launch_group_norm_backward(const GroupNorm& a, hipStream_t s) {
   const GnPlan p = plan(a.op);
   const GnJob J = job(a, p, true);
   if (p.whole) {
-    const dim3 g((unsigned)a.op.n_samples, p.cblocks);
+    const dim3 g((unsigned)whole_blocks(a.op), p.cblocks);
     MGN_GN(k_group_bwd_whole, g, lds_of(a.op, 8) + (size_t)(p.width / (a.op.cols / a.op.groups)) * 8, );
   } else {
     const dim3 g((unsigned)p.tiles, p.cblocks);
@@ -742,7 +754,7 @@ hipError_t launch_group_norm_backward(const GroupNorm& a, hipStream_t s) {
       MGN_GN(k_group_bwd_apply, ga, 0, , false);
   }
   if (!J.part || !p.whole) return hipSuccess;
-  return launch_column_reduce(J.part, a.op.n_samples, a.op.cols, out, 2, a.accumulate, s);
+  return launch_column_reduce(J.part, whole_blocks(a.op), a.op.cols, out, 2, a.accumulate, s);
 }
 
 }  // namespace mgn

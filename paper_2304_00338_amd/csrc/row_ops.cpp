@@ -78,14 +78,16 @@ int check_mat4(const mgn_mat4* a, const char* who, const char* name) {
 }
 
 // c and the epilogue of a product of m x n.
-int check_epilogue(const mgn_epilogue& ep, int32_t c_type, const void* c, int64_t ldc, int64_t m, int64_t n, const char* who) {
+// tiles: whether c may be cut into 128 x 128, 256 threads each.
+int check_epilogue(const mgn_epilogue& ep, int32_t c_type, const void* c, int64_t ldc, int64_t m, int64_t n, bool tiles,
+                   const char* who) {
   if (!c || ldc < n || !fits(m, ldc) || !aligned(c, elem(c_type)))
     return fail(MGN_ERR_ARG, "%s: null or misaligned c, or its leading dimension %lld", who, (long long)ldc);
   if (!aligned(ep.bias, 4)) return fail(MGN_ERR_ARG, "%s: misaligned bias", who);
   if (ep.act == MGN_ACT_RELU_GRAD && (!is_row_type(ep.aux_type) || !ep.aux || ep.ldaux < n || !fits(m, ep.ldaux) ||
                                       !aligned(ep.aux, elem(ep.aux_type))))
     return fail(MGN_ERR_ARG, "%s: null or misaligned aux, its type or leading dimension", who);
-  if (m > 32 && ceil_div(m, 128) * ceil_div(n, 128) > (1 << 24) - 8)  // 256 threads each
+  if (tiles && ceil_div(m, 128) * ceil_div(n, 128) > (1 << 24) - 8)
     return fail(MGN_ERR_SHAPE, "%s: c of %lld x %lld is too large for one call", who, (long long)m, (long long)n);
   return MGN_OK;
 }
@@ -210,7 +212,7 @@ int mgn_matmul8(const mgn_mat8* a, const mgn_mat8* b, const mgn_epilogue* ep, in
   if (ep) m.ep = *ep;
   if (m.ep.act < MGN_ACT_NONE || m.ep.act > MGN_ACT_RELU_GRAD) return fail(MGN_ERR_ARG, "%s: unknown act %d", who, m.ep.act);
   if (a->rows == 0 || b->rows == 0) return MGN_OK;
-  if ((rc = check_epilogue(m.ep, c_type, c, ldc, a->rows, b->rows, who)) != MGN_OK) return rc;
+  if ((rc = check_epilogue(m.ep, c_type, c, ldc, a->rows, b->rows, a->rows > 32, who)) != MGN_OK) return rc;
   const size_t need = matmul8_workspace(a->rows, b->rows, a->cols);
   if (need > 0 && (!ws || ws_bytes < need || !aligned(ws, 16)))
     return fail(MGN_ERR_WORKSPACE, "%s: workspace of %zu bytes, %zu needed", who, ws_bytes, need);
@@ -326,6 +328,7 @@ int mgn_quant4(const void* x, int32_t x_type, int64_t rows, int64_t cols, int64_
     return fail(MGN_ERR_ARG, "%s: rows of qt have to start at multiples of 16 bytes", who);
   if (!aligned(scale, 4) || !aligned(scale_t, 4) || !aligned(colsum, 4))
     return fail(MGN_ERR_ARG, "%s: misaligned scales or sums", who);
+  if (q && (q == qt || scale == scale_t)) return fail(MGN_ERR_ARG, "%s: x and its transpose in the same place", who);
   if (ceil_div(rows, 16) * ceil_div(cols, 128) >= kMost)
     return fail(MGN_ERR_SHAPE, "%s: x of %lld x %lld is too large for one call", who, (long long)rows, (long long)cols);
   if (colsum && need > 0 && (!ws || ws_bytes < need || !aligned(ws, 16)))
@@ -371,7 +374,7 @@ int mgn_matmul4(const mgn_mat4* a, const mgn_mat4* b, const mgn_epilogue* ep, in
   if (ep) m.ep = *ep;
   if (m.ep.act < MGN_ACT_NONE || m.ep.act > MGN_ACT_RELU_GRAD) return fail(MGN_ERR_ARG, "%s: unknown act %d", who, m.ep.act);
   if (a->rows == 0 || b->rows == 0) return MGN_OK;
-  if ((rc = check_epilogue(m.ep, c_type, c, ldc, a->rows, b->rows, who)) != MGN_OK) return rc;
+  if ((rc = check_epilogue(m.ep, c_type, c, ldc, a->rows, b->rows, true, who)) != MGN_OK) return rc;
   const size_t need = matmul4_workspace(a->rows, b->rows, a->cols);
   if (need > 0 && (!ws || ws_bytes < need || !aligned(ws, 16)))
     return fail(MGN_ERR_WORKSPACE, "%s: workspace of %zu bytes, %zu needed", who, ws_bytes, need);

@@ -141,6 +141,28 @@ def test_given_norm():
         assert all(torch.equal(a, b) for a, b in zip(g, now))
 
 
+@pytest.mark.parametrize("sizes", [[100, 200], [100, 20000, 300, 40000, 7, 16384 * 9]])
+def test_gradients_without_a_place(sizes):
+    """Those count for the norm only (through the C entry points, which allow it)."""
+    import ctypes as C
+    g = tensors(sizes, ["fp32"])
+    out = [torch.zeros_like(t) for t in g]
+    table = (mgn.CTensor * len(g))(*[mgn.CTensor(t.data_ptr(), o.data_ptr() if i % 2 else None, t.numel(), 0, 0)
+                                     for i, (t, o) in enumerate(zip(g, out))])
+    n = C.c_int64()
+    assert mgn.lib().mgn_grad_pieces(table, len(g), None, C.byref(n)) == mgn.OK
+    pieces = (mgn.CPiece * n.value)()
+    assert mgn.lib().mgn_grad_pieces(table, len(g), pieces, C.byref(n)) == mgn.OK
+    dev = torch.frombuffer(bytearray(pieces), dtype=torch.uint8).cuda()
+    norm, ws = torch.empty(1, device="cuda"), torch.empty(2048 * 8, dtype=torch.uint8, device="cuda")
+    before = [t.clone() for t in g]
+    assert mgn.lib().mgn_grad_clip(dev.data_ptr(), n.value, 1.0, norm.data_ptr(), 0, ws.data_ptr(), ws.numel(),
+                                   torch.cuda.current_stream().cuda_stream) == mgn.OK
+    assert abs(float(norm) - exact(g)) <= 1.01 * U * exact(g)
+    check(out[1::2], g[1::2], exact(g), 1.0)
+    assert all((o == 0).all() for o in out[::2]) and all(torch.equal(a, b) for a, b in zip(g, before))
+
+
 def test_empty_tensors_only():
     g = [torch.empty(0, device="cuda")]
     assert float(mgn.mgn_grad_norm(mgn.TensorList(g))) == 0

@@ -186,6 +186,13 @@ def test_ragged(rows, cols, groups, samples, dtype):
     case(rows, cols, groups, dtype, ptr=ragged(rows, samples, rows), shift=0.3)
 
 
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("rows,cols,groups,samples", [(5000, 48, 6, 5000), (9000, 16, 2, 3000), (6300, 40, 40, 2100), (2600, 8, 1, 2600)])
+def test_many_samples(rows, cols, groups, samples, dtype):
+    """More samples of equal length than the reverse has blocks."""
+    case(rows, cols, groups, dtype, samples=samples, shift=0.3)
+
+
 @pytest.mark.parametrize("rows", [400, 30000])
 def test_rows_outside(rows):
     """Rows outside of the samples hold anything and stay as they were."""

@@ -16,7 +16,7 @@ def L():
     return mgn.lib()
 
 
-def quant4(x=P, xt=0, rows=4, cols=130, ldx=130, q=P, ldq=80, s=P, qt=P, ldqt=16, st=P, cs=NONE, acc=0, ws=NONE, n=0):
+def quant4(x=P, xt=0, rows=4, cols=130, ldx=130, q=P, ldq=80, s=P, qt=P + 4096, ldqt=16, st=P + 8192, cs=NONE, acc=0, ws=NONE, n=0):
     return L().mgn_quant4(x, xt, rows, cols, ldx, q, ldq, s, qt, ldqt, st, cs, acc, ws, n, None)
 
 
@@ -29,7 +29,7 @@ def quant4(x=P, xt=0, rows=4, cols=130, ldx=130, q=P, ldq=80, s=P, qt=P, ldqt=16
     (dict(rows=1 << 30, cols=1 << 30, ldx=1 << 30, ldq=1 << 29, ldqt=1 << 29), mgn.ERR_SHAPE),
     (dict(cs=P), mgn.ERR_WORKSPACE), (dict(cs=P, ws=P, n=519), mgn.ERR_WORKSPACE),
     (dict(cs=P, ws=P + 4, n=520), mgn.ERR_WORKSPACE), (dict(cs=P + 2, ws=P, n=520), mgn.ERR_ARG),
-    (dict(ldx=1 << 59), mgn.ERR_ARG),
+    (dict(ldx=1 << 59), mgn.ERR_ARG), (dict(q=P + 4096, qt=P + 4096), mgn.ERR_ARG), (dict(st=P, s=P, q=P + 64), mgn.ERR_ARG),
 ])
 def test_quant4_refusals(kw, code):
     assert quant4(**kw) == code
@@ -89,6 +89,9 @@ def test_matmul4_refusals():
     assert L().mgn_matmul4(None, C.byref(b), None, 0, P, 50, NONE, 0, None) == mgn.ERR_ARG
     big = mat4(rows=(1 << 31) - 1, cols=32, ld=16)
     assert go(x=big, y=mat4(rows=1 << 20, cols=32, ld=16), ldc=1 << 20) == mgn.ERR_SHAPE
+    assert go(x=mat4(rows=3, cols=32, ld=16), y=big, ldc=1 << 31) == mgn.ERR_SHAPE  # few rows may be tiles too
+    # rows 2^28 bytes apart
+    assert go(x=mat4(ld=1 << 28)) == mgn.ERR_ARG and go(y=mat4(rows=50, ld=1 << 28)) == mgn.ERR_ARG
     assert go(x=mat4(rows=0)) == mgn.OK and go(y=mat4(rows=0)) == mgn.OK
     n = C.c_size_t()
     assert L().mgn_matmul4_workspace(128, 256, 852640, C.byref(n)) == mgn.OK and n.value > 0
