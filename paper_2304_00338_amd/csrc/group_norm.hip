@@ -31,6 +31,7 @@ struct GnPlan {
   int64_t tile;  // rows of a tile of the sums
   int64_t tiles;
   int64_t atile, atiles;  // of the results
+  uint32_t even;  // rows of a sample, without sample_ptr
 };
 
 struct GnJob {
@@ -119,8 +120,9 @@ __device__ __forceinline__ float activated_grad(float z, float dy) {
 }
 
 // The sample that row r is of: the largest s with ptr[s] <= r.
-__device__ __forceinline__ int64_t sample_of(const mgn_group_norm& op, int64_t r) {
-  if (op.sample_ptr == nullptr) return r / (op.rows / op.n_samples);
+__device__ __forceinline__ int64_t sample_of(const GnJob& J, int64_t r) {
+  const mgn_group_norm& op = J.a.op;
+  if (op.sample_ptr == nullptr) return (uint32_t)r / J.p.even;
   int64_t lo = 0, hi = op.n_samples - 1;
   while (lo < hi) {
     const int64_t m = (lo + hi + 1) >> 1;
@@ -132,11 +134,11 @@ __device__ __forceinline__ int64_t sample_of(const mgn_group_norm& op, int64_t r
   return lo;
 }
 // The rows of sample s, inside the tensor whatever sample_ptr holds.
-__device__ __forceinline__ void rows_of(const mgn_group_norm& op, int64_t s, int64_t& b, int64_t& e) {
+__device__ __forceinline__ void rows_of(const GnJob& J, int64_t s, int64_t& b, int64_t& e) {
+  const mgn_group_norm& op = J.a.op;
   if (op.sample_ptr == nullptr) {
-    const int64_t n = op.rows / op.n_samples;
-    b = s * n;
-    e = b + n;
+    b = s * J.p.even;
+    e = b + J.p.even;
   } else {
     b = max((int64_t)op.sample_ptr[s], (int64_t)0);
     e = min((int64_t)op.sample_ptr[s + 1], op.rows);
@@ -144,12 +146,12 @@ __device__ __forceinline__ void rows_of(const mgn_group_norm& op, int64_t s, int
 }
 // f(s, r, e) for every sample s with rows [r, e) in [r0, r1).
 template <typename F>
-__device__ __forceinline__ void for_samples(const mgn_group_norm& op, int64_t r0, int64_t r1, F f) {
-  int64_t r = op.sample_ptr != nullptr ? max(r0, (int64_t)op.sample_ptr[0]) : r0;
+__device__ __forceinline__ void for_samples(const GnJob& J, int64_t r0, int64_t r1, F f) {
+  int64_t r = J.a.op.sample_ptr != nullptr ? max(r0, (int64_t)J.a.op.sample_ptr[0]) : r0;
   while (r < r1) {
-    const int64_t s = sample_of(op, r);
+    const int64_t s = sample_of(J, r);
     int64_t b, e;
-    rows_of(op, s, b, e);
+    rows_of(J, s, b, e);
     e = min(e, r1);
     if (e <= r) return;  // behind the last one
     f(s, r, e);
@@ -225,12 +227,37 @@ __device__ __forceinline__ float2 moments_to_stats(Pair<double> t, double n, flo
 // What a thread keeps of its columns.
 template <typename T>
 struct Vec {
-  float v[Run<T>::V];
+  static constexpr int V = Run<T>::V;
+  typedef float vec __attribute__((ext_vector_type(V), aligned(4)));
+  float v[V];
   __device__ __forceinline__ Vec(const float* p, const Cols<T>& at, float other) {
+    vec w;
+    if (p != nullptr && at.hi == V) {
+      w = *(const vec*)(p + at.col);
+    } else {
 #pragma unroll
-    for (int e = 0; e < Run<T>::V; ++e) v[e] = p != nullptr && at.has(e) ? p[at.col + e] : other;
+      for (int e = 0; e < V; ++e) w[e] = p != nullptr && e < at.hi ? p[at.col + e] : other;
+    }
+#pragma unroll
+    for (int e = 0; e < V; ++e) v[e] = w[e];
   }
 };
+// Of each column's group of d: f(group) = (x, y).
+template <typename T, typename F>
+__device__ __forceinline__ void of_groups(const Cols<T>& at, int d, F f, float (&x)[Run<T>::V], float (&y)[Run<T>::V]) {
+  int g = at.col / d, in = at.col - g * d;
+  const int last = (at.c1 - 1) / d;
+#pragma unroll
+  for (int k = 0; k < Run<T>::V; ++k) {
+    const float2 s = f(min(g, last));
+    x[k] = s.x;
+    y[k] = s.y;
+    if (++in == d) {
+      in = 0;
+      ++g;
+    }
+  }
+}
 
 // y of rows [r, e) by the statistics of their sample's groups.
 template <typename T, int ACT, bool PAST, typename S>
@@ -239,12 +266,9 @@ __device__ __forceinline__ void apply(const GnJob& J, const Cols<T>& at, int d, 
   if (!at.on) return;
   const Vec<T> gamma(J.a.op.gamma, at, 1.f), beta(J.a.op.beta, at, 0.f);
   float mean[V], f[V];
+  of_groups(at, d, stats_of, mean, f);
 #pragma unroll
-  for (int k = 0; k < V; ++k) {
-    const float2 s = at.has(k) ? stats_of((at.col + k) / d) : float2{0.f, 0.f};
-    mean[k] = s.x;
-    f[k] = s.y * gamma.v[k];
-  }
+  for (int k = 0; k < V; ++k) f[k] *= gamma.v[k];
   for (int64_t i = r + at.rl; i < e; i += U * at.RL) {
     typename Run<T>::vec v[U];
 #pragma unroll
@@ -261,19 +285,13 @@ __device__ __forceinline__ void apply(const GnJob& J, const Cols<T>& at, int d, 
   }
 }
 
-// each(k, xhat, d, gamma, rstd) for every column of rows [r, e), d = dy act'(z), then row(i).
-template <typename T, int ACT, typename S, typename F, typename G>
-__device__ __forceinline__ void reversed(const GnJob& J, const Cols<T>& at, int d, int64_t r, int64_t e, S stats_of, F each,
-                                         G row) {
+// each(k, c, d) for every column of rows [r, e), c = x - mean, d = dy act'(z), then row(i).
+// z is formed as in the forward.
+template <typename T, int ACT, typename F, typename G>
+__device__ __forceinline__ void reversed(const GnJob& J, const Cols<T>& at, int64_t r, int64_t e, const float (&mean)[Run<T>::V],
+                                         const float (&f)[Run<T>::V], F each, G row) {
   constexpr int U = 4, V = Run<T>::V;
-  const Vec<T> gamma(J.a.op.gamma, at, 1.f), beta(J.a.op.beta, at, 0.f);
-  float mean[V], rstd[V];
-#pragma unroll
-  for (int k = 0; k < V; ++k) {
-    const float2 s = at.has(k) ? stats_of((at.col + k) / d) : float2{0.f, 0.f};
-    mean[k] = s.x;
-    rstd[k] = s.y;
-  }
+  const Vec<T> beta(J.a.op.beta, at, 0.f);
   for (int64_t i = r + at.rl; i < e; i += U * at.RL) {
     typename Run<T>::vec v[U], w[U];
 #pragma unroll
@@ -286,8 +304,8 @@ __device__ __forceinline__ void reversed(const GnJob& J, const Cols<T>& at, int 
       if (i + u * at.RL < e) {
 #pragma unroll
         for (int k = 0; k < V; ++k) {
-          const float xhat = ((float)v[u][k] - mean[k]) * rstd[k];
-          each(k, xhat, activated_grad<ACT>(__builtin_fmaf(xhat, gamma.v[k], beta.v[k]), (float)w[u][k]), gamma.v[k], rstd[k]);
+          const float c = (float)v[u][k] - mean[k];
+          each(k, c, activated_grad<ACT>(__builtin_fmaf(c, f[k], beta.v[k]), (float)w[u][k]));
         }
         row(i + u * at.RL);
       }
@@ -297,32 +315,41 @@ __device__ __forceinline__ void reversed(const GnJob& J, const Cols<T>& at, int 
 template <typename T, int ACT, typename S>
 __device__ __forceinline__ void gradient_sums(const GnJob& J, const Cols<T>& at, int d, int64_t r, int64_t e, S stats_of,
                                               float (&b)[Run<T>::V], float (&a)[Run<T>::V]) {
+  constexpr int V = Run<T>::V;
 #pragma unroll
-  for (int k = 0; k < Run<T>::V; ++k) a[k] = b[k] = 0.f;
+  for (int k = 0; k < V; ++k) a[k] = b[k] = 0.f;
   if (!at.on) return;
+  const Vec<T> gamma(J.a.op.gamma, at, 1.f);
+  float mean[V], rstd[V], f[V];
+  of_groups(at, d, stats_of, mean, rstd);
+#pragma unroll
+  for (int k = 0; k < V; ++k) f[k] = rstd[k] * gamma.v[k];
   reversed<T, ACT>(
-      J, at, d, r, e, stats_of,
-      [&](int k, float xhat, float g, float, float) {
+      J, at, r, e, mean, f,
+      [&](int k, float c, float g) {
         a[k] += g;
-        b[k] = __builtin_fmaf(g, xhat, b[k]);
+        b[k] = __builtin_fmaf(g, c * rstd[k], b[k]);
       },
       [](int64_t) {});
 }
+// dx = rstd (gamma d - the mean of u - xhat times that of u xhat).
 template <typename T, int ACT, bool PAST, typename S, typename M>
 __device__ __forceinline__ void input_gradient(const GnJob& J, const Cols<T>& at, int d, int64_t r, int64_t e, S stats_of, M means_of) {
+  constexpr int V = Run<T>::V;
   if (!at.on) return;
-  float m1[Run<T>::V], m2[Run<T>::V], dx[Run<T>::V];
+  const Vec<T> gamma(J.a.op.gamma, at, 1.f);
+  float mean[V], rstd[V], f[V], m1[V], m2[V], dx[V];
+  of_groups(at, d, stats_of, mean, rstd);
+  of_groups(at, d, means_of, m1, m2);
 #pragma unroll
-  for (int k = 0; k < Run<T>::V; ++k) {
-    const float2 s = at.has(k) ? means_of((at.col + k) / d) : float2{0.f, 0.f};
-    m1[k] = s.x;
-    m2[k] = s.y;
+  for (int k = 0; k < V; ++k) {
+    f[k] = rstd[k] * gamma.v[k];
+    m1[k] *= rstd[k];
+    m2[k] *= rstd[k];
   }
   reversed<T, ACT>(
-      J, at, d, r, e, stats_of,
-      [&](int k, float xhat, float g, float gamma, float rstd) {
-        dx[k] = rstd * (__builtin_fmaf(gamma, g, -m1[k]) - xhat * m2[k]);
-      },
+      J, at, r, e, mean, f,
+      [&](int k, float c, float g) { dx[k] = __builtin_fmaf(f[k], g, -m1[k]) - c * rstd[k] * m2[k]; },
       [&](int64_t i) { at.template store<PAST>(J.a.dx, i, dx); });
 }
 // A strip's columns' sums over the threads that share them: put(column, sums).
@@ -379,7 +406,7 @@ __global__ void __launch_bounds__(256) k_group_moments(GnJob J) {
   Pair<double>* buf = (Pair<double>*)gn_lds;
   for (int c = t.c0; c < t.c1; c += Run<T>::strip) {
     const Cols<T> at(c, min(c + Run<T>::strip, t.c1));
-    for_samples(op, t.r0, t.r1, [&](int64_t s, int64_t r, int64_t e) {
+    for_samples(J, t.r0, t.r1, [&](int64_t s, int64_t r, int64_t e) {
       double s1[Run<T>::V], s2[Run<T>::V];
       moments<T>(J.a.x, at, r, e, s1, s2);
       group_sums(at, t.d, s1, s2, buf, [&](int g, Pair<double> v) {
@@ -429,7 +456,7 @@ __global__ void __launch_bounds__(512) k_group_join(GnJob J) {
   const int64_t s = blockIdx.x / gblocks;
   const int g = (int)(blockIdx.x - s * gblocks) * 32 + lane;
   int64_t b, e;
-  rows_of(op, s, b, e);
+  rows_of(J, s, b, e);
   const bool any = e > b;
   const int64_t t0 = any ? b / J.p.tile : 0, t1 = any ? (e - 1) / J.p.tile : -1;
   if (g < op.groups) {
@@ -461,7 +488,7 @@ __global__ void __launch_bounds__(256) k_group_apply(GnJob J) {
   const mgn_group_norm& op = J.a.op;
   for (int c = t.c0; c < t.c1; c += Run<T>::strip) {
     const Cols<T> at(c, min(c + Run<T>::strip, t.c1));
-    for_samples(op, t.r0, t.r1, [&](int64_t s, int64_t r, int64_t e) {
+    for_samples(J, t.r0, t.r1, [&](int64_t s, int64_t r, int64_t e) {
       apply<T, ACT, PAST>(J, at, t.d, r, e, [&](int g) { return J.stats[s * op.groups + g]; });
     });
   }
@@ -475,7 +502,7 @@ __global__ void __launch_bounds__(256) k_group_bwd_sums(GnJob J) {
   for (int c = t.c0; c < t.c1; c += Run<T>::strip) {
     const Cols<T> at(c, min(c + Run<T>::strip, t.c1));
     float ta[Run<T>::V] = {}, tb[Run<T>::V] = {};
-    for_samples(op, t.r0, t.r1, [&](int64_t s, int64_t r, int64_t e) {
+    for_samples(J, t.r0, t.r1, [&](int64_t s, int64_t r, int64_t e) {
       float a[Run<T>::V], b[Run<T>::V], u[Run<T>::V], v[Run<T>::V];
       gradient_sums<T, ACT>(J, at, t.d, r, e, [&](int g) { return J.stats[s * op.groups + g]; }, b, a);
       times_gamma(J, at, u, v, a, b);
@@ -504,7 +531,7 @@ __global__ void __launch_bounds__(256) k_group_bwd_apply(GnJob J) {
   const mgn_group_norm& op = J.a.op;
   for (int c = t.c0; c < t.c1; c += Run<T>::strip) {
     const Cols<T> at(c, min(c + Run<T>::strip, t.c1));
-    for_samples(op, t.r0, t.r1, [&](int64_t s, int64_t r, int64_t e) {
+    for_samples(J, t.r0, t.r1, [&](int64_t s, int64_t r, int64_t e) {
       input_gradient<T, ACT, PAST>(J, at, t.d, r, e, [&](int g) { return J.stats[s * op.groups + g]; },
                              [&](int g) { return J.means[s * op.groups + g]; });
     });
@@ -518,7 +545,7 @@ struct WholePlace {
   double n;
   __device__ __forceinline__ WholePlace(const GnJob& J, int64_t sample) {
     s = sample;
-    rows_of(J.a.op, s, r0, r1);
+    rows_of(J, s, r0, r1);
     d = J.a.op.cols / J.a.op.groups;
     c0 = blockIdx.y * J.p.width;
     c1 = min(c0 + J.p.width, J.a.op.cols);
@@ -624,6 +651,7 @@ GnPlan plan(const mgn_group_norm& op) {
   p.tiles = p.whole ? 0 : ceil_div(op.rows, p.tile);
   p.atile = rows_of(kResultBlocks) > rl * 64 ? rl * 16 : rows_of(kResultBlocks);
   p.atiles = p.whole ? 0 : ceil_div(op.rows, p.atile);
+  p.even = (uint32_t)(op.rows / op.n_samples);
   return p;
 }
 
