@@ -440,7 +440,7 @@ __global__ void __launch_bounds__(512) k_group_join(GnJob J) {
   if (MEANS && blockIdx.x >= op.n_samples * gblocks) {
     const int64_t c = (blockIdx.x - op.n_samples * gblocks) * 32 + lane;
     if (c < op.cols) {
-#pragma unroll 4
+#pragma unroll 8
       for (int64_t i = part; i < J.p.tiles; i += P) {
         const float* v = J.part + i * 2 * op.cols + c;
         t.x += v[0];
@@ -460,7 +460,7 @@ __global__ void __launch_bounds__(512) k_group_join(GnJob J) {
   const bool any = e > b;
   const int64_t t0 = any ? b / J.p.tile : 0, t1 = any ? (e - 1) / J.p.tile : -1;
   if (g < op.groups) {
-#pragma unroll 4
+#pragma unroll 8
     for (int64_t i = t0 + part; i <= t1; i += P) {
       const int64_t at = (i + s) * op.groups + g;
       if constexpr (MEANS) {
@@ -629,10 +629,10 @@ namespace {
 
 // Blocks that tiles are cut for: as many sums as run at a time (three a CU; 307,981 x 128
 // fp32, forward and reverse 96 and 142 us, with 2048 blocks 96 and 154), and as many
-// results, four a CU, or tiles of 16 rows a thread where these are more than four rounds
-// (852,640 x 128 fp32 231 and 397 us, one round 245 and 415).
+// results, in fp32 four a CU (with three the reverse 151, of 307,981 x 128 bf16 83, with four
+// 87), or tiles of 16 rows a thread where these are more than four rounds (852,640 x 128 fp32
+// 231 and 397 us, one round 245 and 415).
 constexpr int kSumBlocks = 768, kResultBlocks = 1024;
-
 
 GnPlan plan(const mgn_group_norm& op) {
   GnPlan p;
@@ -649,7 +649,8 @@ GnPlan plan(const mgn_group_norm& op) {
   auto rows_of = [&](int64_t blocks) { return std::max(ceil_div(op.rows * p.cblocks, blocks), rl * 4); };
   p.tile = rows_of(kSumBlocks);
   p.tiles = p.whole ? 0 : ceil_div(op.rows, p.tile);
-  p.atile = rows_of(kResultBlocks) > rl * 64 ? rl * 16 : rows_of(kResultBlocks);
+  const int64_t results = rows_of(size == 2 ? kSumBlocks : kResultBlocks);
+  p.atile = results > rl * 64 ? rl * 16 : results;
   p.atiles = p.whole ? 0 : ceil_div(op.rows, p.atile);
   p.even = (uint32_t)(op.rows / op.n_samples);
   return p;
