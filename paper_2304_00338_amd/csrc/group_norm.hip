@@ -123,13 +123,15 @@ __device__ __forceinline__ float activated_grad(float z, float dy) {
 __device__ __forceinline__ int64_t sample_of(const GnJob& J, int64_t r) {
   const mgn_group_norm& op = J.a.op;
   if (op.sample_ptr == nullptr) return (uint32_t)r / J.p.even;
-  int64_t lo = 0, hi = op.n_samples - 1;
-  while (lo < hi) {
-    const int64_t m = (lo + hi + 1) >> 1;
-    if (op.sample_ptr[m] <= r)
-      lo = m;
-    else
-      hi = m - 1;
+  // every lane looks at one of 64 places: a trip to memory for each 64 times as many samples
+  const uint32_t lane = threadIdx.x & 63;
+  uint32_t lo = 0, n = (uint32_t)op.n_samples;
+  while (n > 1) {
+    const uint32_t step = (n + 63) / 64, at = lane * step;
+    const uint64_t m = __ballot(at < n && op.sample_ptr[lo + at] <= r);
+    const uint32_t j = m != 0 ? 63 - (uint32_t)__builtin_clzll(m) : 0;
+    lo += j * step;
+    n = min(step, n - j * step);
   }
   return lo;
 }
@@ -160,16 +162,30 @@ __device__ __forceinline__ void for_samples(const GnJob& J, int64_t r0, int64_t 
 }
 
 // Sums over a strip's rows and the columns of each of its groups (d columns) from every
-// thread's: put(g, sums) by one thread for each group.  buf: a pair for each of
-// the block's threads' columns.  Ends with the block together.
+// thread's: put(g, sums) by one thread for each group.  As many neighbouring columns as
+// divide d and the runs are added first.  buf: a pair for each of the block's threads'
+// columns.  Ends with the block together.
 template <typename T, typename V, typename F>
 __device__ __forceinline__ void group_sums(const Cols<T>& at, int d, const V (&s1)[Run<T>::V], const V (&s2)[Run<T>::V],
                                            Pair<V>* buf, F put) {
-  const int w = at.c1 - at.c0, gs = max(w / d, 1), dw = min(d, w);
+  constexpr int N = Run<T>::V;
+  Pair<V> v[N];
+#pragma unroll
+  for (int e = 0; e < N; ++e) v[e] = {s1[e], s2[e]};
+  int q = 1;
+#pragma unroll
+  for (int k = N; k > 1; k >>= 1) {
+    if ((d & (2 * q - 1)) == 0) {
+#pragma unroll
+      for (int e = 0; e < k / 2; ++e) v[e] = {v[2 * e].x + v[2 * e + 1].x, v[2 * e].y + v[2 * e + 1].y};
+      q *= 2;
+    }
+  }
+  const int w = (at.c1 - at.c0) / q, gs = max((at.c1 - at.c0) / d, 1), dw = min(d, at.c1 - at.c0) / q;
   if (at.on) {
 #pragma unroll
-    for (int e = 0; e < Run<T>::V; ++e)
-      if (at.has(e)) buf[at.rl * w + at.col - at.c0 + e] = Pair<V>{s1[e], s2[e]};
+    for (int e = 0; e < N; ++e)
+      if (e * q >= at.lo && e * q < at.hi) buf[at.rl * w + (at.col - at.c0) / q + e] = v[e];
   }
   __syncthreads();
   int P = 64;
@@ -180,9 +196,9 @@ __device__ __forceinline__ void group_sums(const Cols<T>& at, int d, const V (&s
     Pair<V> t = {0, 0};
     for (int i = p; i < n; i += P) {
       const int rl = (int)(((float)i + 0.5f) * inv);
-      const Pair<V> v = buf[rl * w + g * dw + (i - rl * dw)];
-      t.x += v.x;
-      t.y += v.y;
+      const Pair<V> u = buf[rl * w + g * dw + (i - rl * dw)];
+      t.x += u.x;
+      t.y += u.y;
     }
     for (int k = P >> 1; k > 0; k >>= 1) {
       t.x += __shfl_xor(t.x, k);
@@ -633,6 +649,10 @@ namespace {
 // 87), or tiles of 16 rows a thread where these are more than four rounds (852,640 x 128 fp32
 // 231 and 397 us, one round 245 and 415).
 constexpr int kSumBlocks = 768, kResultBlocks = 1024;
+// Rows of a thread, on average, up to which a small call takes one block for a sample (128 bf16
+// columns, both directions through the binding: 300 rows, 19 a thread, 39 us, by tiles 43; 800
+// rows 78, 44; 400 rows of 40 samples 37, 110).
+constexpr int kWholeRows = 20;
 
 GnPlan plan(const mgn_group_norm& op) {
   GnPlan p;
@@ -643,9 +663,9 @@ GnPlan plan(const mgn_group_norm& op) {
   p.cblocks = (int)ceil_div(op.groups, std::max(strip / d, 1));
   p.width = (int)ceil_div(op.groups, p.cblocks) * d;
   const int64_t bytes = op.rows * p.width * size;
-  p.whole = bytes <= (1 << 20) ||
-            (op.sample_ptr == nullptr && bytes / op.n_samples <= (1 << 17) && op.n_samples * p.cblocks >= 256);
   const int64_t lanes = ceil_div(std::min(p.width, strip), run), rl = std::max<int64_t>(256 / lanes, 1);
+  p.whole = (bytes <= (1 << 20) && op.rows <= kWholeRows * rl * op.n_samples) ||
+            (op.sample_ptr == nullptr && bytes / op.n_samples <= (1 << 17) && op.n_samples * p.cblocks >= 256);
   auto rows_of = [&](int64_t blocks) { return std::max(ceil_div(op.rows * p.cblocks, blocks), rl * 4); };
   p.tile = rows_of(kSumBlocks);
   p.tiles = p.whole ? 0 : ceil_div(op.rows, p.tile);

@@ -153,7 +153,7 @@ SHAPES = [(1, 1, 1), (1, 8, 1), (2, 5, 1), (7, 9, 3), (64, 128, 32), (33, 150, 1
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
 @pytest.mark.parametrize("rows,cols,groups", SHAPES)
 def test_shapes(rows, cols, groups, dtype):
-    """Small calls: a block for a sample."""
+    """Small calls, most of them by a block for a sample."""
     case(rows, cols, groups, dtype)
 
 
