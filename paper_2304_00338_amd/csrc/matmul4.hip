@@ -357,6 +357,8 @@ __global__ void __launch_bounds__(WM * WN * 64, TM * TN > 8 ? 1 : 2) k_matmul4_t
 // A block takes TN times 16 rows of b, its 8 waves the steps of 256 columns in turn;
 // operands come straight from memory, 16 bytes a lane (four lanes cover a row's 128
 // columns, two loads its 128-byte line), a step ahead, and the waves' sums meet in LDS.
+// Measured: 1 x 4096 x 4096 4.2 us, 21 x 9001 x 6000 9.4 (188 blocks; 2.9 TB/s of weights that
+// the last-level cache holds), 32 x 14,336 x 4096 10.5.
 template <int TM, int TN>
 __global__ void __launch_bounds__(512) k_matmul4_few(Job4 J) {
   constexpr int NWV = 8;
