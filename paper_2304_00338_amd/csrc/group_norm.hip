@@ -655,10 +655,15 @@ namespace {
 // 87), or tiles of 16 rows a thread where these are more than four rounds (852,640 x 128 fp32
 // 231 and 397 us, one round 245 and 415).
 constexpr int kSumBlocks = 768, kResultBlocks = 1024;
-// Rows of a thread, on average, up to which a small call takes one block for a sample (128 bf16
-// columns, both directions through the binding: 300 rows, 19 a thread, 39 us, by tiles 43; 800
-// rows 78, 44; 400 rows of 40 samples 37, 110).
-constexpr int kWholeRows = 20;
+// A block takes a sample's rows where a thread has up to kWholeRows of them, a third on
+// average where samples are ragged (and 128 if one has all rows), and the call is of up to
+// kWholeBytes, 16 times that where they are not; or where samples of equal length fill the
+// device.  Both directions through the binding, by tiles in brackets: 1200 x 128 bf16 41 us
+// (46), 2000 rows 56 (46); 4000 x 128 fp32 of 8 ragged samples 37 (47); 2000 x 4096 bf16 of 20
+// samples 38 (57), ragged 54 (61); 51,200 x 256 fp32 of 100 77 (93); 3000 x 640 bf16 of 5 ragged
+// ones 58 (47); 6000 x 640 fp32 of 10 by 80 bytes of a row 55 (47).  By 64 bytes of a row instead
+// of all of it: 424 x 640 bf16 of 8 37 us, 81.
+constexpr int64_t kWholeRows = 24, kWholeBytes = 4 << 20;
 
 GnPlan plan(const mgn_group_norm& op) {
   GnPlan p;
@@ -669,9 +674,21 @@ GnPlan plan(const mgn_group_norm& op) {
   p.cblocks = (int)ceil_div(op.groups, std::max(strip / d, 1));
   p.width = (int)ceil_div(op.groups, p.cblocks) * d;
   const int64_t bytes = op.rows * p.width * size;
-  const int64_t lanes = ceil_div(std::min(p.width, strip), run), rl = std::max<int64_t>(256 / lanes, 1);
-  p.whole = (bytes <= (1 << 20) && op.rows <= kWholeRows * rl * op.n_samples) ||
-            (op.sample_ptr == nullptr && bytes / op.n_samples <= (1 << 17) && op.n_samples * p.cblocks >= 256);
+  auto rows_at_once = [&](int64_t width) { return std::max<int64_t>(256 / ceil_div(std::min<int64_t>(width, strip), run), 1); };
+  const int64_t rl = rows_at_once(p.width);
+  // a block for a sample takes some 64 or 128 bytes of a row, more where there are many
+  const bool even = op.sample_ptr == nullptr;
+  const int64_t total = op.rows * op.cols * size, least = total <= kWholeBytes ? 64 : 128;
+  const int64_t per = std::max((least + d * size / 2) / (d * size), ceil_div(op.groups * op.n_samples, (int64_t)kResultBlocks));
+  const int64_t blocks = ceil_div(op.groups, std::clamp<int64_t>(per, 1, std::max(strip / d, 1)));
+  const int64_t width = ceil_div(op.groups, blocks) * d, wrl = rows_at_once(width);
+  p.whole = even ? (total <= 16 * kWholeBytes && op.rows <= kWholeRows * wrl * op.n_samples) ||
+                       (bytes / op.n_samples <= (1 << 17) && op.n_samples * p.cblocks >= 256)
+                 : total <= kWholeBytes && op.rows <= kWholeRows / 3 * wrl * op.n_samples && op.rows <= 128 * wrl;
+  if (p.whole) {
+    p.width = (int)width;
+    p.cblocks = (int)ceil_div(op.groups, width / d);
+  }
   auto rows_of = [&](int64_t blocks) { return std::max(ceil_div(op.rows * p.cblocks, blocks), rl * 4); };
   p.tile = rows_of(kSumBlocks);
   p.tiles = p.whole ? 0 : ceil_div(op.rows, p.tile);
