@@ -193,6 +193,17 @@ def test_many_samples(rows, cols, groups, samples, dtype):
     case(rows, cols, groups, dtype, samples=samples, shift=0.3)
 
 
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("rows,cols,groups,samples", [(2000, 4096, 32, 20), (5120, 250, 25, 10), (7424, 160, 32, 8), (424, 640, 128, 8),
+                                                      (1500, 128, 32, 1), (900, 66, 33, 3), (1000, 72, 2, 250)])
+def test_few_columns_a_block(rows, cols, groups, samples, dtype):
+    """Blocks of some groups' columns and all rows of a sample; the same of ragged samples, one
+    of which has nearly all rows."""
+    case(rows, cols, groups, dtype, samples=samples, shift=0.3)
+    ptr = [0] * samples + [rows] if samples < 9 else [0, 3] + [rows - 5] * (samples - 2) + [rows]
+    case(rows, cols, groups, dtype, ptr=ptr, shift=0.3)
+
+
 @pytest.mark.parametrize("rows", [400, 30000])
 def test_rows_outside(rows):
     """Rows outside of the samples hold anything and stay as they were."""
