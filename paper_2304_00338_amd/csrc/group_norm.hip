@@ -376,7 +376,8 @@ __device__ __forceinline__ void input_gradient(const GnJob& J, const Cols<T>& at
 }
 // A strip's columns' sums over the threads that share them: put(column, sums).
 template <typename T, typename F>
-__device__ __forceinline__ void column_pairs(const Cols<T>& at, const float (&s1)[Run<T>::V], const float (&s2)[Run<T>::V], Pair<float>* buf, F put) {
+__device__ __forceinline__ void column_pairs(const Cols<T>& at, const float (&s1)[Run<T>::V], const float (&s2)[Run<T>::V],
+                                             Pair<float>* buf, F put) {
   const int w = at.c1 - at.c0;
   if (at.on) {
 #pragma unroll
@@ -395,8 +396,8 @@ __device__ __forceinline__ void column_pairs(const Cols<T>& at, const float (&s1
   __syncthreads();
 }
 template <typename T>
-__device__ __forceinline__ void times_gamma(const GnJob& J, const Cols<T>& at, float (&u)[Run<T>::V], float (&v)[Run<T>::V], const float (&a)[Run<T>::V],
-                                            const float (&b)[Run<T>::V]) {
+__device__ __forceinline__ void times_gamma(const GnJob& J, const Cols<T>& at, float (&u)[Run<T>::V], float (&v)[Run<T>::V],
+                                            const float (&a)[Run<T>::V], const float (&b)[Run<T>::V]) {
   const Vec<T> gamma(J.a.op.gamma, at, 1.f);
 #pragma unroll
   for (int k = 0; k < Run<T>::V; ++k) {
