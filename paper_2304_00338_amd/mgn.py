@@ -665,6 +665,14 @@ def _at(t):
     return None if t is None else t.data_ptr()
 
 
+def _matrix_ld(q):
+    """Leading dimension of a matrix's numbers, whose columns have to be adjacent: of one
+    row, whose stride means nothing, its columns rounded up to a multiple of 16."""
+    r, c = q.shape
+    ld = _row_ld(q, "q") if r > 0 else c
+    return ld if r > 1 else -(-c // 16) * 16
+
+
 class Mat8:
     """An mgn_mat8 of include/mgn.h: q, a float8_e4m3fn or float8_e5m2 tensor
     [rows][ld >= cols] whose bytes from cols to the next multiple of 16 are
@@ -933,7 +941,7 @@ class Mat4:
         rows, width = q.shape
         cols = int(cols)
         need = -(-cols // 32) * 16
-        ld = _row_ld(q, "q") if rows > 1 else -(-width // 16) * 16
+        ld = _matrix_ld(q)
         if cols < 0 or (width < need and rows > 0):
             raise MgnError(ERR_ARG, f"q has {width} bytes a row for {cols} columns: {need} are needed")
         want = (-(-cols // 128), rows, 4)
