@@ -693,7 +693,7 @@ class Mat8:
         cols = width if cols is None else int(cols)
         if block_rows not in (1, 128):
             raise MgnError(ERR_ARG, f"blocks of {block_rows} rows (1 or 128)")
-        ld = _row_ld(q, "q") if rows > 1 else -(-width // 16) * 16
+        ld = _matrix_ld(q)
         if not 0 <= cols <= width or (width < -(-cols // 16) * 16 and rows > 0):
             raise MgnError(ERR_ARG, f"q has {width} columns for {cols}: rows are padded to multiples of 16")
         want = (-(-cols // 128), -(-rows // block_rows))

@@ -44,3 +44,21 @@ def test_mat4_one_row_of_any_stride():
         m = mgn.Mat4(q, scale4(1, cols), cols)
         assert (m.rows, m.cols, m.struct.ld, m.struct.q) == (1, cols, ld, q.data_ptr())
     assert mgn.Mat4(wide[:0, ::2], scale4(0, 64), 64).rows == 0
+
+
+@pytest.mark.parametrize("dtype", [torch.float8_e4m3fn, torch.float8_e5m2])
+@pytest.mark.parametrize("rows", [1, 2])
+def test_mat8_columns_apart(rows, dtype):
+    for q in spread(rows, dtype):
+        if q.shape[0] == rows:
+            for block in (1, 128):
+                with pytest.raises(mgn.MgnError, match="adjacent"):
+                    mgn.Mat8(on(q), torch.ones(1, rows if block == 1 else 1), 32, block)
+
+
+def test_mat8_one_row_of_any_stride():
+    wide = on(torch.zeros(5, 75, dtype=torch.float8_e4m3fn))
+    for q, cols, ld in ((wide[2:3, 16:48], 20, 32), (wide[:1], 64, 80), (wide[:1, :16], 16, 16)):
+        m = mgn.Mat8(q, torch.ones(1, 1), cols)
+        assert (m.rows, m.cols, m.struct.ld, m.struct.q) == (1, cols, ld, q.data_ptr())
+    assert mgn.Mat8(wide[:0, ::2], torch.ones(1, 0), 32).rows == 0
