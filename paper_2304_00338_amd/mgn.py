@@ -1070,6 +1070,11 @@ def _group_norm(x, groups, gamma, beta, act, samples, sample_ptr, eps):
     dev = x.device
     if act not in GROUP_ACTS:
         raise MgnError(ERR_ARG, f"unknown act {act!r}")
+    if not 1 <= cols <= NORM_MAX_COLS:  # here: the struct's fields hold 32 bits of these
+        raise MgnError(ERR_SHAPE, f"{cols} columns (1 to {NORM_MAX_COLS})")
+    groups = int(groups)
+    if groups < 1 or cols % groups != 0:
+        raise MgnError(ERR_ARG, f"{groups} groups do not divide {cols} columns")
     if sample_ptr is None:
         n = 1 if samples is None else int(samples)
     else:
@@ -1082,7 +1087,7 @@ def _group_norm(x, groups, gamma, beta, act, samples, sample_ptr, eps):
         _dptr(sample_ptr, torch.int32, (n + 1,), "sample_ptr")
         if sample_ptr.device != dev:
             raise MgnError(ERR_ARG, f"sample_ptr is on {sample_ptr.device}, expected {dev}")
-    return CGroupNorm(rows, cols, int(groups), xt, GROUP_ACTS[act], eps, _vector(gamma, "gamma", cols, dev),
+    return CGroupNorm(rows, cols, groups, xt, GROUP_ACTS[act], eps, _vector(gamma, "gamma", cols, dev),
                       _vector(beta, "beta", cols, dev), _at(sample_ptr), n)
 
 
