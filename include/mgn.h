@@ -558,7 +558,8 @@ typedef struct mgn_mat4 {
  * power of two that puts their largest magnitude in [3.5, 7) (4 or 6 to the nearest
  * number), from 2^-127 on (for smaller ones, and for zeros, 2^-127); a value becomes the
  * number nearest x / X, ties to the even mantissa.  Where one of the 32 is an infinity or
- * a NaN, s is 255 and the numbers are zero.
+ * a NaN, s is 255 and the numbers are zero.  Finite magnitudes from 3.5 times 2^126 (2.98e38)
+ * on become 4 times 2^126 = 2^128, which mgn_dequant4 reads back as an infinity.
  * q, scale: x as an mgn_mat4 (NULL: not wanted).  qt, scale_t: the transpose
  * [cols][rows], whose scales are of 32 rows of one column of x (NULL: not wanted).
  * colsum (nullable): [cols] sums of x over its rows (the gradient of a bias), added to
@@ -570,8 +571,9 @@ int mgn_quant4(const void* x, int32_t x_type, int64_t rows, int64_t cols, int64_
                int64_t ldq, uint8_t* scale, uint8_t* qt, int64_t ldqt, uint8_t* scale_t,
                float* colsum, int32_t accumulate, void* workspace, size_t ws_bytes, void* stream);
 
-/* The values of a as rows of y_type (MGN_FP32, MGN_BF16), [a->rows][ldy].  Exact in both
- * (but for 6 times 2^127 and 4 times 2^127, which are infinities).
+/* The values of a as rows of y_type (MGN_FP32, MGN_BF16), [a->rows][ldy].  Exact in both,
+ * but for values of 2^128 and more (numbers from 2 on times 2^127, 4 and 6 times 2^126), which
+ * become infinities.
  * Errors: ARG, SHAPE, DEVICE. */
 int mgn_dequant4(const mgn_mat4* a, int32_t y_type, void* y, int64_t ldy, void* stream);
 
