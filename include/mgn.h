@@ -560,6 +560,10 @@ typedef struct mgn_mat4 {
  * number nearest x / X, ties to the even mantissa.  Where one of the 32 is an infinity or
  * a NaN, s is 255 and the numbers are zero.  Finite magnitudes from 3.5 times 2^126 (2.98e38)
  * on become 4 times 2^126 = 2^128, which mgn_dequant4 reads back as an infinity.
+ * (The Open Compute Project's MX document gives floor(log2 amax) - 2 as X's exponent and clips
+ * [7 X, 8 X) to 6 X.  Here X is one power more where amax's mantissa is 1.75 or more, and
+ * amax becomes 4 X: such blocks' scales and numbers are not those of programs that go by
+ * the document.  Both kinds are read alike.)
  * q, scale: x as an mgn_mat4 (NULL: not wanted).  qt, scale_t: the transpose
  * [cols][rows], whose scales are of 32 rows of one column of x (NULL: not wanted).
  * colsum (nullable): [cols] sums of x over its rows (the gradient of a bias), added to
