@@ -9,9 +9,11 @@
 // has, since of two such pairs one has the larger tile or sample and neither the smaller.
 // A second joins a sample's slots in order, a third reads the rows again and writes the
 // results.
-// Sums of x and x^2 are of 64 bits, exact enough for any mean: var = E x^2 - (E x)^2
-// loses (mean / std)^2 2^-53.  Small calls take one block for a sample and group columns
-// instead, in one launch.
+// Sums of x and x^2 are of 64 bits: var = E x^2 - (E x)^2 loses (mean / std)^2 2^-53 an
+// addition.  The mean is then rounded to float32, as stats keep it, which shifts xhat of a whole
+// group by up to 2^-24 |mean| / std: as much as half a step of x itself at its mean does, and
+// the reverse, which has z and xhat to the bit, takes them so.  Small calls take one block for a
+// sample and group columns instead, in one launch.
 //
 // Bound by memory in fp32: 307,981 x 128 with SiLU, forward 34 us for the sums (4.7 TB/s) and 50
 // for the results (6.3), reverse 53 (5.9) and 75 (6.3), joins 5 and 6.  In bf16 the vector

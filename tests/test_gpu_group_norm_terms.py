@@ -196,3 +196,16 @@ def test_equal_samples(rows, cols, groups, samples, dtype):
 @pytest.mark.parametrize("rows,cols,groups,ptr", RAGGED)
 def test_ragged_samples(rows, cols, groups, ptr, dtype):
     case(rows, cols, groups, dtype, ptr=ptr, seed=rows)
+
+
+@GPU
+@pytest.mark.parametrize("shift", [1e2, 1e4, 1e6])
+@pytest.mark.parametrize("rows", [60, 30000])
+def test_far_mean(rows, shift):
+    """A mean of many deviations shifts xhat by its rounding to float32, and costs no more; up
+    to 10^4 deviations the reverse's terms are still far larger than that."""
+    terms = ["m1", "m2", "dgamma", "dbeta"] if shift <= 1e4 else []
+    for act in ("none", "silu"):
+        case(rows, 32, 4, "fp32", act, seed=2, shift=shift, terms=terms)
+    if shift == 1e2:
+        case(rows, 32, 4, "bf16", seed=2, shift=shift, terms=["m1"])
