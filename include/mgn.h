@@ -567,7 +567,9 @@ typedef struct mgn_mat4 {
  * q, scale: x as an mgn_mat4 (NULL: not wanted).  qt, scale_t: the transpose
  * [cols][rows], whose scales are of 32 rows of one column of x (NULL: not wanted).
  * colsum (nullable): [cols] sums of x over its rows (the gradient of a bias), added to
- * what is there with accumulate != 0; the workspace is needed for it only.
+ * what is there with accumulate != 0; float32 throughout, of 128 rows first and then of those,
+ * so that of a million rows some 50 additions are on each one's way; the workspace is needed for
+ * it only.
  * Errors: ARG, SHAPE (2^31 rows or columns, or rows x cols of 2^42), WORKSPACE,
  * DEVICE. */
 int mgn_quant4_workspace(int64_t rows, int64_t cols, size_t* ws_bytes);
@@ -596,7 +598,7 @@ int mgn_matmul4(const mgn_mat4* a, const mgn_mat4* b, const mgn_epilogue* epilog
  *   xhat = (x - mean) / sqrt(var + eps) over a sample's rows and a group's channels
  *   (biased variance),  z = gamma xhat + beta,  y = act(z).
  * act is MGN_ACT_NONE, MGN_ACT_RELU or */
-#define MGN_ACT_SILU 3 /* z / (1 + exp(-z)) (mgn_group_norm only) */
+#define MGN_ACT_SILU 3 /* z / (1 + exp(-z)) (mgn_group_norm only), to some (|z| + 8) 2^-24 */
 typedef struct mgn_group_norm {
   int64_t rows;
   int32_t cols;   /* 1 .. MGN_NORM_MAX_COLS */
@@ -629,7 +631,10 @@ int mgn_group_norm_forward(const mgn_group_norm* op, mgn_rows x, mgn_rows y, flo
 /* Reverse: from x, the forward's stats and the gradient dy of y the gradient dx, and
  * (each nullable, float32 [cols], added to what is there with accumulate != 0) dgamma
  * and dbeta, summed over all samples.  xhat is the forward's, with its shift by the mean's
- * rounding.  dx may be dy or x (with the same ld).
+ * rounding.  Sums are of float32 within a block, which has one or more samples in small calls,
+ * else a 768th of the rows, and of 64 bits over such parts of the rows (of a million rows of 128
+ * columns some 170 additions are on an element's way into its group's and its column's sum).
+ * dx may be dy or x (with the same ld).
  * Errors: ARG, SHAPE, WORKSPACE, DEVICE. */
 int mgn_group_norm_backward(const mgn_group_norm* op, mgn_rows x, const float* stats, mgn_rows dy,
                             mgn_rows dx, float* dgamma, float* dbeta, int32_t accumulate,
