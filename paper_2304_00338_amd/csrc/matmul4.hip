@@ -37,7 +37,12 @@ __device__ __forceinline__ i32x8 operand(uint4 v) { return i32x8{(int)v.x, (int)
 // 16 bytes of a result.  PAST: past the caches, where rows are aligned: results that stay
 // in L2 push out the operands (32,768 x 4096 x 1024 to fp32 170 us, through L2 208; 852,640 x
 // 128 x 256 to fp32 121, 144).  Unaligned ones meet in L2 (32,768 x 4099 x 1024 to bf16
-// 144, past it 166).
+// 144, past it 166).  Small results gain too, also where the next launch reads them (calls in a
+// graph: 2048 x 2048 x 512 to fp32 8.6 us, through L2 9.7; 65,536 x 256 x 128 to bf16 11.6, 12.6;
+// 1024 x 1024 x 8192 with its splits' sums 22.0, 23.0; 4096 x 4096 x 512 to bf16 with a quantiser
+// behind it 24.1, 24.8); fp32 results that the last-level cache holds lose (8192 x 2048 x 512
+// 21.4, 20.7; 8192 x 4096 x 512 47.5, 42.2; 128 x 256 x 852,640 with 32 MB of splits' sums 66.3,
+// 63.9): the rule leaves that.
 template <bool PAST>
 __device__ __forceinline__ void store16(void* p, uint4 v) {
   typedef uint32_t u32x4 __attribute__((ext_vector_type(4), aligned(2)));
@@ -59,14 +64,19 @@ __device__ __forceinline__ void store16(void* p, uint4 v) {
 // a wave has read all of the step, whose buffer may be filled again, and waited for its own
 // loads of the next one.
 //
-// Measured: 32,768 x 4096 x 4096 to bf16 297 to 306 us (3.7 PFLOP/s; the library's
+// Measured: 32,768 x 4096 x 4096 to bf16 305 to 313 us (3.5 PFLOP/s; the library's
 // product of such matrices takes 531, and reaches 3.6 at 16,384 each way).  Power
 // bounds it: 1024 of a step's 1520 cycles are products, but at 1.5 GHz on random
 // numbers (2.2 on zeros: 0.71 us a step instead of 1.0; products alone, on what the
 // registers hold, 0.72 and 0.54).  A tile's filling takes 2.4 us, its results 3.6.  With
 // three buffers 128 x 128 has three blocks a CU: 852,640 x 128 x 256 to fp32 106 us (of
-// two blocks 121), 852,640 x 256 x 128 148 (6.3 TB/s).  Four waves of 128 x 128 took 355
-// us instead of 323, loads between the products 321.
+// two blocks 121), now in a graph of such calls 89 and between a layer's quantisers, which leave
+// the caches full, 111; 852,640 x 256 x 128 156 (6.0 TB/s) and 161; 128 x 256 x 852,640 in 247 parts
+// with their join 66 and 82 (its operands' rows are 426,320 bytes apart, so that in three of four
+// rows every second step's 64 bytes lie in two lines; at 426,368, a multiple of 128, 55).  Results that read aux or c take longer,
+// by 4 columns a lane: 852,640 x 128 x 256 with a ReLU's gradient 209 us (206 at the rate of a
+// copy), 32,768 x 4096 x 4096 503.  Four waves of 128 x 128 took 355 us instead of 323, loads
+// between the products 321.
 template <int WM, int WN, int TM, int TN, int NB, bool PAST>
 __global__ void __launch_bounds__(WM * WN * 64, TM * TN > 8 ? 1 : 2) k_matmul4_tile(Job4 J) {
   constexpr int BM = WM * TM * 32, BN = WN * TN * 32, NWV = WM * WN, ROWS = BM + BN;
@@ -357,8 +367,9 @@ __global__ void __launch_bounds__(WM * WN * 64, TM * TN > 8 ? 1 : 2) k_matmul4_t
 // A block takes TN times 16 rows of b, its 8 waves the steps of 256 columns in turn;
 // operands come straight from memory, 16 bytes a lane (four lanes cover a row's 128
 // columns, two loads its 128-byte line), a step ahead, and the waves' sums meet in LDS.
-// Measured: 1 x 4096 x 4096 4.2 us, 21 x 9001 x 6000 9.4 (188 blocks; 2.9 TB/s of weights that
-// the last-level cache holds), 32 x 14,336 x 4096 10.5.
+// Measured, in a graph of such calls: 1 x 4096 x 4096 4.6 us, 21 x 9001 x 6000 10.0 (188 blocks;
+// 2.9 TB/s of weights that the last-level cache holds), 32 x 14,336 x 4096 10.8; through the
+// binding 9.7 and under the profiler 10.5 for the second.
 template <int TM, int TN>
 __global__ void __launch_bounds__(512) k_matmul4_few(Job4 J) {
   constexpr int NWV = 8;
@@ -462,7 +473,11 @@ struct Plan {
 };
 
 // Which kernel, and into how many parts the sums are split: the least of what these
-// take by a model of their times (us), fitted to calls in a graph:
+// take by a model of their times (us), fitted to calls in a graph.  A tile's times have no
+// bytes in them: where memory bounds a call they are too short, which leaves the choice as it is
+// for many rows (852,640 x 128 x 256 57 expected, 89 measured; 852,640 x 256 x 128 93, 156; 128 x
+// 256 x 852,640 42, 66), and for a few rows takes tiles of wide and long weights (1 x 65,536 x 4096 25,
+// 34, which is 4 TB/s).
 //  * few rows: 3 and what all blocks read (their rows of b, and a each) at 6.2 TB/s
 //    (1 x 4096 x 4096 4.2, 32 x 4096 x 4096 6.4, 64 x 4096 x 4096 8.8, tiles 12.5; 21 x
 //    9001 x 6000 with 16, 32, 48 and 64 rows of b a block 12.9, 13.3, 9.5, 10.9; 64 x 8192
@@ -493,7 +508,9 @@ Plan plan(int64_t m, int64_t n, int64_t k) {
     r = {kBigTile, m2, n2, 0, 1, 0};
   }
   if (m <= kFewRows) {
-    // as many rows of b a block as leave it a CU of its own, up to what registers and LDS hold
+    // as many rows of b a block as leave it a CU of its own, up to what registers and LDS hold.
+    // For up to 16 rows of a and over 16,384 of b up to 32: 1 x 20,000 x 4096 11.4 us, with 64
+    // 14.6; 16 x 32,768 x 1024 8.1, 8.6; 16 x 65,536 x 1024 10.7, 15.0; but 1 x 32,768 x 4096 21, 17.0.
     const int64_t rows = m <= 16 ? 16 : m <= 32 ? 32 : 64, most = rows == 64 || (rows == 16 && n > 4 * 16 * kCUs) ? 2 : 4;
     const int64_t tn = std::min(ceil_div(ceil_div(n, 16), kCUs), most), nt = ceil_div(n, 16 * tn);
     if (3 + (double)nt * (rows + 16 * tn) * k / 2 / 6.2e6 < best)
