@@ -134,6 +134,46 @@ def test_group_norm_strides(dtype):
         assert (wide[:, :at] == 7).all() and (wide[:, at + cols:] == 7).all()
 
 
+@pytest.mark.parametrize("by", ["samples", "sample_ptr"])
+@pytest.mark.parametrize("n,groups,d", [(1 << 21, 2, 4), (1 << 17, 1024, 1)])
+def test_group_norm_most_samples(n, groups, d, by):
+    """The largest number of samples, and of samples times 32 groups.  Sums of 8 or 2 values, and
+    six roundings more, under 64 u of the magnitudes; xhat is off by u (|mean| rstd + 4 |xhat|).  A
+    column's sum is of 1024 samples a block (one of 2048) or 2731 (a 768th), 256 row lanes and 50
+    additions more."""
+    rows, cols, eps = 2 * n, groups * d, 1e-2
+    blocks, depth = (2048, 1330) if by == "samples" else (768, 3040)
+    x, dy = randn(rows, cols, seed=1), 0.7 + randn(rows, cols, seed=2)
+    g, b = 1 + 0.3 * randn(cols, seed=3), randn(cols, seed=4)
+
+    def split(v):
+        return v.double().view(n, 2, groups, d)
+
+    def mean_of(v):
+        return v.mean((1, 3), keepdim=True)
+    mean = mean_of(split(x))
+    rstd = 1 / torch.sqrt(mean_of((split(x) - mean) ** 2) + eps)
+    xhat = (split(x) - mean) * rstd
+    ex = U * (mean.abs() * rstd + 4 * xhat.abs())
+    gv, bv = g.double().view(1, 1, groups, d), b.double().view(1, 1, groups, d)
+    u = split(dy) * gv
+    m2 = mean_of(u * xhat)
+    dx = rstd * (u - mean_of(u) - xhat * m2)
+    tdx = rstd * (64 * U * (u.abs() + mean_of(u.abs()) + xhat.abs() * mean_of((u * xhat).abs())) + ex * m2.abs() +
+                  xhat.abs() * mean_of(u.abs() * ex))
+    with_ = dict(gamma=g, beta=b, eps=eps)
+    with_.update(samples=n) if by == "samples" else with_.update(sample_ptr=torch.arange(0, rows + 1, 2, dtype=torch.int32, device="cuda"))
+    y, st = mgn.mgn_group_norm_forward(x, groups, save=True, **with_)
+    r = mgn.mgn_group_norm_backward(x, st, dy, groups, **with_)
+    assert ((split(y) - xhat * gv - bv).abs() <= gv.abs() * ex + 4 * U * ((gv * xhat).abs() + bv.abs())).all()
+    assert ((split(r.dx) - dx).abs() <= tdx).all()
+    for got, v, e in ((r.dgamma, split(dy) * xhat, split(dy).abs() * ex), (r.dbeta, split(dy), 0 * ex)):
+        ref, tol = v.view(rows, cols).sum(0), depth * U * v.abs().view(rows, cols).sum(0) + e.view(rows, cols).sum(0)
+        assert ((got.double() - ref).abs() <= tol).all()
+    # a block's samples would be missed
+    assert (split(dy)[:n // blocks].sum((0, 1)).abs() > 2 * depth * U * split(dy).abs().sum((0, 1))).any()
+
+
 # ------------------------------------------- 256 x 256 products with an epilogue
 def values(m):
     q = torch.stack([m.q & 15, m.q >> 4], 2).flatten(1)[:, :m.cols].long()
