@@ -1161,7 +1161,10 @@ class TensorList:
     float32 or bfloat16 tensors of one device and any sizes, and, for clipping,
     the places of the clipped ones, as many tensors of the same sizes (out;
     None: the gradients themselves).  A program makes it once and keeps it; it
-    keeps its tensors, whose values may change but not their places."""
+    keeps its tensors, whose values may change but not their places.  Making it copies
+    its table to the device and waits for that (75 us for 6 tensors, 1.2 ms for 290 of 300 M
+    elements), so not while a graph is captured; where every step's gradients are new
+    tensors, every step pays for it."""
 
     def __init__(self, tensors, out=None):
         torch = _torch()
